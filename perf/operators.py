@@ -328,14 +328,14 @@ def _framework(s):
     op = c["op"]
     where = {"page_size": max(1, c["page"]), "block_table": s["table"], "N": c["N"]}
     if op == "store":
-        sts.sts_kv4_store(s["k"], s["v"], s["codes"], s["scales"], pos=s["pos"], lens=s["lens"], **where)
-        return sts.sts_kv4_load(s["codes"], s["scales"], c["T"], pos=s["pos"], lens=s["lens"], out=(s["k_out"], s["v_out"]), **where)
+        sts.sts_packed_store(s["k"], s["v"], s["codes"], s["scales"], pos=s["pos"], lens=s["lens"], **where)
+        return sts.sts_packed_load(s["codes"], s["scales"], c["T"], pos=s["pos"], lens=s["lens"], out=(s["k_out"], s["v_out"]), **where)
     if op == "load":
-        return sts.sts_kv4_load(s["codes"], s["scales"], c["N"], **where)
+        return sts.sts_packed_load(s["codes"], s["scales"], c["N"], **where)
     if "call" not in s:      # a serving loop builds the call on its buffers once
         new = {"seq_lens": s["lens"], "k_new": s["k_new"], "v_new": s["v_new"], "prepare": True, **where}
         if op == "attn4":
-            s["call"] = sts.sts_kv4_attn(s["q"], s["codes"], s["scales"], s["scale"], indices=s["idx"], counts=s["cnt"], head_map=s["head_map"], **new)
+            s["call"] = sts.sts_packed_attn(s["q"], s["codes"], s["scales"], s["scale"], indices=s["idx"], counts=s["cnt"], head_map=s["head_map"], **new)
         else:
             s["call"] = sts.sts_window_attn(s["q"], s["k"], s["v"], s["scale"], c["window"], sinks=c["sinks"], **new)
     return s["call"]()
