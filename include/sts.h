@@ -288,6 +288,119 @@ sts_status sts_dense_attn(const sts_attn_params *p, void *stream);
 #define STS_STATIC_SCRATCH_BYTES ((size_t)8 << 20)
 sts_status sts_sparse_attn_static(const sts_attn_params *p, void *stream);
 
+/* ----------------------------------------------------------------------------------------
+ * A cache held in 4 bits (paper Section 2.3 keeps the full cache, whose size Section 6.2 has to move to
+ * host memory: at 4.25 bits a value it takes 0.27 of the bf16 cache's bytes). Per token and KV head `codes` hold d/2
+ * bytes for K, then d/2 for V, two values to a byte (the even channel in the low half): a sign in
+ * the top bit and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6. `scales` hold one byte s for every 32
+ * neighbouring channels, d/32 for K, then d/32 for V: the codes stand for their number times 2^(s-127), and all 32
+ * for NaN where s is 255. (These are the e2m1 and e8m0 types of the OCP microscaling formats.)
+ *
+ * Token n of batch element b and KV head g lies at b*stride_b + g*stride_h + n*stride_n of either
+ * array (byte strides); with block_table, at page*stride_page + g*stride_h + (n % page_size)*stride_n with
+ * page = block_table[b, n / page_size] (clamped into [0, num_pages)).
+ *
+ * Supported: d in {64,128}; page_size 1, 2, 4, 8, 16 or 32; codes 16-byte aligned with strides that are
+ * multiples of 16, scales aligned to d/16 with strides that are multiples of it, stride_n at least a token's
+ * bytes (d codes, d/16 scales). Tokens, heads, batch elements and pages must not overlap where the cache is
+ * written to.
+ */
+typedef struct {
+  uint8_t *codes;           /* [dev] */
+  uint8_t *scales;          /* [dev] */
+  int64_t code_stride_b, code_stride_h, code_stride_n, code_stride_page;       /* bytes */
+  int64_t scale_stride_b, scale_stride_h, scale_stride_n, scale_stride_page;
+  const int32_t *block_table; /* [dev] [B, table_stride], or NULL (contiguous; stride_page is ignored) */
+  int32_t table_stride;     /* entries per batch row, >= ceil(N / page_size) */
+  int32_t num_pages;        /* pages in the pool (paged only) */
+  int32_t page_size;        /* 0 or 1, or tokens per page / per index entry */
+  int32_t N;                /* tokens per batch element */
+} sts_packed_cache;
+
+/* sts_packed_store -- T rows of K and V per batch element into the cache, at positions pos[b] .. pos[b] + T - 1.
+ * Every group of 32 channels takes the smallest power of two 2^e, -125 <= e <= 125, with max|x| <= 7 * 2^e (so no value
+ * is off by more than half a step, saturation at 6 included) and rounds x / 2^e to the nearest code, ties to the even
+ * one. A group with a NaN or an infinity becomes NaN as a whole. Rows i >= lens[b], and positions outside
+ * [0, N), are not stored; nothing else of the cache is written to. Two rows of one call must not name the same
+ * place (pages shared between batch elements, for instance).
+ *
+ * sts_packed_load -- the same rows of the cache as the bf16 values they stand for (exact). Rows i >= lens[b] of the
+ * outputs stay as they were; rows at positions outside [0, N) become 0.
+ */
+typedef struct {
+  int32_t B, T, Hkv, d;
+  void *k, *v;              /* [dev] bf16 [B,T,Hkv,d] contiguous, 16-byte aligned; read by the store, written by the load */
+  const int32_t *pos;       /* [dev] [B] position of row 0, or NULL (0) */
+  const int32_t *lens;      /* [dev] [B] rows that hold tokens (padded batches), or NULL (T) */
+  sts_packed_cache cache;
+} sts_packed_rows_params;
+
+/* sts_packed_attn -- sts_sparse_attn (indices given) or sts_dense_attn (indices NULL) over the 4-bit cache: the formulas,
+ * lists, blocks, pages and the block's own tokens of sts_attn_params with K and V the values that the cache stands for.
+ * The products are bf16 with fp32 sums; the cached values are exact in bf16. Fields as there.
+ */
+typedef struct {
+  int32_t B, Tq, Hq, Hkv, d;
+  const void *q;            /* [dev] bf16 [B,Tq,Hq,d] contiguous */
+  sts_packed_cache cache;      /* only read */
+  const int32_t *indices;   /* [dev] [B,Hq,kmax], or NULL: all tokens */
+  const int32_t *counts;    /* [dev] [B,Hq] or NULL (lists only) */
+  int32_t kmax;
+  const int32_t *head_map;  /* [host] optional hint [Hq] (lists only) */
+  const int32_t *seq_lens;  /* [dev] [B] or NULL (without lists only) */
+  float scale;
+  void *out;                /* [dev] [B,Tq,Hq,d] of out_dtype */
+  int32_t out_dtype;
+  float *lse_out;           /* [dev] optional [B,Hq,Tq] */
+  const void *k_new, *v_new; /* [dev] optional bf16 [B,Tq,Hkv,d] contiguous (not quantised) */
+  int32_t causal;
+  int64_t idx_stride_b, cnt_stride_b;
+  void *workspace;          /* [dev] 256-byte aligned scratch */
+  size_t workspace_bytes;
+} sts_packed_attn_params;
+
+/* ----------------------------------------------------------------------------------------
+ * sts_window_attn -- attention with a sliding window and a few first tokens that stay visible
+ * (attention sinks; the paper compares with such a policy in Section 6.1, and layers whose sparsity it
+ * finds too low for lists need one that no draft decides), over a bf16 cache.
+ *
+ * Query row i of batch element b stands at position p_i: without k_new the block's own tokens are the
+ * cache's last, p_i = L_b - Tq + i; with k_new they are not in the cache yet, p_i = L_b + i, and
+ * row i also attends to the new tokens 0..i. A cached token n < L_b is visible to row i iff
+ *     n <= p_i  and  (n < sinks  or  n > p_i - window).
+ * Otherwise the formulas of sts_dense_attn. Rows at negative positions (a padded batch: L_b < Tq) and rows that see
+ * nothing give out = 0 and lse = -inf. Tq may be a whole prompt; window >= L_b is plain causal attention.
+ *
+ * Supported: d in {64,128}; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; Tq >= 1, with k_new Tq <= 16 and window >= Tq;
+ * window >= 1, sinks >= 0; kv strides as in sts_attn_params; page_size 1, 2, 4, 8, 16 or 32.
+ */
+typedef struct {
+  int32_t B, Tq, Hq, Hkv, d, N;
+  const void *q;            /* [dev] bf16 [B,Tq,Hq,d] contiguous */
+  const void *k, *v;        /* [dev] bf16 [B,Hkv,N,d], or pools of pages (block_table) */
+  int64_t kv_stride_b, kv_stride_h, kv_stride_n;   /* in elements, shared by k and v */
+  const int32_t *seq_lens;  /* [dev] [B] L_b <= N, or NULL (N) */
+  int32_t window, sinks;
+  float scale;
+  void *out;                /* [dev] [B,Tq,Hq,d] of out_dtype */
+  int32_t out_dtype;
+  float *lse_out;           /* [dev] optional [B,Hq,Tq] */
+  int32_t page_size;
+  const int32_t *block_table; /* [dev] [B, table_stride] or NULL */
+  int32_t table_stride, num_pages;
+  int64_t kv_stride_page;
+  const void *k_new, *v_new; /* [dev] optional bf16 [B,Tq,Hkv,d] contiguous */
+  void *workspace;          /* [dev] 256-byte aligned scratch */
+  size_t workspace_bytes;
+} sts_window_params;
+
+sts_status sts_packed_store(const sts_packed_rows_params *p, void *stream);
+sts_status sts_packed_load(const sts_packed_rows_params *p, void *stream);
+size_t sts_packed_attn_workspace_bytes(const sts_packed_attn_params *p);
+sts_status sts_packed_attn(const sts_packed_attn_params *p, void *stream);
+size_t sts_window_attn_workspace_bytes(const sts_window_params *p);
+sts_status sts_window_attn(const sts_window_params *p, void *stream);
+
 const char *sts_strerror(int status);   /* any int: values that are no sts_status give "unknown status" */
 int sts_version(void);
 
@@ -320,7 +433,11 @@ typedef enum {
   STS_K_SELECT_FUSED = 14, /* long rows: sample, aggregation, threshold and compaction in one launch */
   STS_K_UNION_ROWS = 15,   /* union of per-row index lists + row bits */
   STS_K_SELECT_BAND = 16,  /* the same with a row for every second compute unit or more (clearing included) */
-  STS_K_COUNT_ = 17
+  STS_K_PACKED_STORE = 17,    /* bf16 rows -> 4-bit cache */
+  STS_K_PACKED_LOAD = 18,     /* rows of the 4-bit cache -> bf16 */
+  STS_K_PACKED_ATTN = 19,     /* split attention over a 4-bit cache */
+  STS_K_WINDOW = 20,       /* attention with a sliding window and sinks (short blocks and prompts) */
+  STS_K_COUNT_ = 21
 } sts_kernel_kind;
 #define STS_PROF_MAX 4096
 

@@ -21,14 +21,17 @@ STS_BF16, STS_F32 = 0, 1
 KERNEL_KINDS = {"select_clear": 0, "select_agg": 1, "select_hist": 2, "select_rowpass": 3,
                 "select_write": 4, "attn_sparse": 5, "attn_dense": 6, "attn_combine": 7, "select_block": 8,
                 "headmap": 9, "select_small": 10, "select_local": 11, "select_pool": 12,
-                "attn_probsum": 13, "select_fused": 14, "union_rows": 15, "select_band": 16}
+                "attn_probsum": 13, "select_fused": 14, "union_rows": 15, "select_band": 16, "packed_store": 17,
+                "packed_load": 18, "packed_attn": 19, "window": 20}
 KNOBS = {"attn_wgs_per_cu": 0, "select_spin_limit": 1, "probsum_wgs_per_cu": 2, "select_path": 3, "select_row_threads": 4}
 
 # every symbol include/sts.h declares
 EXPORTS = ["sts_select_workspace_bytes", "sts_attn_workspace_bytes", "sts_select", "sts_sparse_attn",
            "sts_dense_attn", "sts_strerror", "sts_version", "sts_prof_enable", "sts_prof_reset",
            "sts_prof_read", "sts_attn_plan", "sts_head_map", "sts_headmap_workspace_bytes",
-           "sts_sparse_attn_static", "sts_set_knob", "sts_get_knob", "sts_union_rows"]
+           "sts_sparse_attn_static", "sts_set_knob", "sts_get_knob", "sts_union_rows", "sts_packed_store",
+           "sts_packed_load", "sts_packed_attn", "sts_packed_attn_workspace_bytes", "sts_window_attn",
+           "sts_window_attn_workspace_bytes"]
 STS_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -78,6 +81,45 @@ class HeadmapParams(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+class PackedCache(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("code_stride_b", ctypes.c_int64), ("code_stride_h", ctypes.c_int64),
+                ("code_stride_n", ctypes.c_int64), ("code_stride_page", ctypes.c_int64),
+                ("scale_stride_b", ctypes.c_int64), ("scale_stride_h", ctypes.c_int64),
+                ("scale_stride_n", ctypes.c_int64), ("scale_stride_page", ctypes.c_int64),
+                ("block_table", ctypes.c_void_p), ("table_stride", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("N", ctypes.c_int32)]
+
+
+class PackedRowsParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("cache", PackedCache)]
+
+
+class PackedAttnParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Tq", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("q", ctypes.c_void_p), ("cache", PackedCache),
+                ("indices", ctypes.c_void_p), ("counts", ctypes.c_void_p), ("kmax", ctypes.c_int32),
+                ("head_map", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("scale", ctypes.c_float),
+                ("out", ctypes.c_void_p), ("out_dtype", ctypes.c_int32), ("lse_out", ctypes.c_void_p),
+                ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p), ("causal", ctypes.c_int32),
+                ("idx_stride_b", ctypes.c_int64), ("cnt_stride_b", ctypes.c_int64),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class WindowParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Tq", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("N", ctypes.c_int32), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("kv_stride_b", ctypes.c_int64), ("kv_stride_h", ctypes.c_int64),
+                ("kv_stride_n", ctypes.c_int64), ("seq_lens", ctypes.c_void_p), ("window", ctypes.c_int32),
+                ("sinks", ctypes.c_int32), ("scale", ctypes.c_float), ("out", ctypes.c_void_p),
+                ("out_dtype", ctypes.c_int32), ("lse_out", ctypes.c_void_p), ("page_size", ctypes.c_int32),
+                ("block_table", ctypes.c_void_p), ("table_stride", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("kv_stride_page", ctypes.c_int64), ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -118,6 +160,15 @@ def load_library():
     lib.sts_attn_plan.argtypes = [ctypes.POINTER(AttnParams), ctypes.c_int] + [ctypes.POINTER(ctypes.c_int32)] * 3
     lib.sts_union_rows.restype = ctypes.c_int
     lib.sts_union_rows.argtypes = [ctypes.POINTER(UnionParams), ctypes.c_void_p]
+    for f in (lib.sts_packed_store, lib.sts_packed_load):
+        f.restype = ctypes.c_int
+        f.argtypes = [ctypes.POINTER(PackedRowsParams), ctypes.c_void_p]
+    for f, s, params in ((lib.sts_packed_attn, lib.sts_packed_attn_workspace_bytes, PackedAttnParams),
+                         (lib.sts_window_attn, lib.sts_window_attn_workspace_bytes, WindowParams)):
+        f.restype = ctypes.c_int
+        f.argtypes = [ctypes.POINTER(params), ctypes.c_void_p]
+        s.restype = ctypes.c_size_t
+        s.argtypes = [ctypes.POINTER(params)]
     lib.sts_set_knob.restype = None
     lib.sts_set_knob.argtypes = [ctypes.c_int, ctypes.c_double]
     lib.sts_get_knob.restype = ctypes.c_double
@@ -447,6 +498,203 @@ def sts_dense_attn(q, k, v, scale, seq_lens=None, out=None, out_dtype=None, want
                      lse_out=lse_out, logits_out=logits_out, page_size=page_size,
                      block_table=block_table, N=N, k_new=k_new, v_new=v_new, causal=causal,
                      weights_sum_out=weights_sum_out, prepare=prepare)
+
+
+def _packed_cache(codes, scales, page_size, block_table, N, B=None):
+    """The cache block of the 4-bit calls -> (block, Hkv, d, B). codes [B,Hkv,N,2,d/2], scales [B,Hkv,N,2,d/32] uint8, or pools
+    [pages,Hkv,page_size,2,...] with a block table [B,T]; any strides on the first three dimensions."""
+    import torch
+
+    _current(codes.device)
+    assert codes.device == scales.device
+    assert codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and codes.dim() == 5
+    rooms, Hkv, slots, two, dh = codes.shape
+    assert two == 2 and tuple(scales.shape) == (rooms, Hkv, slots, 2, dh // 16) and dh % 16 == 0
+    for t in (codes, scales):
+        assert t.stride(4) == 1 and t.stride(3) == t.shape[4], "a token's K and V lie next to each other"
+    if block_table is None:
+        assert B is None or B == rooms
+        N = slots if N is None else N
+        assert 0 <= N <= slots
+        B, ts, pages = rooms, 0, 0
+        cb, cp, sb, sp = codes.stride(0), 0, scales.stride(0), 0
+    else:
+        assert slots == page_size and N is not None, "a paged cache has page_size slots per page and needs the length bound N"
+        assert block_table.device == codes.device and block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous()
+        assert B is None or B == block_table.shape[0]
+        B, ts, pages = block_table.shape[0], block_table.shape[1], rooms
+        cb, cp, sb, sp = 0, codes.stride(0), 0, scales.stride(0)
+    c = PackedCache(codes=_ptr(codes), scales=_ptr(scales), code_stride_b=cb, code_stride_h=codes.stride(1), code_stride_n=codes.stride(2),
+                    code_stride_page=cp, scale_stride_b=sb, scale_stride_h=scales.stride(1), scale_stride_n=scales.stride(2),
+                    scale_stride_page=sp, block_table=_ptr(block_table), table_stride=ts, num_pages=pages, page_size=int(page_size), N=int(N))
+    return c, Hkv, 2 * dh, B
+
+
+def _current(dev):
+    """Calls go to the current device's stream: tensors of another device are refused."""
+    import torch
+
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise StsError(f"tensors on {dev}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _per_batch(t, B, dev):
+    """Pointer of an optional int32 [B] tensor."""
+    import torch
+
+    if t is None:
+        return None
+    assert t.device == dev and t.dtype == torch.int32 and tuple(t.shape) == (B,) and t.is_contiguous()
+    return t.data_ptr()
+
+
+def sts_packed_store(k, v, codes, scales, pos=None, lens=None, page_size=1, block_table=None, N=None):
+    """Rows k, v [B,T,Hkv,d] bf16 into the 4-bit cache (codes [B,Hkv,N,2,d/2], scales [B,Hkv,N,2,d/32] uint8, or pools of pages
+    with a block table), at positions pos[b] + 0 .. T-1 (pos None: 0); only the first lens[b] rows. See sts_packed_store
+    in include/sts.h."""
+    import torch
+
+    lib = load_library()
+    B, T, Hkv, d = k.shape
+    cache, ch, cd, _ = _packed_cache(codes, scales, page_size, block_table, N, B)
+    assert (ch, cd) == (Hkv, d)
+    for t in (k, v):
+        assert t.device == codes.device and t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == (B, T, Hkv, d)
+    p = PackedRowsParams(B=B, T=T, Hkv=Hkv, d=d, k=_ptr(k), v=_ptr(v), pos=_per_batch(pos, B, k.device), lens=_per_batch(lens, B, k.device), cache=cache)
+    _check(lib.sts_packed_store(ctypes.byref(p), _stream()), "sts_packed_store")
+
+
+def sts_packed_load(codes, scales, T: int, pos=None, lens=None, page_size=1, block_table=None, N=None, out=None):
+    """Rows pos[b] + 0 .. T-1 of the 4-bit cache as the bf16 values they stand for -> (k, v) [B,T,Hkv,d]. Rows from lens[b] on stay
+    as they are in `out` (zeros without one). See sts_packed_load in include/sts.h."""
+    import torch
+
+    lib = load_library()
+    cache, Hkv, d, B = _packed_cache(codes, scales, page_size, block_table, N)
+    if out is None:
+        make = torch.empty if lens is None else torch.zeros
+        out = tuple(make(B, T, Hkv, d, dtype=torch.bfloat16, device=codes.device) for _ in range(2))
+    k, v = out
+    for t in (k, v):
+        assert t.device == codes.device and t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == (B, T, Hkv, d)
+    p = PackedRowsParams(B=B, T=int(T), Hkv=Hkv, d=d, k=_ptr(k), v=_ptr(v), pos=_per_batch(pos, B, k.device), lens=_per_batch(lens, B, k.device), cache=cache)
+    _check(lib.sts_packed_load(ctypes.byref(p), _stream()), "sts_packed_load")
+    return k, v
+
+
+def _outputs(q, out, out_dtype, want_lse, lse_out):
+    """The output tensors of an attention call on q [B,Tq,Hq,d]: given ones are checked, missing ones made."""
+    import torch
+
+    _current(q.device)
+    assert q.dtype == torch.bfloat16 and q.is_contiguous() and q.dim() == 4
+    B, Tq, Hq, d = q.shape
+    if out is None:
+        out = torch.empty(B, Tq, Hq, d, dtype=out_dtype or torch.bfloat16, device=q.device)
+    assert out.device == q.device and out.dtype in (torch.bfloat16, torch.float32) and out.is_contiguous() and out.shape == q.shape
+    if lse_out is None and want_lse:
+        lse_out = torch.empty(B, Hq, Tq, dtype=torch.float32, device=q.device)
+    assert lse_out is None or (lse_out.device == q.device and lse_out.dtype == torch.float32 and lse_out.is_contiguous() and tuple(lse_out.shape) == (B, Hq, Tq))
+    return out, lse_out
+
+
+def _new_rows(q, Hkv, k_new, v_new):
+    import torch
+
+    B, Tq, _, d = q.shape
+    assert (k_new is None) == (v_new is None)
+    for t in (k_new, v_new):
+        assert t is None or (t.device == q.device and t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == (B, Tq, Hkv, d))
+
+
+def _run_with_workspace(fn, size, p, what, tag, workspace, dev, result, keep, prepare):
+    import torch
+
+    ws = workspace
+    if ws is None:
+        need = size(ctypes.byref(p))
+        # A prepared call has a workspace of its own, and so has a call that is captured into a graph (it lives in the graph's
+        # pool): such calls may run at the same time, on other streams than this one.
+        if prepare or torch.cuda.is_current_stream_capturing():
+            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        else:
+            ws = _workspace(tag, need, dev)
+    p.workspace, p.workspace_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
+    if prepare:       # build once, launch many times (see PreparedCall)
+        return PreparedCall(fn, p, what, result, (keep, ws))
+    _check(fn(ctypes.byref(p), _stream()), what)
+    return result
+
+
+def sts_packed_attn(q, codes, scales, scale, indices=None, counts=None, head_map=None, seq_lens=None, out=None, out_dtype=None,
+                    want_lse=True, workspace=None, lse_out=None, page_size=1, block_table=None, N=None, k_new=None, v_new=None,
+                    causal=True, prepare=False):
+    """Attention over a 4-bit cache (see sts_packed_store): all tokens, or the rows that indices [B,Hq,kmax] name, as in
+    sts_dense_attn and sts_sparse_attn -> (out [B,Tq,Hq,d], lse [B,Hq,Tq]). prepare=True returns a PreparedCall."""
+    import torch
+
+    lib = load_library()
+    out, lse = _outputs(q, out, out_dtype, want_lse, lse_out)
+    B, Tq, Hq, d = q.shape
+    cache, Hkv, cd, _ = _packed_cache(codes, scales, page_size, block_table, N, B)
+    assert cd == d and codes.device == q.device
+    _new_rows(q, Hkv, k_new, v_new)
+    kmax = isb = csb = 0
+    if indices is not None:
+        # [B,Hq,kmax], rows contiguous; the batch stride may be wider (a slice of heads of a wider list)
+        assert indices.device == q.device and indices.dtype == torch.int32 and indices.dim() == 3 and tuple(indices.shape[:2]) == (B, Hq)
+        kmax = indices.shape[2]
+        assert kmax == 0 or (indices.stride(2) == 1 and (Hq == 1 or indices.stride(1) == kmax))
+        isb = indices.stride(0) if B > 1 else 0
+        if kmax == 0:           # empty lists: a tensor without elements has no address, and none is read
+            indices, isb = out, 0
+    else:
+        assert counts is None and head_map is None
+    if counts is not None:
+        assert counts.device == q.device and counts.dtype == torch.int32 and tuple(counts.shape) == (B, Hq)
+        assert Hq == 1 or counts.stride(1) == 1
+        csb = counts.stride(0) if B > 1 else 0
+    hm = _host_i32(head_map) if head_map is not None else None
+    assert hm is None or len(hm) == Hq
+    p = PackedAttnParams(B=B, Tq=Tq, Hq=Hq, Hkv=Hkv, d=d, q=_ptr(q), cache=cache, indices=_ptr(indices), counts=_ptr(counts), kmax=kmax,
+                         head_map=ctypes.cast(hm, ctypes.c_void_p) if hm is not None else None, seq_lens=_per_batch(seq_lens, B, q.device),
+                         scale=float(scale), out=_ptr(out), out_dtype=STS_BF16 if out.dtype == torch.bfloat16 else STS_F32, lse_out=_ptr(lse),
+                         k_new=_ptr(k_new), v_new=_ptr(v_new), causal=1 if causal else 0, idx_stride_b=isb, cnt_stride_b=csb)
+    return _run_with_workspace(lib.sts_packed_attn, lib.sts_packed_attn_workspace_bytes, p, "sts_packed_attn", "attn", workspace, q.device, (out, lse),
+                               (q, codes, scales, indices, counts, seq_lens, block_table, k_new, v_new, hm), prepare)
+
+
+def sts_window_attn(q, k, v, scale, window: int, sinks: int = 0, seq_lens=None, out=None, out_dtype=None, want_lse=True, workspace=None,
+                    lse_out=None, page_size=1, block_table=None, N=None, k_new=None, v_new=None, prepare=False):
+    """Attention with a sliding window of `window` tokens and `sinks` first tokens that stay visible, q [B,Tq,Hq,d] bf16, k/v
+    [B,Hkv,N,d] bf16 (strided ok) or pools of pages -> (out [B,Tq,Hq,d], lse [B,Hq,Tq]). Without k_new the block's own tokens
+    are the last Tq of the seq_lens[b] (N) cached ones. See sts_window_attn in include/sts.h."""
+    import torch
+
+    lib = load_library()
+    out, lse = _outputs(q, out, out_dtype, want_lse, lse_out)
+    B, Tq, Hq, d = q.shape
+    for t in (k, v):
+        assert t.device == q.device and t.dtype == torch.bfloat16 and t.dim() == 4
+    assert v.shape == k.shape and v.stride() == k.stride() and k.stride(3) == 1 and k.shape[3] == d
+    rooms, Hkv, slots, _ = k.shape
+    sb, sp, pages, ts = k.stride(0), 0, 0, 0
+    if block_table is None:
+        assert rooms == B
+        N = slots if N is None else N
+        assert 0 <= N <= slots
+    else:
+        assert slots == page_size and N is not None, "a paged cache has page_size slots per page and needs the length bound N"
+        assert block_table.device == q.device and block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.dim() == 2
+        assert block_table.shape[0] == B
+        sb, sp, pages, ts = 0, k.stride(0), rooms, block_table.shape[1]
+    _new_rows(q, Hkv, k_new, v_new)
+    p = WindowParams(B=B, Tq=Tq, Hq=Hq, Hkv=Hkv, d=d, N=int(N), q=_ptr(q), k=_ptr(k), v=_ptr(v), kv_stride_b=sb, kv_stride_h=k.stride(1),
+                     kv_stride_n=k.stride(2), seq_lens=_per_batch(seq_lens, B, q.device), window=int(window), sinks=int(sinks), scale=float(scale),
+                     out=_ptr(out), out_dtype=STS_BF16 if out.dtype == torch.bfloat16 else STS_F32, lse_out=_ptr(lse), page_size=int(page_size),
+                     block_table=_ptr(block_table), table_stride=ts, num_pages=pages, kv_stride_page=sp, k_new=_ptr(k_new), v_new=_ptr(v_new))
+    return _run_with_workspace(lib.sts_window_attn, lib.sts_window_attn_workspace_bytes, p, "sts_window_attn", "attn", workspace, q.device, (out, lse),
+                               (q, k, v, seq_lens, block_table, k_new, v_new), prepare)
 
 
 def sts_head_map(a_d, a_t, k: int, workspace=None):

@@ -132,40 +132,15 @@ int page_of(const sts_attn_params *p) { return p->page_size <= 1 ? 1 : p->page_s
 sts_status plan_attn(const sts_attn_params *p, int sparse, AttnPlan &pl) {
   const sts_status v = validate_attn(p, sparse);
   if (v != STS_OK) return v;
-  const int G = p->Hq / p->Hkv;
   // at most 4 query tiles of 16 rows per unit; 2 for the logits dump at head size 128, whose
   // four-tile form would not fit the register file (a KV group with more rows is served by two
   // units, each reading K and V: next to the dump's own writes that costs little)
   int max_heads = ((!sparse && p->logits_out && p->d == 128) ? 32 : 64) / p->Tq;
   if (max_heads < 1) max_heads = 1;
   if (max_heads > STS_MAX_GROUP) max_heads = STS_MAX_GROUP;
-  int nu = 0, max_rows = 0;
-  memset(&pl.units, 0, sizeof(pl.units));
-  for (int g = 0; g < p->Hkv; ++g) {
-    bool done[STS_MAX_GROUP] = {false};
-    for (int i = 0; i < G; ++i) {
-      if (done[i]) continue;
-      // members of the set led by head i, in head order
-      int members[STS_MAX_GROUP], nm = 0;
-      for (int j2 = i; j2 < G; ++j2) {
-        if (done[j2]) continue;
-        const bool same = !sparse || j2 == i ||
-                          (p->head_map && p->head_map[g * G + j2] == p->head_map[g * G + i]);
-        if (same) {
-          members[nm++] = j2;
-          done[j2] = true;
-        }
-      }
-      for (int s0 = 0; s0 < nm; s0 += max_heads) {
-        const int cnt = (nm - s0 < max_heads) ? nm - s0 : max_heads;
-        uint32_t mask = 0;
-        for (int m = 0; m < cnt; ++m) mask |= 1u << members[s0 + m];
-        if (nu >= STS_MAX_HEADS) return STS_EUNSUPPORTED;
-        pl.units.unit[nu++] = (uint32_t)g | (mask << 8) | ((uint32_t)cnt << 24);
-        if (cnt * p->Tq > max_rows) max_rows = cnt * p->Tq;
-      }
-    }
-  }
+  int max_rows = 0;
+  const int nu = sts_group_units(p->Hq, p->Hkv, p->Tq, max_heads, sparse ? p->head_map : nullptr, !sparse, pl.units, max_rows);
+  if (nu < 0) return STS_EUNSUPPORTED;
   pl.num_units = nu;
   pl.nq = max_rows <= 16 ? 1 : (max_rows <= 32 ? 2 : 4);
   const int64_t len = sparse ? (int64_t)p->kmax * page_of(p) : p->N;
@@ -580,6 +555,11 @@ sts_status plan_select(const sts_select_params *p, SelectPlan &pl) {
 }
 
 }  // namespace
+
+hipError_t sts_run_launch(int kind, hipStream_t s, hipError_t (*launch)(void *), void *with) {
+  return run_kernel(kind, s, [&] { return launch(with); });
+}
+int sts_cu_count() { return cu_count(); }
 
 extern "C" {
 

@@ -1,0 +1,580 @@
+// Split attention of short query blocks (up to 16 rows) over a cache of one of two forms (gfx950): held in 4 bits
+// (sts_packed_attn: all tokens, or index lists), or bf16 with a sliding window and sinks (sts_window_attn).
+//
+// Units, splits and partials are those of the bf16 kernels (attn.hip), whose combine kernel merges the splits and appends
+// the block's own tokens. One workgroup of four waves per (batch, unit, split); waves take alternating tiles of 32 keys
+// and keep an online softmax of their own, with maximum, sum and accumulators in fp32.
+//
+// Tiles in the transposed orientation, S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x32_bf16, lane (a, b) =
+// (lane / 16, lane % 16). Which key a row of K's operand holds is free, so row 4a + i of half h is the tile's key
+// a + 4i + 16h. Then
+//   - lane (a, b) ends up with the scores of keys a + 4m, m = 0..7, of query b, which is what it has to supply as the B
+//     operand of the second product: P stays in its lane;
+//   - V's rows for it are a + 4m, so that the four lane groups load four neighbouring rows at a time;
+//   - K's operand is loaded as it is used, a lane's share of one key's row: no LDS, no exchange. Of a row of 4-bit codes
+//     lane a has the a-th quarter, 16 bytes at head size 128 and one scale; of a bf16 row every fourth chunk of 16 bytes.
+// The codes become bf16 pairs in the chip's conversion, scale included, exactly. V's pairs are two channels of one key and have to
+// become two keys of one channel: two byte permutes per pair of registers, as for bf16.
+// Scales: a lane loads the word of one token of the tile, K's in the lower half of the wave, V's in the upper, makes
+// them the floats that the conversion takes, and the lanes pick theirs up from LDS, one tile ahead of their use.
+#include "cache.h"
+
+namespace {
+
+// position of the n-th set bit (n < popcount) of a mask that is the same for all lanes, nearly always one run of bits
+__device__ __forceinline__ int nth_member(uint32_t mask, int n) {
+  const int first = __builtin_ctz(mask);
+  const uint32_t run = mask >> first;
+  if ((run & (run + 1)) == 0) return first + n;
+  int pos = 0;
+#pragma unroll
+  for (int i = 0; i < STS_MAX_GROUP; ++i) {
+    const bool set = (mask >> i) & 1u;
+    if (set && n == 0) pos = i;
+    n -= set ? 1 : 0;
+  }
+  return pos;
+}
+
+// the larger of two numbers in one instruction (see attn.hip)
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
+
+// maximum over the four lanes 16 apart
+__device__ __forceinline__ float max_over_groups(float x) {
+  const uint32_t w = __builtin_bit_cast(uint32_t, x);
+  const auto p = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+  const float y = larger(__builtin_bit_cast(float, (uint32_t)p[0]), __builtin_bit_cast(float, (uint32_t)p[1]));
+  const uint32_t v = __builtin_bit_cast(uint32_t, y);
+  const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return larger(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
+}
+
+// a lane's share of a row: K's quarter and V's D / 16 channels
+template <int D, bool FOUR> struct Share;
+template <> struct Share<128, true> { typedef u32x4 k; typedef uint32_t v; };
+template <> struct Share<64, true> { typedef u32x2 k; typedef uint16_t v; };
+template <> struct Share<128, false> { typedef u32x4 k; typedef u32x4 v; };
+template <> struct Share<64, false> { typedef u32x4 k; typedef u32x2 v; };
+
+template <int D, int NQ, bool FOUR> constexpr int tiles_ahead() { return FOUR ? 3 : 2; }
+
+__device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale, int byte) {
+  switch (byte) {
+    case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+  }
+}
+
+// FOUR: a 4-bit cache without a window, else a bf16 cache with one. GATHER: the rows come from a list or a page
+// table, at offsets of 64 bits (FAR) or 32.
+template <int D, int NQ, bool FOUR, bool GATHER, bool FAR>
+__global__ void __launch_bounds__(64 * STS_WG_WAVES, NQ == 4 || (!FOUR && D == 128) ? 1 : 2) cache_attn_kernel(const CacheAttnArgs C) {
+  typedef typename Share<D, FOUR>::k k_t;
+  typedef typename Share<D, FOUR>::v v_t;
+  typedef typename std::conditional<FAR, uint64_t, uint32_t>::type off_t;
+  constexpr int W = STS_WG_WAVES, TK = STS_TILE_KEYS, PF = tiles_ahead<D, NQ, FOUR>();
+  constexpr int NT = D / 16, KK = D / 32;
+  constexpr int KL = FOUR ? 1 : KK;              // loads of K per lane and half tile
+  constexpr int OPITCH = D + 4;
+  constexpr bool WIN = !FOUR;
+  constexpr bool QLDS = NQ >= 2;
+  __shared__ __attribute__((aligned(16))) float lds_o[W * 16 * OPITCH];
+  __shared__ float lds_ml[W][NQ * 16][2];
+  __shared__ __attribute__((aligned(16))) u32x4 lds_q[QLDS ? NQ * KK * 64 : 1];
+  __shared__ __attribute__((aligned(16))) off_t lds_off[GATHER ? W : 1][2][TK];                // by (slot % 4) * 8 + slot / 4
+  __shared__ __attribute__((aligned(16))) uint32_t lds_sc[FOUR ? W : 1][2][2][D / 32][TK];     // [tile parity][K, V][group], slots as above
+
+  const AttnArgs &A = C.a;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int a = lane >> 4, b = lane & 15;
+  const int S = A.num_splits, U = A.num_units;
+  int split = blockIdx.x, bt = blockIdx.z;
+  const int u = blockIdx.y;
+  if (A.z_rounds > 1) {                 // more batch elements than a grid's last dimension holds
+    bt += split / S * STS_GRID_Z;
+    split %= S;
+    if (bt >= A.B) return;
+  }
+  const uint32_t unit = A.units.unit[u];
+  const int g = unit & 0xff;
+  const uint32_t mask = (unit >> 8) & 0xffff;
+  const int nheads = (unit >> 24) & 0x1f;
+  const int rows_valid = nheads * A.Tq;
+  const int head0 = g * A.G + __builtin_ctz(mask);
+  const int psh = A.page_shift, pmask = A.page - 1;
+  const bool list = GATHER && A.indices != nullptr, paged = GATHER && A.block_table != nullptr;
+
+  // ---- the keys of this unit: positions 0 .. c - 1 of its list (or of the cache), and which tiles of 32 are looked at
+  const int32_t *len_src = list ? (A.counts ? A.counts + (int64_t)bt * A.cnt_stride_b + head0 : nullptr) : (A.seq_lens ? A.seq_lens + bt : nullptr);
+  const int n_max = list ? A.kmax : A.N;
+  const int c = (len_src ? min(max(*len_src, 0), n_max) : n_max) << (list ? psh : 0);
+  const int tiles_end = (c + TK - 1) / TK;
+  // a window: tiles of sinks, then those from row 0's first key in the window on
+  const int p0 = WIN ? (C.behind ? c : c - A.Tq) : 0;
+  const int lo = WIN ? max(0, (int)max((int64_t)p0 - C.window + 1, (int64_t)0)) : 0;
+  const int sink_tiles = WIN ? min((min(C.sinks, c) + TK - 1) / TK, lo / TK) : 0;
+  const int skipped = WIN ? lo / TK - sink_tiles : 0;
+  const int tiles = max(tiles_end - skipped, 0);
+  const int tps = (tiles + S - 1) / S;
+  const int t_begin = split * tps, t_end = min(t_begin + tps, tiles);
+  const int nv = t_end - t_begin > wave ? (t_end - t_begin - wave + W - 1) / W : 0;       // tiles of this wave
+  auto tile_of = [&](int v) { return min(t_begin + wave + v * W, t_end - 1); };           // past the last, the last again
+  auto first_of = [&](int t) { return (WIN && t >= sink_tiles ? t + skipped : t) * TK; };   // position of a tile's first key
+
+  // ---- query rows of this lane: row nq * 16 + b. A negative scale turns the signs of Q, a scale of 0 clears it.
+  const uint32_t q_keep = A.scale == 0.f ? 0u : 0xffffffffu, q_flip = A.scale < 0.f ? 0x80008000u : 0u;
+  const float sl2 = A.scale == 0.f ? 1.f : fabsf(A.scale_log2);
+  u32x4 Q[QLDS ? 1 : NQ][QLDS ? 1 : KK];
+  int q_tq[NQ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    const int r = nq * 16 + b;
+    const bool ok = r < rows_valid;
+    const int hsel = ok ? r / A.Tq : 0;
+    q_tq[nq] = ok ? r - hsel * A.Tq : 0;
+    const uint16_t *qp = A.q + (((size_t)bt * A.Tq + q_tq[nq]) * A.Hq + g * A.G + nth_member(mask, hsel)) * D;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      u32x4 w = *reinterpret_cast<const u32x4 *>(qp + (FOUR ? a * (D / 4) + 8 * kk : 8 * (a + 4 * kk)));
+      w = (w & (ok ? q_keep : 0u)) ^ q_flip;
+      if (!QLDS) Q[nq][kk] = w;
+      else if (wave == 0) lds_q[(nq * KK + kk) * 64 + lane] = w;
+    }
+  }
+  if (QLDS) __syncthreads();
+
+  float m_run[NQ], l_run[NQ];
+  f32x4 acc[NQ][NT];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    m_run[nq] = -INFINITY;
+    l_run[nq] = 0.f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) acc[nq][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // ---- loads
+  struct Tile {
+    k_t k[2][KL];
+    v_t v[8];
+    uint32_t sc;
+  };
+  const int64_t row_bytes = FOUR ? C.code_n : A.stride_n * 2, page_bytes = FOUR ? C.code_page : A.stride_page * 2;
+  const int64_t head_off = FOUR ? (paged ? 0 : bt * C.code_b) + g * C.code_h : ((paged ? 0 : bt * A.stride_b) + g * A.stride_h) * 2;
+  const unsigned char *kuni = (FOUR ? C.codes : reinterpret_cast<const unsigned char *>(A.k)) + head_off;
+  const unsigned char *vuni = (FOUR ? C.codes + D / 2 : reinterpret_cast<const unsigned char *>(A.v)) + head_off;
+  const unsigned char *suni = FOUR ? C.scales + (paged ? 0 : bt * C.scale_b) + g * C.scale_h : nullptr;
+  constexpr int KCH = FOUR ? D / 8 : 16, VCH = FOUR ? D / 32 : D / 8;      // bytes of a lane's chunk
+  const int slot = lane & 31, slot_at = (slot & 3) * 8 + (slot >> 2);
+  const int k_slot = (b >> 2) + 4 * (b & 3), k_at = (b >> 2) * 8 + (b & 3);
+  const uint32_t half = FOUR && D == 128 ? (lane >> 5) * 4 : 0;            // K's or V's word of a token's scales
+
+  auto load_k = [&](const unsigned char *base, off_t off, k_t (&k)[KL]) {
+#pragma unroll
+    for (int j = 0; j < KL; ++j) k[j] = *reinterpret_cast<const k_t *>(base + (off + (off_t)(64 * j)));
+  };
+  auto load_v = [&](const unsigned char *base, off_t off) { return *reinterpret_cast<const v_t *>(base + off); };
+
+  // contiguous: offsets of the lane's rows in a tile, which a tile's end and gap move to rows that are attended to (their weight is 0,
+  // but 0 times what lies there may be NaN)
+  uint32_t k_off[2], v_off[8];
+  if (!GATHER) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) k_off[h] = (uint32_t)((k_slot + 16 * h) * (int)row_bytes);
+#pragma unroll
+    for (int m = 0; m < 8; ++m) v_off[m] = (uint32_t)((a + 4 * m) * (int)row_bytes);
+  }
+  auto seen_row = [&](int n) { return WIN && n >= C.sinks && n < lo ? lo : n; };
+  auto issue_near = [&](int t, Tile &R) {
+    const int n0 = first_of(t);
+    const unsigned char *kb = kuni + n0 * row_bytes, *vb = vuni + n0 * row_bytes;
+    if (WIN && n0 < lo) {               // tiles of sinks, and the one that the window begins in
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load_k(kuni + min(seen_row(n0 + k_slot + 16 * h), c - 1) * row_bytes, (off_t)(a * KCH), R.k[h]);
+#pragma unroll
+      for (int m = 0; m < 8; ++m) R.v[m] = load_v(vuni + min(seen_row(n0 + a + 4 * m), c - 1) * row_bytes, (off_t)(b * VCH));
+    } else {
+      const uint32_t last = (uint32_t)(min(c - 1 - n0, TK - 1) * (int)row_bytes);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load_k(kb, (off_t)(min(k_off[h], last) + a * KCH), R.k[h]);
+#pragma unroll
+      for (int m = 0; m < 8; ++m) R.v[m] = load_v(vb, (off_t)(min(v_off[m], last) + b * VCH));
+    }
+    if (FOUR) R.sc = *reinterpret_cast<const uint32_t *>(suni + n0 * C.scale_n + (min(slot, c - 1 - n0) * (int)C.scale_n + (int)half));
+  };
+
+  // gather: list entry (or block) -> page -> offset, each a step of its own
+  const int32_t *idx_row = list ? A.indices + (size_t)bt * A.idx_stride_b + (size_t)head0 * A.kmax : nullptr;
+  const int32_t *table_row = paged ? A.block_table + (size_t)bt * A.table_stride : nullptr;
+  const int nb_max = (A.N + A.page - 1) >> psh;
+  auto fetch = [&](int t) -> int {      // entry of this lane's slot of tile t
+    const int pos = min(seen_row(first_of(t) + slot), c - 1) >> psh;
+    return list ? idx_row[pos] : pos;
+  };
+  auto block_of = [&](int entry) { return min(max(entry, 0), nb_max - 1); };
+  auto look_up = [&](int blk) { return paged ? table_row[blk] : blk; };
+  off_t scale_off = 0;
+  auto place = [&](int blk, int page, int t, int par, uint32_t &tile_mask) {
+    const int pos = first_of(t) + slot, in_page = min(seen_row(pos), c - 1) & pmask, tok = (blk << psh) + in_page;
+    // (of a block that the cache's end cuts, the rows behind it read the cache's last row, which is in the block)
+    const int over = max(tok - (A.N - 1), 0), at = paged ? in_page - over : tok - over;
+    if (!WIN) tile_mask = (uint32_t)__ballot(pos < c && over == 0);
+    const int64_t pg = paged ? (int64_t)min(max(page, 0), A.num_pages - 1) : 0;
+    lds_off[GATHER ? wave : 0][par][slot_at] = (off_t)((FAR ? pg * page_bytes : 0) + at * row_bytes);
+    if (FOUR) scale_off = (off_t)((FAR ? pg * C.scale_page : 0) + at * C.scale_n) + (off_t)half;
+  };
+  auto issue_far = [&](int par, Tile &R) {
+    off_t ko[2], vo[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) ko[h] = lds_off[GATHER ? wave : 0][par][k_at + 4 * h];
+#pragma unroll
+    for (int m = 0; m < 8; ++m) vo[m] = lds_off[GATHER ? wave : 0][par][a * 8 + m];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_k(kuni, ko[h] + (off_t)(a * KCH), R.k[h]);
+#pragma unroll
+    for (int m = 0; m < 8; ++m) R.v[m] = load_v(vuni, vo[m] + (off_t)(b * VCH));
+    if (FOUR) R.sc = *reinterpret_cast<const uint32_t *>(suni + scale_off);
+  };
+
+  // ---- scales of one tile: own token's word -> LDS -> the two of K's rows and the eight of V's
+  uint32_t ks[2], vs[8];
+  auto put_scales = [&](uint32_t w, int par) {
+    if constexpr (FOUR) {
+      const int kv = D == 128 ? lane >> 5 : 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t f = (j == 0 ? w << 23 : j == 1 ? w << 15 : j == 2 ? w << 7 : w >> 1) & 0x7f800000u;
+        if (D == 128) lds_sc[wave][par][kv][j & (D / 32 - 1)][slot_at] = f;
+        else lds_sc[wave][par][j >> 1][j & 1][slot_at] = f;
+      }
+    }
+  };
+  auto get_scales = [&](int par) {
+    if constexpr (FOUR) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) ks[h] = lds_sc[wave][par][0][a * (D / 32) / 4][k_at + 4 * h];
+#pragma unroll
+      for (int m = 0; m < 8; ++m) vs[m] = lds_sc[wave][par][1][b * (D / 32) / 16][a * 8 + m];
+    }
+  };
+
+  // ---- one tile
+  auto consume = [&](const Tile &R, int t, uint32_t tile_mask) {
+    f32x4 St[NQ][2];
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) St[nq][0] = St[nq][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      u32x4 Ka[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if constexpr (FOUR) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) Ka[h][j] = pair_of(R.k[h][0][kk], __builtin_bit_cast(float, ks[h]), j);
+        } else {
+          Ka[h] = R.k[h][kk];
+        }
+      }
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        const u32x4 Qb = QLDS ? lds_q[(nq * KK + kk) * 64 + lane] : Q[QLDS ? 0 : nq][QLDS ? 0 : kk];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          St[nq][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, Ka[h]), __builtin_bit_cast(bf16x8, Qb), St[nq][h], 0, 0, 0);
+      }
+    }
+    // (V's conversions do not move up here, where their results would take the registers of the tiles on the way)
+    if (FOUR && NQ >= 2) __builtin_amdgcn_sched_barrier(0);
+    // keys that a row does not see score -inf
+    const int n0 = first_of(t);
+    bool partly = false;                 // some row does not see some key
+    auto sees = [&](int n, int nq) {
+      const int p = p0 + q_tq[nq];
+      return n < c && n <= p && (n < C.sinks || p - n < C.window);
+    };
+    if constexpr (WIN) {
+      const int pl = p0 + A.Tq - 1;
+      partly = !(n0 + TK <= c && n0 + TK - 1 <= p0 && (n0 + TK <= C.sinks || pl - n0 < C.window));
+      if (partly) {
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (!sees(n0 + a + 4 * i, nq)) St[nq][i >> 2][i & 3] = -INFINITY;
+      }
+    } else if (tile_mask != 0xffffffffu) {
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (!((tile_mask >> (a + 4 * i)) & 1u)) St[nq][i >> 2][i & 3] = -INFINITY;
+    }
+    u32x4 P[NQ];
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+      const f32x4 s0 = St[nq][0], s1 = St[nq][1];
+      const float mt = sl2 * max_over_groups(larger(larger(larger(s0[0], s0[1]), larger(s0[2], s0[3])), larger(larger(s1[0], s1[1]), larger(s1[2], s1[3]))));
+      if (__builtin_amdgcn_ballot_w64(mt > m_run[nq]) != 0) {
+        const float m_new = larger(m_run[nq], mt);
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[nq] - m_new);
+        l_run[nq] *= alpha;
+        m_run[nq] = m_new;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[nq][nt] *= alpha;
+      }
+      const float m_ref = WIN && m_run[nq] == -INFINITY ? 0.f : m_run[nq];
+      float p[8], sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(St[nq][i >> 2][i & 3], sl2, -m_ref));
+        sum += p[i];
+      }
+      l_run[nq] += sum;
+      // the weights enter the second product as bf16 (half a step, 2^-9 of each), the sum above in fp32
+#pragma unroll
+      for (int i = 0; i < 4; ++i) P[nq][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p[2 * i], p[2 * i + 1]}), bf16x2));
+    }
+    // pair j of channels of the lane's 8 keys, and of those the keys of channel 2 j (hi: 2 j + 1) as pairs
+    auto v_pairs = [&](int j, uint32_t (&w)[8]) {
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        if constexpr (FOUR) w[m] = pair_of(R.v[m], __builtin_bit_cast(float, vs[m]), j);
+        else w[m] = R.v[m][j];
+      }
+    };
+    auto v_keys = [&](const uint32_t (&w)[8], bool hi) {
+      u32x4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], hi ? 0x07060302u : 0x05040100u);
+      return x;
+    };
+    if constexpr (WIN) {
+      if (partly) {
+        // A value that is no number, or infinite, must not reach the rows that do not see it, and 0 times it is not 0: then key by key,
+        // and only where it is seen.
+        uint32_t odd = 0;
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+#pragma unroll
+          for (int j = 0; j < NT / 2; ++j) odd |= ((R.v[m][j] & 0x7f80u) == 0x7f80u) | ((R.v[m][j] & 0x7f800000u) == 0x7f800000u);
+        if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
+          for (int key = 0; key < TK; ++key) {
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+              const bool see = sees(n0 + key, nq);
+              u32x4 own;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) own[i] = (a + 8 * i == key ? 0xffffu : 0u) | (a + 8 * i + 4 == key ? 0xffff0000u : 0u);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                uint32_t w[8];
+                v_pairs(nt >> 1, w);
+                const u32x4 Vk = v_keys(w, nt & 1) & own;
+                const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, Vk), __builtin_bit_cast(bf16x8, P[nq] & own), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[nq][nt][r] += see ? x[r] : 0.f;
+              }
+            }
+          }
+          return;
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT / 2; ++j) {
+      uint32_t w[8];
+      v_pairs(j, w);
+#pragma unroll
+      for (int hi = 0; hi < 2; ++hi) {
+        const bf16x8 Va = __builtin_bit_cast(bf16x8, v_keys(w, hi));
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq)
+          acc[nq][2 * j + hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Va, __builtin_bit_cast(bf16x8, P[nq]), acc[nq][2 * j + hi], 0, 0, 0);
+      }
+    }
+  };
+
+  // ---- main loop: PF tiles on the way, each asked for again when it has been used. One exit, and code of its own for what is left over, so
+  // that the loop's head knows which loads are in flight.
+  if (nv > 0) {
+    Tile R[PF];
+    uint32_t seen[PF];
+    if constexpr (!GATHER) {
+#pragma unroll
+      for (int j = 0; j < PF; ++j) issue_near(tile_of(j), R[j]);
+      put_scales(R[0].sc, 0);
+      get_scales(0);
+      auto step = [&](int v, int j, bool more) {
+        const int t = tile_of(v), left = c - first_of(t);
+        put_scales(R[(j + 1) % PF].sc, (v + 1) & 1);
+        consume(R[j], t, left >= TK ? 0xffffffffu : (1u << left) - 1u);
+        get_scales((v + 1) & 1);
+        if (more) issue_near(tile_of(v + PF), R[j]);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      int v = 0;
+      for (; v + PF <= nv; v += PF) {
+#pragma unroll
+        for (int j = 0; j < PF; ++j) step(v + j, j, true);
+      }
+#pragma unroll
+      for (int j = 0; j < PF - 1; ++j)
+        if (v + j < nv) step(v + j, j, false);
+    } else {
+      // tile j of the ring: a list entry fetched 3 PF tiles ahead of its use, its page looked up 2 PF ahead, the offset placed PF + 1
+      // ahead
+      int entry[PF], blk[PF], page[PF];
+      uint32_t next_seen = 0;
+      int e0[PF + 1];
+#pragma unroll
+      for (int j = 0; j <= PF; ++j) e0[j] = fetch(tile_of(j));
+#pragma unroll
+      for (int j = 0; j < PF; ++j) blk[(j + 1) % PF] = fetch(tile_of(PF + 1 + j));
+#pragma unroll
+      for (int j = 0; j < PF; ++j) entry[(j + 1) % PF] = fetch(tile_of(2 * PF + 1 + j));
+      int pg0[PF + 1];
+#pragma unroll
+      for (int j = 0; j <= PF; ++j) e0[j] = block_of(e0[j]), pg0[j] = look_up(e0[j]);
+#pragma unroll
+      for (int j = 0; j < PF; ++j) blk[j] = block_of(blk[j]), page[j] = look_up(blk[j]);
+#pragma unroll
+      for (int j = 0; j <= PF; ++j) {
+        place(e0[j], pg0[j], tile_of(j), j & 1, next_seen);
+        if (j < PF) {
+          issue_far(j & 1, R[j]);
+          seen[j] = next_seen;
+        }
+      }
+      put_scales(R[0].sc, 0);
+      get_scales(0);
+      auto step = [&](int v, int j, bool more) {
+        const int t = tile_of(v), n = (j + 1) % PF;
+        put_scales(R[n].sc, (v + 1) & 1);
+        consume(R[j], t, seen[j]);
+        get_scales((v + 1) & 1);
+        if (more) {
+          issue_far((v + PF) & 1, R[j]);
+          seen[j] = next_seen;
+          __builtin_amdgcn_sched_barrier(0);
+          place(blk[n], page[n], tile_of(v + PF + 1), (v + PF + 1) & 1, next_seen);
+          blk[n] = block_of(entry[n]);
+          page[n] = look_up(blk[n]);
+          entry[n] = fetch(tile_of(v + 3 * PF + 1));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      int v = 0;
+      for (; v + PF <= nv; v += PF) {
+#pragma unroll
+        for (int j = 0; j < PF; ++j) step(v + j, j, true);
+      }
+#pragma unroll
+      for (int j = 0; j < PF - 1; ++j)
+        if (v + j < nv) step(v + j, j, false);
+    }
+  }
+
+  // ---- the waves are merged, the workgroup's partial is written (or the result, where nothing is left to be merged)
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    float l = l_run[nq];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (a == 0) {
+      lds_ml[wave][nq * 16 + b][0] = m_run[nq];
+      lds_ml[wave][nq * 16 + b][1] = l;
+    }
+  }
+  __syncthreads();
+  const size_t part = ((size_t)bt * U + u) * S + split;
+  float *po = A.part_o + part * (size_t)(NQ * 16 * D), *pml = A.part_ml + part * (size_t)(NQ * 16 * 2);
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    auto top_of = [&](int r) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < W; ++w) m = fmaxf(m, lds_ml[w][r][0]);
+      return m;
+    };
+    const float top = top_of(nq * 16 + b);
+    const float f = m_run[nq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[nq] - top);
+    float *orow = lds_o + (wave * 16 + b) * OPITCH;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int v4 = 0; v4 < NT / 4; ++v4) {
+        f32x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = acc[nq][4 * v4 + e][r] * f;
+        *reinterpret_cast<f32x4 *>(orow + NT * (4 * a + r) + 4 * v4) = o;
+      }
+    __syncthreads();
+    constexpr int SEGF = D / 16;
+    const int row = threadIdx.x >> 4, seg = threadIdx.x & 15, r = nq * 16 + row;
+    f32x4 sum[SEGF / 4];
+#pragma unroll
+    for (int e = 0; e < SEGF / 4; ++e) sum[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int e = 0; e < SEGF / 4; ++e) sum[e] += *reinterpret_cast<const f32x4 *>(lds_o + (w * 16 + row) * OPITCH + seg * SEGF + 4 * e);
+    const float m = top_of(r);
+    float L = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float mw = lds_ml[w][r][0];
+      L += mw == -INFINITY ? 0.f : lds_ml[w][r][1] * __builtin_amdgcn_exp2f(mw - m);
+    }
+    if (!A.direct) {
+#pragma unroll
+      for (int e = 0; e < SEGF / 4; ++e) *reinterpret_cast<f32x4 *>(po + (size_t)r * D + seg * SEGF + 4 * e) = sum[e];
+      if (seg == 0) *reinterpret_cast<f32x2 *>(pml + r * 2) = f32x2{m, L};
+    } else if (r < rows_valid) {
+      const int hsel = r / A.Tq, tq = r - hsel * A.Tq, head = g * A.G + nth_member(mask, hsel);
+      const float inv = L > 0.f ? 1.f / L : 0.f;
+      const size_t at = (((size_t)bt * A.Tq + tq) * A.Hq + head) * D + seg * SEGF;
+#pragma unroll
+      for (int e = 0; e < SEGF / 4; ++e) {
+        const f32x4 x = sum[e] * inv;
+        if (A.out_dtype == STS_F32) {
+          *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 4 * e) = x;
+        } else {
+          const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2)),
+                           __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2], x[3]}), bf16x2))};
+          *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at + 4 * e) = w;
+        }
+      }
+      if (A.lse_out && seg == 0)
+        A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + tq] = L > 0.f ? (m + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
+    }
+    __syncthreads();
+  }
+}
+
+template <int D, int NQ>
+hipError_t launch(const CacheAttnArgs &a, bool four_bit, bool far, hipStream_t s) {
+  const unsigned z = a.a.B < STS_GRID_Z ? a.a.B : STS_GRID_Z;
+  const dim3 grid((unsigned)(a.a.num_splits * a.a.z_rounds), a.a.num_units, z), block(64 * STS_WG_WAVES);
+  const bool gather = a.a.indices || a.a.block_table;
+  if (four_bit) {
+    if (far) STS_LAUNCH((cache_attn_kernel<D, NQ, true, true, true>), grid, block, 0, s, a);
+    else if (gather) STS_LAUNCH((cache_attn_kernel<D, NQ, true, true, false>), grid, block, 0, s, a);
+    else STS_LAUNCH((cache_attn_kernel<D, NQ, true, false, false>), grid, block, 0, s, a);
+  } else if constexpr (NQ <= 2) {
+    if (far) STS_LAUNCH((cache_attn_kernel<D, NQ, false, true, true>), grid, block, 0, s, a);
+    else STS_LAUNCH((cache_attn_kernel<D, NQ, false, false, false>), grid, block, 0, s, a);
+  } else {
+    return hipErrorInvalidValue;
+  }
+  return sts_take_launch_status();
+}
+
+}  // namespace
+
+hipError_t launch_cache_attn(const CacheAttnArgs &a, int d, int nq, bool four_bit, bool far, hipStream_t s) {
+  if ((size_t)a.a.B * a.a.num_units * a.a.num_splits == 0) return hipSuccess;
+  if (d == 128) return nq == 1 ? launch<128, 1>(a, four_bit, far, s) : nq == 2 ? launch<128, 2>(a, four_bit, far, s) : launch<128, 4>(a, four_bit, far, s);
+  return nq == 1 ? launch<64, 1>(a, four_bit, far, s) : nq == 2 ? launch<64, 2>(a, four_bit, far, s) : launch<64, 4>(a, four_bit, far, s);
+}

@@ -1,0 +1,313 @@
+// Attention with a sliding window and sinks over many query rows: a prompt, or a chunk of one (gfx950).
+//
+// A workgroup of four waves has 128 query rows of one KV head: row r of the head's Tq * G rows is query r / G of the
+// group's head r % G, so that the heads of a group share every K and V tile and a block spans 128 / G positions: with a
+// window of W it looks at W + 128 / G keys and at the tiles of sinks. A wave has 32 rows; tiles are 64 keys, K and V
+// in LDS, two of each, the next tile on its way there while one is worked on.
+//
+// Transposed as in the split kernels, on v_mfma_f32_32x32x16_bf16: S^T = K Q^T gives lane (h, c) = (lane / 32, lane % 32) the
+// scores of query c with keys 8 j + 4 h + i (j = 0..3, i = 0..3) of each 32, two j of which are what it supplies as the B operand of
+// O^T += V^T P^T for 16 keys: P stays in its lane, and V's operand takes the keys in that order. It comes from V's rows in
+// LDS by the transposing read (four lanes have 16 channels of a key, lane i gets channel i of four keys).
+// LDS chunks of 16 bytes are permuted within a row so that neither K's reads (16 rows, one chunk each) nor V's (4 rows, 64
+// bytes each) meet in a bank.
+#include "cache.h"
+
+namespace {
+
+constexpr int WAVES = 4, ROWS = 32 * WAVES, TK = 64;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
+
+// where chunk c of row r lies in its row
+template <int D> __device__ __forceinline__ int k_chunk(int r, int c) { return D == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7); }
+template <int D> __device__ __forceinline__ int v_chunk(int r, int c) { return D == 128 ? c ^ ((r & 3) << 2) : c ^ ((r & 2) << 1); }
+
+// bits 0 .. n - 1, none for n <= 0
+__device__ __forceinline__ uint64_t first_keys(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+__device__ __forceinline__ float top(float x, float y) { return __builtin_elementwise_maximum(x, y); }      // (a NaN wins)
+
+template <int D, bool PAGED>
+__global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const WindowArgs A) {
+  constexpr int KS = D / 16;             // contraction steps of S
+  constexpr int DT = D / 32;             // 32-channel tiles of O
+  constexpr int CH = D / 8;              // 16-byte chunks of a row
+  constexpr int NL = TK * CH / (64 * WAVES);       // chunks of K (and of V) per thread and tile
+  constexpr int RL = 64 / CH;                      // rows that a wave's load covers
+  // (four arrays, not two of two: so the compiler can tell the loads that fill one from the reads of another)
+  __shared__ __attribute__((aligned(16))) u32x4 lds_k0[TK * CH], lds_k1[TK * CH], lds_v0[TK * CH], lds_v1[TK * CH];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
+  // Blocks of one KV head next to each other on one die (workgroup i runs on die i % 8), the later positions, which may have
+  // more keys, first.
+  const int nb = (int)(((int64_t)A.Tq * A.G + ROWS - 1) / ROWS);
+  const int total = gridDim.x, x = blockIdx.x % STS_XCDS;
+  const int j = x * (total / STS_XCDS) + min(x, total % STS_XCDS) + blockIdx.x / STS_XCDS;
+  const int blk = nb - 1 - j % nb, g = j / nb % A.Hkv, bt = j / nb / A.Hkv;
+
+  const int L = A.seq_lens ? min(max(A.seq_lens[bt], 0), A.N) : A.N;
+  const int p_first = L - A.Tq;                                   // position of query 0
+  const int64_t rows = (int64_t)A.Tq * A.G;
+  const int64_t r_mine = (int64_t)blk * ROWS + wave * 32 + col;
+  const bool ok = r_mine < rows;
+  const int r = (int)min(r_mine, rows - 1);
+  const int qi = r / A.G, head = g * A.G + r - qi * A.G;
+  const int p = p_first + qi;                                     // this lane's query
+  const int b_lo = p_first + blk * ROWS / A.G, b_hi = p_first + (int)min((int64_t)blk * ROWS + ROWS - 1, rows - 1) / A.G;       // the workgroup's
+  const int w_lo = p_first + (int)(min((int64_t)blk * ROWS + wave * 32, rows - 1)) / A.G;                                       // the wave's
+  const int w_hi = p_first + (int)(min((int64_t)blk * ROWS + wave * 32 + 31, rows - 1)) / A.G;
+
+  // keys 0 .. sinks - 1 and lo .. end - 1
+  const int end = min(b_hi + 1, L);
+  const int lo = (int)max((int64_t)b_lo - A.window + 1, (int64_t)0);
+  const int tiles_end = end > 0 ? (end + TK - 1) / TK : 0;
+  const int sink_tiles = min((min(A.sinks, max(end, 0)) + TK - 1) / TK, lo / TK);
+  const int skipped = lo / TK - sink_tiles;
+  const int tiles = max(tiles_end - skipped, 0);
+  auto first_of = [&](int t) { return (t >= sink_tiles ? t + skipped : t) * TK; };
+
+  // ---- Q, as the B operand: channels 16 s + 8 h .. of query col. The scale's sign goes to Q.
+  const uint32_t q_keep = A.scale == 0.f ? 0u : 0xffffffffu, q_flip = A.scale < 0.f ? 0x80008000u : 0u;
+  const float sl2 = A.scale == 0.f ? 1.f : fabsf(A.scale_log2);
+  bf16x8 Q[KS];
+  {
+    const uint16_t *qp = A.q + (((size_t)bt * A.Tq + qi) * A.Hq + head) * D + 8 * h;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) Q[s] = __builtin_bit_cast(bf16x8, (*reinterpret_cast<const u32x4 *>(qp + 16 * s) & q_keep) ^ q_flip);
+  }
+
+  // ---- loads, straight to LDS: load m of a wave fills the 1 KB of rows (wave NL + m) RL .., lane by lane, so the permutation of a
+  // row's chunks is in what a lane asks for. Rows that no query of the block sees are read from ones that some query does: their weight
+  // is 0, but 0 times what lies there may be NaN.
+  const int row0 = wave * NL * RL + lane / CH, slot0 = lane % CH;
+  const int64_t row_bytes = A.stride_n * 2, head_off = ((PAGED ? 0 : bt * A.stride_b) + g * A.stride_h) * 2;
+  const unsigned char *kbase = reinterpret_cast<const unsigned char *>(A.k) + head_off, *vbase = reinterpret_cast<const unsigned char *>(A.v) + head_off;
+  const int32_t *table = PAGED ? A.block_table + (size_t)bt * A.table_stride : nullptr;
+  auto row_of = [&](int n) {
+    n = n >= A.sinks && n < lo ? lo : n;
+    return min(n, end - 1);
+  };
+  typedef __attribute__((address_space(3))) unsigned char *lds_ptr;
+  auto load = [&](int t, u32x4 *k, u32x4 *v) {
+    const int n0 = first_of(t);
+    int l_row = row0, l_slot = slot0;
+    asm("" : "+v"(l_row), "+v"(l_slot));         // (as in consume)
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int m = 0; m < NL; ++m) {
+        const int row = l_row + RL * m, n = row_of(n0 + row);
+        const int page = min(max(table[n >> A.page_shift], 0), A.num_pages - 1);
+        const int64_t off = (page * A.stride_page + (n & ((1 << A.page_shift) - 1)) * A.stride_n) * 2;
+        typedef const __attribute__((address_space(1))) unsigned char *global_ptr;
+        __builtin_amdgcn_global_load_lds((global_ptr)(kbase + off + 16 * k_chunk<D>(row, l_slot)), (lds_ptr)(k + (wave * NL + m) * 64), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_ptr)(vbase + off + 16 * v_chunk<D>(row, l_slot)), (lds_ptr)(v + (wave * NL + m) * 64), 16, 0, 0);
+      }
+    } else {
+      const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(kbase + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
+      const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(vbase + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
+      const bool inside = n0 >= lo && n0 + TK <= end;
+#pragma unroll
+      for (int m = 0; m < NL; ++m) {
+        const int row = l_row + RL * m;
+        const uint32_t off = (uint32_t)((inside ? row : row_of(n0 + row) - n0) * (int)row_bytes);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_ptr)(k + (wave * NL + m) * 64), 16, (int)(off + 16 * k_chunk<D>(row, l_slot)), 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_ptr)(v + (wave * NL + m) * 64), 16, (int)(off + 16 * v_chunk<D>(row, l_slot)), 0, 0, 0);
+      }
+    }
+  };
+  // does every query of a range lo_p .. hi_p see all keys of the tile at n0?
+  auto whole = [&](int n0, int lo_p, int hi_p) { return n0 + TK - 1 <= lo_p && (n0 + TK <= A.sinks || hi_p - n0 < A.window); };
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 acc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
+
+  // Where the lane reads: K's chunk 2 s + h of row 32 kt + col, and V's operand for channels 32 dt .. and keys 16 s .., two transposed
+  // reads of keys 16 s + 4 h + 0..3 and 8 further on. Both are one address with a few bits flipped by s or dt, plus a constant.
+  typedef const __attribute__((address_space(3))) u32x4 *lds_u32x4;
+  const int k_lane = col * CH * 16 + 16 * k_chunk<D>(col, h);
+  const int t_row = 4 * h + ((lane & 15) >> 2), t_col = (lane & 16) + 4 * (lane & 3);       // within 16 keys, 32 channels
+  const int v_lane = (t_row * CH + v_chunk<D>(t_row, t_col >> 3)) * 16 + (t_col & 7) * 2;
+  auto v_operand = [&](const u32x4 *v, int at, int dt, int s) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const u32x2 v2 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_ptr)v + (at ^ (64 * dt)) + (16 * s + 8 * e) * CH * 16)));
+      w[2 * e] = v2[0];
+      w[2 * e + 1] = v2[1];
+    }
+    return w;
+  };
+
+  auto consume = [&](int t, const u32x4 *k, const u32x4 *v) {
+    const int n0 = first_of(t);
+    int k_at = k_lane, v_at = v_lane;
+    asm("" : "+v"(k_at), "+v"(v_at));            // (what comes of them is made anew in every tile, not kept in registers)
+    f32x16 S[2];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[kt][i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const bf16x8 Ka = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)k + (k_at ^ (32 * s)) + 32 * kt * CH * 16));
+        S[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Ka, Q[s], S[kt], 0, 0, 0);
+      }
+    auto sees = [&](int n) { return n <= p && (n < A.sinks || p - n < A.window); };       // (n < L follows from n <= p)
+    const bool partly = !whole(n0, w_lo, w_hi);
+    if (partly) {
+      // a bit per key of the tile, then per half of the wave: keys up to the query, without those between the sinks and the window
+      const uint64_t seen = (first_keys(p + 1 - n0) & (first_keys(A.sinks - n0) | ~first_keys((int)max((int64_t)p - A.window + 1, (int64_t)0) - n0))) >> (4 * h);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const int word = (int)(uint32_t)(seen >> (32 * kt));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(word, (i & 3) + 8 * (i >> 2), 1), x = __builtin_bit_cast(uint32_t, (float)S[kt][i]);
+          S[kt][i] = __builtin_bit_cast(float, (x & keep) | (0xff800000u & ~keep));
+        }
+      }
+    }
+    float mt = top(S[0][0], S[1][0]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mt = top(mt, top(S[0][i], S[1][i]));
+    {
+      const uint32_t w = __builtin_bit_cast(uint32_t, mt);
+      const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+      const uint32_t q0 = q[0], q1 = q[1];
+      mt = sl2 * top(__builtin_bit_cast(float, q0), __builtin_bit_cast(float, q1));
+    }
+    if (__builtin_amdgcn_ballot_w64(mt > m_run) != 0) {
+      const float m_new = fmaxf(m_run, mt);
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
+    }
+    const float m_ref = m_run == -INFINITY ? 0.f : m_run;
+    u32x4 P[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * e], sl2, -m_ref));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * e + 1], sl2, -m_ref));
+        l_run += p0;
+        l_run += p1;
+        // the weights enter the second product as bf16 (half a step, 2^-9 of each), the sum in fp32
+        P[s][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+      }
+    bool odd = false;        // values that are no numbers, or infinite, in a tile that not everyone sees
+    if (partly) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int m = 0; m < TK * CH / 64; ++m) {
+        const u32x4 w = *(lds_u32x4)((lds_ptr)v + 16 * lane + 1024 * m);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
+      }
+      odd = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+    }
+    if (odd) {
+      // key by key, and only where it is seen
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        for (int key = 0; key < 16; ++key) {
+          u32x4 own;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
+            own[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
+          }
+          const bool see = sees(n0 + 16 * s + key);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            f32x16 z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.f;
+            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v, v_at, dt, s) & own), __builtin_bit_cast(bf16x8, P[s] & own), z, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[dt][i] += see ? z[i] : 0.f;
+            __builtin_amdgcn_sched_barrier(0);         // (one product's registers at a time)
+          }
+        }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v, v_at, dt, s)), __builtin_bit_cast(bf16x8, P[s]), acc[dt], 0, 0, 0);
+    }
+  };
+
+  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); };
+  if (tiles > 0) {
+    load(0, lds_k0, lds_v0);
+    arrived();
+    int t = 0;
+    for (;;) {
+      if (t + 1 < tiles) load(t + 1, lds_k1, lds_v1);
+      consume(t, lds_k0, lds_v0);
+      if (++t >= tiles) break;
+      arrived();
+      if (t + 1 < tiles) load(t + 1, lds_k0, lds_v0);
+      consume(t, lds_k1, lds_v1);
+      if (++t >= tiles) break;
+      arrived();
+    }
+  }
+
+  // ---- out
+  {
+    const uint32_t w = __builtin_bit_cast(uint32_t, l_run);
+    const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    const uint32_t q0 = q[0], q1 = q[1];
+    l_run = __builtin_bit_cast(float, q0) + __builtin_bit_cast(float, q1);
+  }
+  if (!ok) return;
+  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+  const size_t at = (((size_t)bt * A.Tq + qi) * A.Hq + head) * D + 4 * h;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x4 o = {acc[dt][4 * e] * inv, acc[dt][4 * e + 1] * inv, acc[dt][4 * e + 2] * inv, acc[dt][4 * e + 3] * inv};
+      if (A.out_dtype == STS_F32) {
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 32 * dt + 8 * e) = o;
+      } else {
+        const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[0], o[1]}), bf16x2)),
+                         __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[2], o[3]}), bf16x2))};
+        *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at + 32 * dt + 8 * e) = w;
+      }
+    }
+  if (A.lse_out && h == 0)
+    A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + qi] = l_run == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_run)) * 0.69314718055994530942f;
+}
+
+}  // namespace
+
+hipError_t launch_window_prompt(const WindowArgs &a, int d, hipStream_t s) {
+  const int64_t blocks = ((int64_t)a.Tq * a.G + ROWS - 1) / ROWS * a.Hkv * a.B;
+  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks), block(64 * WAVES);
+  if (d == 128) {
+    if (a.block_table) STS_LAUNCH((window_prompt_kernel<128, true>), grid, block, 0, s, a);
+    else STS_LAUNCH((window_prompt_kernel<128, false>), grid, block, 0, s, a);
+  } else {
+    if (a.block_table) STS_LAUNCH((window_prompt_kernel<64, true>), grid, block, 0, s, a);
+    else STS_LAUNCH((window_prompt_kernel<64, false>), grid, block, 0, s, a);
+  }
+  return sts_take_launch_status();
+}

@@ -1,0 +1,45 @@
+// Declarations shared by the operators around a small cache: the 4-bit cache and attention with a sliding window.
+#pragma once
+
+#include "common.h"
+
+// Attention of short query blocks (Tq <= 16) over a 4-bit cache, or over a bf16 cache with a window (attn_cache.hip).
+// `a` holds what the shared combine kernel reads: shapes, units, partials, outputs and the block's own tokens.
+struct CacheAttnArgs {
+  AttnArgs a;                        // k, v and the strides in elements: bf16 caches; indices NULL: all tokens
+  const uint8_t *codes, *scales;     // 4-bit cache; strides in bytes
+  int64_t code_b, code_h, code_n, code_page;
+  int64_t scale_b, scale_h, scale_n, scale_page;
+  int32_t window, sinks;             // bf16 cache: see sts_window_attn
+  int32_t behind;                    // bf16 cache: 1 = the block's own tokens are not in the cache (k_new)
+};
+
+struct PackedRowsArgs {
+  uint16_t *k, *v;                   // [B,T,Hkv,d]
+  const int32_t *pos, *lens;
+  uint8_t *codes, *scales;
+  int64_t code_b, code_h, code_n, code_page;
+  int64_t scale_b, scale_h, scale_n, scale_page;
+  const int32_t *block_table;
+  int32_t table_stride, num_pages, page_shift, N;
+  int32_t B, T, Hkv, d;
+};
+
+// Attention with a window over many query rows (attn_window.hip)
+struct WindowArgs {
+  const uint16_t *q, *k, *v;
+  int64_t stride_b, stride_h, stride_n, stride_page;     // elements
+  const int32_t *seq_lens, *block_table;
+  int32_t B, Tq, Hq, Hkv, G, N, window, sinks;
+  int32_t page_shift, table_stride, num_pages;
+  float scale, scale_log2;
+  void *out;
+  float *lse_out;
+  int32_t out_dtype;
+};
+
+hipError_t launch_packed_store(const PackedRowsArgs &a, hipStream_t s);
+hipError_t launch_packed_load(const PackedRowsArgs &a, hipStream_t s);
+// far: rows at offsets of more than 32 bits, or pages
+hipError_t launch_cache_attn(const CacheAttnArgs &a, int d, int nq, bool four_bit, bool far, hipStream_t s);
+hipError_t launch_window_prompt(const WindowArgs &a, int d, hipStream_t s);

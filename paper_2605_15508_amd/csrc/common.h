@@ -70,6 +70,42 @@ struct AttnUnitTable {
   uint32_t unit[STS_MAX_HEADS];
 };
 
+// Groups the query heads of every KV group into units of at most max_heads: all of the group (whole_groups), or those with equal
+// head_map values (each on its own without one). Returns the number of units, or -1 if there are too many; max_rows: the most
+// query rows of one.
+inline int sts_group_units(int Hq, int Hkv, int Tq, int max_heads, const int32_t *head_map, bool whole_groups, AttnUnitTable &units,
+                           int &max_rows) {
+  const int G = Hq / Hkv;
+  int nu = 0;
+  max_rows = 0;
+  for (uint32_t &u : units.unit) u = 0;
+  for (int g = 0; g < Hkv; ++g) {
+    bool done[STS_MAX_GROUP] = {false};
+    for (int i = 0; i < G; ++i) {
+      if (done[i]) continue;
+      // members of the set led by head i, in head order
+      int members[STS_MAX_GROUP], nm = 0;
+      for (int j = i; j < G; ++j) {
+        if (done[j]) continue;
+        const bool same = whole_groups || j == i || (head_map && head_map[g * G + j] == head_map[g * G + i]);
+        if (same) {
+          members[nm++] = j;
+          done[j] = true;
+        }
+      }
+      for (int s0 = 0; s0 < nm; s0 += max_heads) {
+        const int cnt = (nm - s0 < max_heads) ? nm - s0 : max_heads;
+        uint32_t mask = 0;
+        for (int m = 0; m < cnt; ++m) mask |= 1u << members[s0 + m];
+        if (nu >= STS_MAX_HEADS) return -1;
+        units.unit[nu++] = (uint32_t)g | (mask << 8) | ((uint32_t)cnt << 24);
+        if (cnt * Tq > max_rows) max_rows = cnt * Tq;
+      }
+    }
+  }
+  return nu;
+}
+
 struct AttnArgs {
   const uint16_t *q, *k, *v;
   const int32_t *indices, *counts, *seq_lens;
@@ -198,6 +234,14 @@ struct UnionArgs {
   uint8_t map[STS_MAX_HEADS]; // target head -> draft head
 };
 hipError_t launch_union_rows(const UnionArgs &a, hipStream_t s);
+
+// host parts of api.hip that the other host files use: a launch under the timing aid, and the compute units of the device
+hipError_t sts_run_launch(int kind, hipStream_t s, hipError_t (*launch)(void *), void *with);
+template <class F>
+inline hipError_t sts_run_kernel(int kind, hipStream_t s, F launch) {
+  return sts_run_launch(kind, s, [](void *f) { return (*static_cast<F *>(f))(); }, &launch);
+}
+int sts_cu_count();
 
 // device address of the current device's copy of the static scratch array (scratch.hip)
 sts_status sts_static_scratch(void **out);
