@@ -141,7 +141,7 @@ sts_status plan_packed(const sts_packed_attn_params *p, CachePlan &pl) {
     return STS_EINVAL;
   }
   const int64_t len = lists ? (int64_t)p->kmax * page : p->cache.N;
-  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 64, p->head_map, !lists, (len + STS_TILE_KEYS - 1) / STS_TILE_KEYS, packed_resident, pl);
+  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, p->head_map, !lists, (len + STS_TILE_KEYS - 1) / STS_TILE_KEYS, packed_resident, pl);
 }
 
 int64_t window_resident(int nq, int d) { return (int64_t)sts_cu_count() * (d == 128 ? 1 : 2); }

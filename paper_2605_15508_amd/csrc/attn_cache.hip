@@ -13,10 +13,14 @@
 //   - V's rows for it are a + 4m, so that the four lane groups load four neighbouring rows at a time;
 //   - K's operand is loaded as it is used, a lane's share of one key's row: no LDS, no exchange. Of a row of 4-bit codes
 //     lane a has the a-th quarter, 16 bytes at head size 128 and one scale; of a bf16 row every fourth chunk of 16 bytes.
-// The codes become bf16 pairs in the chip's conversion, scale included, exactly. V's pairs are two channels of one key and have to
+// S over 4-bit codes: v_mfma_scale_f32_16x16x128_f8f6f4 takes K's codes and scales as they lie in memory, a lane 32 channels of a key
+// and their scale. Q, the other operand, is the sum of two e4m3 numbers, high and low, with a scale per 32 channels: four significant bits
+// each hold the eight of a bf16 exactly down to 2^-10 of the group's largest value, and what lies further down to 2^-18 of it.
+// At head size 64 both halves go into one instruction, K's row taken twice.
+// V's codes become bf16 pairs in the chip's conversion, scale included, exactly. The pairs are two channels of one key and have to
 // become two keys of one channel: two byte permutes per pair of registers, as for bf16.
-// Scales: a lane loads the word of one token of the tile, K's in the lower half of the wave, V's in the upper, makes
-// them the floats that the conversion takes, and the lanes pick theirs up from LDS, one tile ahead of their use.
+// Scales: a lane loads the word of one token of the tile, K's in the lower half of the wave, V's in the upper, and
+// the lanes pick up those of their rows from LDS, one tile ahead of their use: bytes for K, the conversion's floats for V.
 #include "cache.h"
 
 namespace {
@@ -39,6 +43,8 @@ __device__ __forceinline__ int nth_member(uint32_t mask, int n) {
 // the larger of two numbers in one instruction (see attn.hip)
 __device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
 
+__device__ __forceinline__ float top(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
 // maximum over the four lanes 16 apart
 __device__ __forceinline__ float max_over_groups(float x) {
   const uint32_t w = __builtin_bit_cast(uint32_t, x);
@@ -52,11 +58,59 @@ __device__ __forceinline__ float max_over_groups(float x) {
 // a lane's share of a row: K's quarter and V's D / 16 channels
 template <int D, bool FOUR> struct Share;
 template <> struct Share<128, true> { typedef u32x4 k; typedef uint32_t v; };
-template <> struct Share<64, true> { typedef u32x2 k; typedef uint16_t v; };
+template <> struct Share<64, true> { typedef u32x4 k; typedef uint16_t v; };
 template <> struct Share<128, false> { typedef u32x4 k; typedef u32x4 v; };
 template <> struct Share<64, false> { typedef u32x4 k; typedef u32x2 v; };
 
+// bits 0 .. n - 1 of a word, none for n <= 0
+__device__ __forceinline__ uint32_t first_keys(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+
 template <int D, int NQ, bool FOUR> constexpr int tiles_ahead() { return FOUR ? 3 : 2; }
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// The larger magnitude of both halves of 8 words of bf16 pairs
+__device__ __forceinline__ uint32_t largest(const uint32_t (&w)[8]) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t x = w[i] & 0x7fff7fffu;
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x));
+  }
+  const uint32_t lo = m[0], hi = m[1];
+  return max(lo, hi);
+}
+
+// 16 bf16 values as e4m3 numbers hi + lo, each times 2^(s - 127); s puts a group's largest value, of magnitude bits m, at 2^7 .. 2^8 (255 for one
+// that is no number, or infinite: the products are NaN then)
+__device__ __forceinline__ uint32_t q_scale(uint32_t m) { return m >= 0x7f80u ? 255u : (uint32_t)max((int)(m >> 7) - 7, 1); }
+__device__ __forceinline__ void q_halves(const uint32_t (&w)[8], uint32_t s, u32x4 &hi, u32x4 &lo) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  const float f = __builtin_bit_cast(float, s << 23);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s16x2 h = {0, 0}, l = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t x = w[2 * i + e];
+      h = e ? __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, x), f, true)
+            : __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, x), f, false);
+      const f32x2 back = e ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(__builtin_bit_cast(uint32_t, h), f, true)
+                           : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(__builtin_bit_cast(uint32_t, h), f, false);
+      const float r0 = __builtin_bit_cast(float, x << 16) - back[0], r1 = __builtin_bit_cast(float, x & 0xffff0000u) - back[1];
+      l = e ? __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, r0, r1, f, true) : __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, r0, r1, f, false);
+    }
+    hi[i] = __builtin_bit_cast(uint32_t, h);
+    lo[i] = __builtin_bit_cast(uint32_t, l);
+  }
+}
+
+__device__ __forceinline__ f32x4 scaled_product(u32x4 codes, uint32_t k_scale, u32x4 q0, u32x4 q1, uint32_t q_scale, f32x4 c) {
+  const i32x8 A = {(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0};
+  const i32x8 B = {(int)q0[0], (int)q0[1], (int)q0[2], (int)q0[3], (int)q1[0], (int)q1[1], (int)q1[2], (int)q1[3]};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, c, 4 /* e2m1 */, 0 /* e4m3 */, 0, (int)k_scale, 0, (int)q_scale);
+}
 
 __device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale, int byte) {
   switch (byte) {
@@ -70,19 +124,21 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale, int byt
 // FOUR: a 4-bit cache without a window, else a bf16 cache with one. GATHER: the rows come from a list or a page
 // table, at offsets of 64 bits (FAR) or 32.
 template <int D, int NQ, bool FOUR, bool GATHER, bool FAR>
-__global__ void __launch_bounds__(64 * STS_WG_WAVES, NQ == 4 || (!FOUR && D == 128) ? 1 : 2) cache_attn_kernel(const CacheAttnArgs C) {
+__global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) cache_attn_kernel(const CacheAttnArgs C) {
   typedef typename Share<D, FOUR>::k k_t;
   typedef typename Share<D, FOUR>::v v_t;
   typedef typename std::conditional<FAR, uint64_t, uint32_t>::type off_t;
   constexpr int W = STS_WG_WAVES, TK = STS_TILE_KEYS, PF = tiles_ahead<D, NQ, FOUR>();
   constexpr int NT = D / 16, KK = D / 32;
   constexpr int KL = FOUR ? 1 : KK;              // loads of K per lane and half tile
+  constexpr int QR = FOUR ? D / 32 : KK;         // quads of registers of Q per lane and query tile: bf16, or halves in e4m3
   constexpr int OPITCH = D + 4;
   constexpr bool WIN = !FOUR;
   constexpr bool QLDS = NQ >= 2;
-  __shared__ __attribute__((aligned(16))) float lds_o[W * 16 * OPITCH];
+    __shared__ __attribute__((aligned(16))) float lds_o[W * 16 * OPITCH];
   __shared__ float lds_ml[W][NQ * 16][2];
-  __shared__ __attribute__((aligned(16))) u32x4 lds_q[QLDS ? NQ * KK * 64 : 1];
+  __shared__ __attribute__((aligned(16))) u32x4 lds_q[QLDS ? NQ * QR * 64 : 1];
+  __shared__ uint32_t lds_qs[FOUR && QLDS ? NQ : 1][64];
   __shared__ __attribute__((aligned(16))) off_t lds_off[GATHER ? W : 1][2][TK];                // by (slot % 4) * 8 + slot / 4
   __shared__ __attribute__((aligned(16))) uint32_t lds_sc[FOUR ? W : 1][2][2][D / 32][TK];     // [tile parity][K, V][group], slots as above
 
@@ -126,7 +182,8 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, NQ == 4 || (!FOUR && D == 1
   // ---- query rows of this lane: row nq * 16 + b. A negative scale turns the signs of Q, a scale of 0 clears it.
   const uint32_t q_keep = A.scale == 0.f ? 0u : 0xffffffffu, q_flip = A.scale < 0.f ? 0x80008000u : 0u;
   const float sl2 = A.scale == 0.f ? 1.f : fabsf(A.scale_log2);
-  u32x4 Q[QLDS ? 1 : NQ][QLDS ? 1 : KK];
+  u32x4 Q[QLDS ? 1 : NQ][QLDS ? 1 : QR];
+  uint32_t qs[FOUR ? NQ : 1];
   int q_tq[NQ];
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
@@ -135,15 +192,43 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, NQ == 4 || (!FOUR && D == 1
     const int hsel = ok ? r / A.Tq : 0;
     q_tq[nq] = ok ? r - hsel * A.Tq : 0;
     const uint16_t *qp = A.q + (((size_t)bt * A.Tq + q_tq[nq]) * A.Hq + g * A.G + nth_member(mask, hsel)) * D;
+    auto put = [&](int i, u32x4 w) {
+      if (!QLDS) Q[QLDS ? 0 : nq][QLDS ? 0 : i] = w;
+      else lds_q[(nq * QR + i) * 64 + lane] = w;
+    };
+    if (QLDS && wave != nq % W) continue;        // (a query tile by each wave, for all of them)
+    auto get = [&](int chan) { return (*reinterpret_cast<const u32x4 *>(qp + chan) & (ok ? q_keep : 0u)) ^ q_flip; };
+    if constexpr (FOUR) {
+      // Channels 16 a .. of the first 64 and of the rest: the first and the second half of the operand. A group of 32 channels is in
+      // two neighbouring lane groups, and its scale goes to the lane group that has K's share of it.
+      uint32_t s[D / 64];
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      u32x4 w = *reinterpret_cast<const u32x4 *>(qp + (FOUR ? a * (D / 4) + 8 * kk : 8 * (a + 4 * kk)));
-      w = (w & (ok ? q_keep : 0u)) ^ q_flip;
-      if (!QLDS) Q[nq][kk] = w;
-      else if (wave == 0) lds_q[(nq * KK + kk) * 64 + lane] = w;
+      for (int j = 0; j < D / 64; ++j) {
+        const u32x4 w0 = get(64 * j + 16 * a), w1 = get(64 * j + 16 * a + 8);
+        const uint32_t w[8] = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
+        uint32_t m = largest(w);
+        m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+        s[j] = q_scale(m);
+        u32x4 hi, lo;
+        q_halves(w, s[j], hi, lo);
+        put(D == 128 ? j : 0, hi);
+        put(D == 128 ? 2 + j : 1, lo);
+      }
+      const uint32_t s0 = s[0], s1 = s[D / 64 - 1];
+      const uint32_t o0 = (uint32_t)__shfl_xor((int)s0, 48, 64), o1 = (uint32_t)__shfl_xor((int)s1, 48, 64);
+      qs[nq] = a == 0 ? s0 : a == 3 ? s1 : a == 1 ? o0 : o1;
+      if (QLDS) lds_qs[QLDS ? nq : 0][lane] = qs[nq];
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) put(kk, get(8 * (a + 4 * kk)));
     }
   }
-  if (QLDS) __syncthreads();
+  if (QLDS) {
+    __syncthreads();
+    if (FOUR)
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) qs[FOUR ? nq : 0] = lds_qs[FOUR ? nq : 0][lane];
+  }
 
   float m_run[NQ], l_run[NQ];
   f32x4 acc[NQ][NT];
@@ -166,7 +251,8 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, NQ == 4 || (!FOUR && D == 1
   const unsigned char *kuni = (FOUR ? C.codes : reinterpret_cast<const unsigned char *>(A.k)) + head_off;
   const unsigned char *vuni = (FOUR ? C.codes + D / 2 : reinterpret_cast<const unsigned char *>(A.v)) + head_off;
   const unsigned char *suni = FOUR ? C.scales + (paged ? 0 : bt * C.scale_b) + g * C.scale_h : nullptr;
-  constexpr int KCH = FOUR ? D / 8 : 16, VCH = FOUR ? D / 32 : D / 8;      // bytes of a lane's chunk
+  constexpr int VCH = FOUR ? D / 32 : D / 8;      // bytes of a lane's chunk of V
+  const int k_chunk = FOUR && D == 64 ? (a & 1) * 16 : a * 16;
   const int slot = lane & 31, slot_at = (slot & 3) * 8 + (slot >> 2);
   const int k_slot = (b >> 2) + 4 * (b & 3), k_at = (b >> 2) * 8 + (b & 3);
   const uint32_t half = FOUR && D == 128 ? (lane >> 5) * 4 : 0;            // K's or V's word of a token's scales
@@ -182,27 +268,28 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, NQ == 4 || (!FOUR && D == 1
   uint32_t k_off[2], v_off[8];
   if (!GATHER) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) k_off[h] = (uint32_t)((k_slot + 16 * h) * (int)row_bytes);
+    for (int h = 0; h < 2; ++h) k_off[h] = (uint32_t)((k_slot + 16 * h) * (int)row_bytes + k_chunk);
 #pragma unroll
-    for (int m = 0; m < 8; ++m) v_off[m] = (uint32_t)((a + 4 * m) * (int)row_bytes);
+    for (int m = 0; m < 8; ++m) v_off[m] = (uint32_t)((a + 4 * m) * (int)row_bytes + b * VCH);
   }
   auto seen_row = [&](int n) { return WIN && n >= C.sinks && n < lo ? lo : n; };
   auto issue_near = [&](int t, Tile &R) {
     const int n0 = first_of(t);
+    // (the scales first: they are waited for a tile before the rest)
+    if (FOUR) R.sc = *reinterpret_cast<const uint32_t *>(suni + n0 * C.scale_n + (min(slot, c - 1 - n0) * (int)C.scale_n + (int)half));
     const unsigned char *kb = kuni + n0 * row_bytes, *vb = vuni + n0 * row_bytes;
     if (WIN && n0 < lo) {               // tiles of sinks, and the one that the window begins in
 #pragma unroll
-      for (int h = 0; h < 2; ++h) load_k(kuni + min(seen_row(n0 + k_slot + 16 * h), c - 1) * row_bytes, (off_t)(a * KCH), R.k[h]);
+      for (int h = 0; h < 2; ++h) load_k(kuni + min(seen_row(n0 + k_slot + 16 * h), c - 1) * row_bytes, (off_t)k_chunk, R.k[h]);
 #pragma unroll
       for (int m = 0; m < 8; ++m) R.v[m] = load_v(vuni + min(seen_row(n0 + a + 4 * m), c - 1) * row_bytes, (off_t)(b * VCH));
     } else {
-      const uint32_t last = (uint32_t)(min(c - 1 - n0, TK - 1) * (int)row_bytes);
+      const uint32_t last = (uint32_t)(min(c - 1 - n0, TK - 1) * (int)row_bytes), last_k = last + k_chunk, last_v = last + b * VCH;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) load_k(kb, (off_t)(min(k_off[h], last) + a * KCH), R.k[h]);
+      for (int h = 0; h < 2; ++h) load_k(kb, (off_t)min(k_off[h], last_k), R.k[h]);
 #pragma unroll
-      for (int m = 0; m < 8; ++m) R.v[m] = load_v(vb, (off_t)(min(v_off[m], last) + b * VCH));
+      for (int m = 0; m < 8; ++m) R.v[m] = load_v(vb, (off_t)min(v_off[m], last_v));
     }
-    if (FOUR) R.sc = *reinterpret_cast<const uint32_t *>(suni + n0 * C.scale_n + (min(slot, c - 1 - n0) * (int)C.scale_n + (int)half));
   };
 
   // gather: list entry (or block) -> page -> offset, each a step of its own
@@ -227,34 +314,34 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, NQ == 4 || (!FOUR && D == 1
   };
   auto issue_far = [&](int par, Tile &R) {
     off_t ko[2], vo[8];
+    if (FOUR) R.sc = *reinterpret_cast<const uint32_t *>(suni + scale_off);
 #pragma unroll
     for (int h = 0; h < 2; ++h) ko[h] = lds_off[GATHER ? wave : 0][par][k_at + 4 * h];
 #pragma unroll
     for (int m = 0; m < 8; ++m) vo[m] = lds_off[GATHER ? wave : 0][par][a * 8 + m];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) load_k(kuni, ko[h] + (off_t)(a * KCH), R.k[h]);
+    for (int h = 0; h < 2; ++h) load_k(kuni, ko[h] + (off_t)k_chunk, R.k[h]);
 #pragma unroll
     for (int m = 0; m < 8; ++m) R.v[m] = load_v(vuni, vo[m] + (off_t)(b * VCH));
-    if (FOUR) R.sc = *reinterpret_cast<const uint32_t *>(suni + scale_off);
   };
 
   // ---- scales of one tile: own token's word -> LDS -> the two of K's rows and the eight of V's
   uint32_t ks[2], vs[8];
   auto put_scales = [&](uint32_t w, int par) {
     if constexpr (FOUR) {
-      const int kv = D == 128 ? lane >> 5 : 0;
+      const int kv = D == 128 ? lane >> 5 : 0, up = kv ? 23 : 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t f = (j == 0 ? w << 23 : j == 1 ? w << 15 : j == 2 ? w << 7 : w >> 1) & 0x7f800000u;
-        if (D == 128) lds_sc[wave][par][kv][j & (D / 32 - 1)][slot_at] = f;
-        else lds_sc[wave][par][j >> 1][j & 1][slot_at] = f;
+        const uint32_t s = (w >> (8 * j)) & 255u;
+        if (D == 128) lds_sc[wave][par][kv][j & (D / 32 - 1)][slot_at] = s << up;
+        else lds_sc[wave][par][j >> 1][j & 1][slot_at] = j >= 2 ? s << 23 : s;
       }
     }
   };
   auto get_scales = [&](int par) {
     if constexpr (FOUR) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) ks[h] = lds_sc[wave][par][0][a * (D / 32) / 4][k_at + 4 * h];
+      for (int h = 0; h < 2; ++h) ks[h] = lds_sc[wave][par][0][a & (D / 32 - 1)][k_at + 4 * h];
 #pragma unroll
       for (int m = 0; m < 8; ++m) vs[m] = lds_sc[wave][par][1][b * (D / 32) / 16][a * 8 + m];
     }
@@ -262,79 +349,107 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, NQ == 4 || (!FOUR && D == 1
 
   // ---- one tile
   auto consume = [&](const Tile &R, int t, uint32_t tile_mask) {
-    f32x4 St[NQ][2];
-#pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) St[nq][0] = St[nq][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      u32x4 Ka[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if constexpr (FOUR) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) Ka[h][j] = pair_of(R.k[h][0][kk], __builtin_bit_cast(float, ks[h]), j);
-        } else {
-          Ka[h] = R.k[h][kk];
-        }
-      }
-#pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) {
-        const u32x4 Qb = QLDS ? lds_q[(nq * KK + kk) * 64 + lane] : Q[QLDS ? 0 : nq][QLDS ? 0 : kk];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          St[nq][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, Ka[h]), __builtin_bit_cast(bf16x8, Qb), St[nq][h], 0, 0, 0);
-      }
-    }
-    // (V's conversions do not move up here, where their results would take the registers of the tiles on the way)
-    if (FOUR && NQ >= 2) __builtin_amdgcn_sched_barrier(0);
-    // keys that a row does not see score -inf
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    auto q_at = [&](int nq, int i) { return QLDS ? lds_q[(nq * QR + i) * 64 + lane] : Q[QLDS ? 0 : nq][QLDS ? 0 : i]; };
     const int n0 = first_of(t);
     bool partly = false;                 // some row does not see some key
-    auto sees = [&](int n, int nq) {
+    // which of the tile's keys query row q_tq[nq] sees: those up to it, without those between the sinks and its window
+    auto seen_keys = [&](int nq) {
       const int p = p0 + q_tq[nq];
-      return n < c && n <= p && (n < C.sinks || p - n < C.window);
+      return first_keys(min(p + 1, c) - n0) & (first_keys(C.sinks - n0) | ~first_keys((int)max((int64_t)p - C.window + 1, (int64_t)0) - n0));
     };
     if constexpr (WIN) {
       const int pl = p0 + A.Tq - 1;
       partly = !(n0 + TK <= c && n0 + TK - 1 <= p0 && (n0 + TK <= C.sinks || pl - n0 < C.window));
-      if (partly) {
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq)
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (!sees(n0 + a + 4 * i, nq)) St[nq][i >> 2][i & 3] = -INFINITY;
-      }
-    } else if (tile_mask != 0xffffffffu) {
-#pragma unroll
-      for (int nq = 0; nq < NQ; ++nq)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (!((tile_mask >> (a + 4 * i)) & 1u)) St[nq][i >> 2][i & 3] = -INFINITY;
     }
     u32x4 P[NQ];
+    {
+      f32x4 St[NQ][2];
+      if constexpr (FOUR) {
 #pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) {
-      const f32x4 s0 = St[nq][0], s1 = St[nq][1];
-      const float mt = sl2 * max_over_groups(larger(larger(larger(s0[0], s0[1]), larger(s0[2], s0[3])), larger(larger(s1[0], s1[1]), larger(s1[2], s1[3]))));
-      if (__builtin_amdgcn_ballot_w64(mt > m_run[nq]) != 0) {
-        const float m_new = larger(m_run[nq], mt);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[nq] - m_new);
-        l_run[nq] *= alpha;
-        m_run[nq] = m_new;
+        for (int j = 0; j < NQ; ++j) {
+          const u32x4 q0 = q_at(j, 0), q1 = q_at(j, 1);
+          const uint32_t s = qs[FOUR ? j : 0];
+          f32x4 x[2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[nq][nt] *= alpha;
+          for (int h = 0; h < 2; ++h) x[h] = scaled_product(R.k[h][0], ks[h], q0, q1, s, zero);
+          if constexpr (D == 128) {
+            const u32x4 l0 = q_at(j, 2), l1 = q_at(j, 3);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) St[j][h] = scaled_product(R.k[h][0], ks[h], l0, l1, s, x[h]);
+            // The instruction takes eight passes: a result in registers that are partly an operand's would be wrong, and the compiler
+            // sees to that for larger results only. So all operands are in use until the results are there.
+            asm volatile("" ::"v"(St[j][0]), "v"(St[j][1]), "v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(l0), "v"(l1), "v"(R.k[0][0]), "v"(R.k[1][0]));
+          } else {
+            St[j][0] = x[0];
+            St[j][1] = x[1];
+            asm volatile("" ::"v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(R.k[0][0]), "v"(R.k[1][0]));
+          }
+        }
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+          for (int j = 0; j < NQ; ++j) {
+            const u32x4 Qb = q_at(j, kk);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const u32x4 Ka = R.k[h][FOUR ? 0 : kk];
+              St[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, Ka), __builtin_bit_cast(bf16x8, Qb), kk ? St[j][h] : zero, 0, 0, 0);
+            }
+          }
       }
-      const float m_ref = WIN && m_run[nq] == -INFINITY ? 0.f : m_run[nq];
-      float p[8], sum = 0.f;
+      // (V's conversions do not move up here, where their results would take the registers of the tiles on the way)
+      if (FOUR && NQ >= 2) __builtin_amdgcn_sched_barrier(0);
+      // keys that a row does not see score -inf
+      if (WIN ? partly : tile_mask != 0xffffffffu) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(St[nq][i >> 2][i & 3], sl2, -m_ref));
-        sum += p[i];
+        for (int j = 0; j < NQ; ++j) {
+          const int mine = (int)((WIN ? seen_keys(j) : tile_mask) >> a);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(mine, 4 * i, 1);
+            const float x = St[j][i >> 2][i & 3];
+            St[j][i >> 2][i & 3] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) & keep) | (0xff800000u & ~keep));
+          }
+        }
       }
-      l_run[nq] += sum;
-      // the weights enter the second product as bf16 (half a step, 2^-9 of each), the sum above in fp32
+      // Most tiles of a long list raise no row's maximum: it is put together from the four lanes of a row only where one of them does.
+      float mine[NQ];
+      bool grown = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) P[nq][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p[2 * i], p[2 * i + 1]}), bf16x2));
+      for (int j = 0; j < NQ; ++j) {
+        const f32x4 s0 = St[j][0], s1 = St[j][1];
+        mine[j] = sl2 * top(top(top(s0[0], s0[1]), top(s0[2], s0[3])), top(top(s1[0], s1[1]), top(s1[2], s1[3])));
+        grown |= mine[j] > m_run[j];
+      }
+      if (__builtin_amdgcn_ballot_w64(grown) != 0) {
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+          const int nq = j;
+          const float m_new = larger(m_run[nq], max_over_groups(mine[j]));
+          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[nq] - m_new);
+          l_run[nq] *= alpha;
+          m_run[nq] = m_new;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) acc[nq][nt] *= alpha;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NQ; ++j) {
+        const int nq = j;
+        const float m_ref = WIN && m_run[nq] == -INFINITY ? 0.f : m_run[nq];
+        float p[8], sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(St[j][i >> 2][i & 3], sl2, -m_ref));
+          sum += p[i];
+        }
+        l_run[nq] += sum;
+        // the weights enter the second product as bf16 (half a step, 2^-9 of each), the sum above in fp32
+#pragma unroll
+        for (int i = 0; i < 4; ++i) P[nq][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p[2 * i], p[2 * i + 1]}), bf16x2));
+      }
     }
     // pair j of channels of the lane's 8 keys, and of those the keys of channel 2 j (hi: 2 j + 1) as pairs
     auto v_pairs = [&](int j, uint32_t (&w)[8]) {
@@ -363,7 +478,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, NQ == 4 || (!FOUR && D == 1
           for (int key = 0; key < TK; ++key) {
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq) {
-              const bool see = sees(n0 + key, nq);
+              const bool see = (seen_keys(nq) >> key) & 1u;
               u32x4 own;
 #pragma unroll
               for (int i = 0; i < 4; ++i) own[i] = (a + 8 * i == key ? 0xffffu : 0u) | (a + 8 * i + 4 == key ? 0xffff0000u : 0u);
@@ -562,11 +677,9 @@ hipError_t launch(const CacheAttnArgs &a, bool four_bit, bool far, hipStream_t s
     if (far) STS_LAUNCH((cache_attn_kernel<D, NQ, true, true, true>), grid, block, 0, s, a);
     else if (gather) STS_LAUNCH((cache_attn_kernel<D, NQ, true, true, false>), grid, block, 0, s, a);
     else STS_LAUNCH((cache_attn_kernel<D, NQ, true, false, false>), grid, block, 0, s, a);
-  } else if constexpr (NQ <= 2) {
+  } else {
     if (far) STS_LAUNCH((cache_attn_kernel<D, NQ, false, true, true>), grid, block, 0, s, a);
     else STS_LAUNCH((cache_attn_kernel<D, NQ, false, false, false>), grid, block, 0, s, a);
-  } else {
-    return hipErrorInvalidValue;
   }
   return sts_take_launch_status();
 }
@@ -575,6 +688,7 @@ hipError_t launch(const CacheAttnArgs &a, bool four_bit, bool far, hipStream_t s
 
 hipError_t launch_cache_attn(const CacheAttnArgs &a, int d, int nq, bool four_bit, bool far, hipStream_t s) {
   if ((size_t)a.a.B * a.a.num_units * a.a.num_splits == 0) return hipSuccess;
-  if (d == 128) return nq == 1 ? launch<128, 1>(a, four_bit, far, s) : nq == 2 ? launch<128, 2>(a, four_bit, far, s) : launch<128, 4>(a, four_bit, far, s);
-  return nq == 1 ? launch<64, 1>(a, four_bit, far, s) : nq == 2 ? launch<64, 2>(a, four_bit, far, s) : launch<64, 4>(a, four_bit, far, s);
+  if (nq > 2) return hipErrorInvalidValue;
+  if (d == 128) return nq == 1 ? launch<128, 1>(a, four_bit, far, s) : launch<128, 2>(a, four_bit, far, s);
+  return nq == 1 ? launch<64, 1>(a, four_bit, far, s) : launch<64, 2>(a, four_bit, far, s);
 }
