@@ -92,30 +92,29 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
     return min(n, end - 1);
   };
   typedef __attribute__((address_space(3))) unsigned char *lds_ptr;
-  auto load = [&](int t, u32x4 *k, u32x4 *v) {
-    const int n0 = first_of(t);
+  // K's or V's tile t (past the last: the last again, which nobody reads)
+  auto load = [&](int t, const unsigned char *from, u32x4 *to, bool is_v) {
+    const int n0 = first_of(min(t, tiles - 1));
     int l_row = row0, l_slot = slot0;
-    asm("" : "+v"(l_row), "+v"(l_slot));         // (as in consume)
-    if constexpr (PAGED) {
+    asm("" : "+v"(l_row), "+v"(l_slot));         // (what comes of them is made anew in every tile, not kept in registers)
+    const bool inside = n0 >= lo && n0 + TK <= end;
+    uint32_t off[NL];
 #pragma unroll
-      for (int m = 0; m < NL; ++m) {
-        const int row = l_row + RL * m, n = row_of(n0 + row);
-        const int page = min(max(table[n >> A.page_shift], 0), A.num_pages - 1);
-        const int64_t off = (page * A.stride_page + (n & ((1 << A.page_shift) - 1)) * A.stride_n) * 2;
+    for (int m = 0; m < NL; ++m) off[m] = (uint32_t)(l_row + RL * m);
+    if (!inside)
+#pragma unroll
+      for (int m = 0; m < NL; ++m) off[m] = (uint32_t)(row_of(n0 + l_row + RL * m) - n0);
+#pragma unroll
+    for (int m = 0; m < NL; ++m) {
+      const int row = l_row + RL * m, chunk = 16 * (is_v ? v_chunk<D>(row, l_slot) : k_chunk<D>(row, l_slot));
+      const lds_ptr dst = (lds_ptr)(to + (wave * NL + m) * 64);
+      if constexpr (PAGED) {
         typedef const __attribute__((address_space(1))) unsigned char *global_ptr;
-        __builtin_amdgcn_global_load_lds((global_ptr)(kbase + off + 16 * k_chunk<D>(row, l_slot)), (lds_ptr)(k + (wave * NL + m) * 64), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((global_ptr)(vbase + off + 16 * v_chunk<D>(row, l_slot)), (lds_ptr)(v + (wave * NL + m) * 64), 16, 0, 0);
-      }
-    } else {
-      const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(kbase + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
-      const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(vbase + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
-      const bool inside = n0 >= lo && n0 + TK <= end;
-#pragma unroll
-      for (int m = 0; m < NL; ++m) {
-        const int row = l_row + RL * m;
-        const uint32_t off = (uint32_t)((inside ? row : row_of(n0 + row) - n0) * (int)row_bytes);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_ptr)(k + (wave * NL + m) * 64), 16, (int)(off + 16 * k_chunk<D>(row, l_slot)), 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_ptr)(v + (wave * NL + m) * 64), 16, (int)(off + 16 * v_chunk<D>(row, l_slot)), 0, 0, 0);
+        const int n = n0 + (int)off[m], page = min(max(table[n >> A.page_shift], 0), A.num_pages - 1);
+        __builtin_amdgcn_global_load_lds((global_ptr)(from + (page * A.stride_page + (n & ((1 << A.page_shift) - 1)) * A.stride_n) * 2 + chunk), dst, 16, 0, 0);
+      } else {
+        const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(from + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, dst, 16, (int)(off[m] * (uint32_t)row_bytes + chunk), 0, 0, 0);
       }
     }
   };
@@ -146,48 +145,53 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
     return w;
   };
 
-  auto consume = [&](int t, const u32x4 *k, const u32x4 *v) {
-    const int n0 = first_of(t);
-    int k_at = k_lane, v_at = v_lane;
-    asm("" : "+v"(k_at), "+v"(v_at));            // (what comes of them is made anew in every tile, not kept in registers)
-    f32x16 S[2];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) S[kt][i] = 0.f;
+  // which keys of the tile at n0 the lane's query sees, a bit each: those up to it, without those between the sinks and its window
+  auto seen_keys = [&](int n0) {
+    return first_keys(p + 1 - n0) & (first_keys(A.sinks - n0) | ~first_keys((int)max((int64_t)p - A.window + 1, (int64_t)0) - n0));
+  };
+  auto masked = [&](int t) { return !whole(first_of(t), w_lo, w_hi); };        // (of the wave's queries)
+  // S of one tile
+  auto product = [&](const u32x4 *k, f32x16 (&S)[2]) {
+    int k_at = k_lane;
+    asm("" : "+v"(k_at));                        // (what comes of it is made anew in every tile, not kept in registers)
+    const f32x16 zero = {};
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
         const bf16x8 Ka = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)k + (k_at ^ (32 * s)) + 32 * kt * CH * 16));
-        S[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Ka, Q[s], S[kt], 0, 0, 0);
+        S[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Ka, Q[s], s ? S[kt] : zero, 0, 0, 0);
       }
-    auto sees = [&](int n) { return n <= p && (n < A.sinks || p - n < A.window); };       // (n < L follows from n <= p)
-    const bool partly = !whole(n0, w_lo, w_hi);
-    if (partly) {
-      // a bit per key of the tile, then per half of the wave: keys up to the query, without those between the sinks and the window
-      const uint64_t seen = (first_keys(p + 1 - n0) & (first_keys(A.sinks - n0) | ~first_keys((int)max((int64_t)p - A.window + 1, (int64_t)0) - n0))) >> (4 * h);
+  };
+  // keys that the query does not see score -inf
+  auto hide = [&](int n0, f32x16 (&S)[2]) {
+    const uint64_t seen = seen_keys(n0) >> (4 * h);
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const int word = (int)(uint32_t)(seen >> (32 * kt));
+    for (int kt = 0; kt < 2; ++kt) {
+      const int word = (int)(uint32_t)(seen >> (32 * kt));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(word, (i & 3) + 8 * (i >> 2), 1), x = __builtin_bit_cast(uint32_t, (float)S[kt][i]);
-          S[kt][i] = __builtin_bit_cast(float, (x & keep) | (0xff800000u & ~keep));
-        }
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(word, (i & 3) + 8 * (i >> 2), 1);
+        const float x = S[kt][i];
+        S[kt][i] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) & keep) | (0xff800000u & ~keep));
       }
     }
-    float mt = top(S[0][0], S[1][0]);
+  };
+  auto highest = [&](const f32x16 (&S)[2]) {
+    float m[4];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mt = top(mt, top(S[0][i], S[1][i]));
-    {
-      const uint32_t w = __builtin_bit_cast(uint32_t, mt);
+    for (int j = 0; j < 4; ++j) m[j] = top(S[0][j], S[1][j]);
+#pragma unroll
+    for (int i = 4; i < 16; ++i) m[i & 3] = top(m[i & 3], top(S[0][i], S[1][i]));
+    return sl2 * top(top(m[0], m[1]), top(m[2], m[3]));
+  };
+  // the running maximum takes in a tile's; both halves of the wave hold half of a query's scores
+  auto raise = [&](float mine) {
+    if (__builtin_amdgcn_ballot_w64(mine > m_run) != 0) {
+      const uint32_t w = __builtin_bit_cast(uint32_t, mine);
       const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
       const uint32_t q0 = q[0], q1 = q[1];
-      mt = sl2 * top(__builtin_bit_cast(float, q0), __builtin_bit_cast(float, q1));
-    }
-    if (__builtin_amdgcn_ballot_w64(mt > m_run) != 0) {
-      const float m_new = fmaxf(m_run, mt);
+      const float m_new = fmaxf(m_run, top(__builtin_bit_cast(float, q0), __builtin_bit_cast(float, q1)));
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= alpha;
       m_run = m_new;
@@ -196,76 +200,117 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
     }
+  };
+  // exp(S - m), as the B operands of the second product (bf16, half a step, 2^-9 of each), and their sum in fp32
+  auto weights = [&](const f32x16 (&S)[2], u32x4 (&P)[4]) {
     const float m_ref = m_run == -INFINITY ? 0.f : m_run;
-    u32x4 P[4];
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * e], sl2, -m_ref));
         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * e + 1], sl2, -m_ref));
-        l_run += p0;
-        l_run += p1;
-        // the weights enter the second product as bf16 (half a step, 2^-9 of each), the sum in fp32
+        sum[e] += p0 + p1;
         P[s][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
       }
-    bool odd = false;        // values that are no numbers, or infinite, in a tile that not everyone sees
-    if (partly) {
-      uint32_t any = 0;
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+  // a tile that not every query sees whole, with a value that is no number, or infinite
+  auto odd_values = [&](int t, const u32x4 *v) {
+    if (!masked(t)) return false;
+    uint32_t any = 0;
 #pragma unroll
-      for (int m = 0; m < TK * CH / 64; ++m) {
-        const u32x4 w = *(lds_u32x4)((lds_ptr)v + 16 * lane + 1024 * m);
+    for (int m = 0; m < TK * CH / 64; ++m) {
+      const u32x4 w = *(lds_u32x4)((lds_ptr)v + 16 * lane + 1024 * m);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) any |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
-      }
-      odd = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+      for (int e = 0; e < 4; ++e) any |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
     }
-    if (odd) {
-      // key by key, and only where it is seen
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-        for (int key = 0; key < 16; ++key) {
-          u32x4 own;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
-            own[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
-          }
-          const bool see = sees(n0 + 16 * s + key);
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            f32x16 z;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = 0.f;
-            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v, v_at, dt, s) & own), __builtin_bit_cast(bf16x8, P[s] & own), z, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[dt][i] += see ? z[i] : 0.f;
-            __builtin_amdgcn_sched_barrier(0);         // (one product's registers at a time)
-          }
-        }
-    } else {
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v, v_at, dt, s)), __builtin_bit_cast(bf16x8, P[s]), acc[dt], 0, 0, 0);
-    }
+    return __builtin_amdgcn_ballot_w64(any != 0) != 0;
   };
 
+  // ---- The next tile's scores are worked out while this one's weights are: matrix and vector instructions of one wave, which do not wait
+  // for each other. K is a tile ahead of V.
   auto arrived = [] { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); };
+  bool later = false;              // tiles left for the end: see below
   if (tiles > 0) {
-    load(0, lds_k0, lds_v0);
+    f32x16 S[2];
+    load(0, kbase, lds_k0, false);
     arrived();
-    int t = 0;
-    for (;;) {
-      if (t + 1 < tiles) load(t + 1, lds_k1, lds_v1);
-      consume(t, lds_k0, lds_v0);
-      if (++t >= tiles) break;
+    load(1, kbase, lds_k1, false);
+    load(0, vbase, lds_v0, true);
+    product(lds_k0, S);
+    if (masked(0)) hide(first_of(0), S);
+    raise(highest(S));
+    auto step = [&](int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
       arrived();
-      if (t + 1 < tiles) load(t + 1, lds_k0, lds_v0);
-      consume(t, lds_k1, lds_v1);
-      if (++t >= tiles) break;
-      arrived();
+      load(t + 2, kbase, k_free, false);
+      load(t + 1, vbase, v_free, true);
+      const bool odd = odd_values(t, v);
+      f32x16 N[2];
+      u32x4 P[4];
+      product(k_next, N);
+      const float sum = weights(S, P);
+      if (!odd) {
+        l_run += sum;
+        int v_at = v_lane;
+        asm("" : "+v"(v_at));
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v, v_at, dt, s)), __builtin_bit_cast(bf16x8, P[s]), acc[dt], 0, 0, 0);
+      }
+      later |= odd;
+      if (t + 1 < tiles) {
+        if (masked(t + 1)) hide(first_of(t + 1), N);
+        raise(highest(N));
+      }
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) S[kt] = N[kt];
+    };
+    for (int t = 0;; t += 2) {
+      step(t, lds_k1, lds_k0, lds_v0, lds_v1);
+      if (t + 1 >= tiles) break;
+      step(t + 1, lds_k0, lds_k1, lds_v1, lds_v0);
+      if (t + 2 >= tiles) break;
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);              // all that was asked for has come
+    // What is infinite or no number must not reach queries that do not see it, and 0 times it is not 0: such tiles come last, key by key, and
+    // a key's row is taken in only where it is seen.
+    if (__syncthreads_or(later)) {
+      for (int t = 0; t < tiles; ++t) {
+        arrived();
+        load(t, kbase, lds_k0, false);
+        load(t, vbase, lds_v0, true);
+        arrived();
+        if (!odd_values(t, lds_v0)) continue;
+        u32x4 P[4];
+        product(lds_k0, S);
+        hide(first_of(t), S);
+        l_run += weights(S, P);
+        const uint64_t seen = seen_keys(first_of(t));
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          for (int key = 0; key < 16; ++key) {
+            u32x4 own;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
+              own[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
+            }
+            const bool see = (seen >> (16 * s + key)) & 1u;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+              const f32x16 zero = {};
+              const f32x16 z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(lds_v0, v_lane, dt, s) & own),
+                                                                       __builtin_bit_cast(bf16x8, P[s] & own), zero, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) acc[dt][i] += see ? z[i] : 0.f;
+              __builtin_amdgcn_sched_barrier(0);         // (one product's registers at a time)
+            }
+          }
+      }
     }
   }
 
