@@ -61,14 +61,14 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
   const int w_lo = p_first + (int)(min((int64_t)blk * ROWS + wave * 32, rows - 1)) / A.G;                                       // the wave's
   const int w_hi = p_first + (int)(min((int64_t)blk * ROWS + wave * 32 + 31, rows - 1)) / A.G;
 
-  // keys 0 .. sinks - 1 and lo .. end - 1
-  const int end = min(b_hi + 1, L);
-  const int lo = (int)max((int64_t)b_lo - A.window + 1, (int64_t)0);
-  const int tiles_end = end > 0 ? (end + TK - 1) / TK : 0;
-  const int sink_tiles = min((min(A.sinks, max(end, 0)) + TK - 1) / TK, lo / TK);
-  const int skipped = lo / TK - sink_tiles;
-  const int tiles = max(tiles_end - skipped, 0);
-  auto first_of = [&](int t) { return (t >= sink_tiles ? t + skipped : t) * TK; };
+  // The keys that some query of the block sees, one after the other: those of `firsts` sinks before lo, then lo .. end - 1. Place v holds key v, or
+  // v + skipped from `firsts` on.
+  const int end = max(min(b_hi + 1, L), 0);
+  const int lo = (int)min(max((int64_t)b_lo - A.window + 1, (int64_t)0), (int64_t)end);
+  const int firsts = min(A.sinks, lo), skipped = lo - firsts;
+  const int places = end - skipped, tiles = (places + TK - 1) / TK;
+  // the key at a tile's first place, if that is none of the sinks
+  auto first_of = [&](int t) { return t * TK + skipped; };
 
   // ---- Q, as the B operand: channels 16 s + 8 h .. of query col. The scale's sign goes to Q.
   const uint32_t q_keep = A.scale == 0.f ? 0u : 0xffffffffu, q_flip = A.scale < 0.f ? 0x80008000u : 0u;
@@ -87,39 +87,45 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
   const int64_t row_bytes = A.stride_n * 2, head_off = ((PAGED ? 0 : bt * A.stride_b) + g * A.stride_h) * 2;
   const unsigned char *kbase = reinterpret_cast<const unsigned char *>(A.k) + head_off, *vbase = reinterpret_cast<const unsigned char *>(A.v) + head_off;
   const int32_t *table = PAGED ? A.block_table + (size_t)bt * A.table_stride : nullptr;
-  auto row_of = [&](int n) {
-    n = n >= A.sinks && n < lo ? lo : n;
-    return min(n, end - 1);
+  auto row_of = [&](int v) {           // (past the last place: the last key)
+    v = min(v, places - 1);
+    return v < firsts ? v : v + skipped;
   };
   typedef __attribute__((address_space(3))) unsigned char *lds_ptr;
+  // where a lane's chunks of a tile lie, counted from its first row
+  uint32_t k_off[NL], v_off[NL];
+#pragma unroll
+  for (int m = 0; m < NL; ++m) {
+    const int row = row0 + RL * m;
+    k_off[m] = (uint32_t)(row * (int)row_bytes + 16 * k_chunk<D>(row, slot0));
+    v_off[m] = (uint32_t)(row * (int)row_bytes + 16 * v_chunk<D>(row, slot0));
+  }
   // K's or V's tile t (past the last: the last again, which nobody reads)
   auto load = [&](int t, const unsigned char *from, u32x4 *to, bool is_v) {
-    const int n0 = first_of(min(t, tiles - 1));
-    int l_row = row0, l_slot = slot0;
-    asm("" : "+v"(l_row), "+v"(l_slot));         // (what comes of them is made anew in every tile, not kept in registers)
-    const bool inside = n0 >= lo && n0 + TK <= end;
-    uint32_t off[NL];
+    const int v0 = min(t, tiles - 1) * TK, n0 = v0 + skipped;
+    u32x4 *const mine = to + wave * NL * 64;
+    auto chunk = [&](int m) { return 16 * (is_v ? v_chunk<D>(row0 + RL * m, slot0) : k_chunk<D>(row0 + RL * m, slot0)); };
+    if (!PAGED && v0 >= firsts && v0 + TK <= places) {
+      const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(from + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
 #pragma unroll
-    for (int m = 0; m < NL; ++m) off[m] = (uint32_t)(l_row + RL * m);
-    if (!inside)
+      for (int m = 0; m < NL; ++m) __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_ptr)(mine + 64 * m), 16, (int)(is_v ? v_off[m] : k_off[m]), 0, 0, 0);
+    } else {
+      // (sinks, the cache's end, pages: any row at any distance)
+      typedef const __attribute__((address_space(1))) unsigned char *global_ptr;
 #pragma unroll
-      for (int m = 0; m < NL; ++m) off[m] = (uint32_t)(row_of(n0 + l_row + RL * m) - n0);
-#pragma unroll
-    for (int m = 0; m < NL; ++m) {
-      const int row = l_row + RL * m, chunk = 16 * (is_v ? v_chunk<D>(row, l_slot) : k_chunk<D>(row, l_slot));
-      const lds_ptr dst = (lds_ptr)(to + (wave * NL + m) * 64);
-      if constexpr (PAGED) {
-        typedef const __attribute__((address_space(1))) unsigned char *global_ptr;
-        const int n = n0 + (int)off[m], page = min(max(table[n >> A.page_shift], 0), A.num_pages - 1);
-        __builtin_amdgcn_global_load_lds((global_ptr)(from + (page * A.stride_page + (n & ((1 << A.page_shift) - 1)) * A.stride_n) * 2 + chunk), dst, 16, 0, 0);
-      } else {
-        const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(from + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, dst, 16, (int)(off[m] * (uint32_t)row_bytes + chunk), 0, 0, 0);
+      for (int m = 0; m < NL; ++m) {
+        const int n = row_of(v0 + row0 + RL * m);
+        int64_t at = n * row_bytes;
+        if (PAGED) at = (min(max(table[n >> A.page_shift], 0), A.num_pages - 1) * A.stride_page + (n & ((1 << A.page_shift) - 1)) * A.stride_n) * 2;
+        __builtin_amdgcn_global_load_lds((global_ptr)(from + at + chunk(m)), (lds_ptr)(mine + 64 * m), 16, 0, 0);
       }
     }
   };
-  // does every query of a range lo_p .. hi_p see all keys of the tile at n0?
-  auto whole = [&](int n0, int lo_p, int hi_p) { return n0 + TK - 1 <= lo_p && (n0 + TK <= A.sinks || hi_p - n0 < A.window); };
+  // does every query of the wave see all keys of tile t?
+  auto masked = [&](int t) {
+    const int n0 = first_of(t);
+    return !(n0 + TK - 1 <= w_lo && (n0 + TK <= A.sinks || w_hi - max(n0, lo) < A.window));
+  };
 
   float m_run = -INFINITY, l_run = 0.f;
   f32x16 acc[DT];
@@ -145,11 +151,12 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
     return w;
   };
 
-  // which keys of the tile at n0 the lane's query sees, a bit each: those up to it, without those between the sinks and its window
-  auto seen_keys = [&](int n0) {
-    return first_keys(p + 1 - n0) & (first_keys(A.sinks - n0) | ~first_keys((int)max((int64_t)p - A.window + 1, (int64_t)0) - n0));
+  // which keys of tile t the lane's query sees, a bit each: the sinks, then those up to it, without those between the sinks and its window
+  auto seen_keys = [&](int t) {
+    const int n0 = first_of(t);
+    return first_keys(firsts - t * TK) |
+           (first_keys(p + 1 - n0) & (first_keys(A.sinks - n0) | ~first_keys((int)max((int64_t)p - A.window + 1, (int64_t)0) - n0)));
   };
-  auto masked = [&](int t) { return !whole(first_of(t), w_lo, w_hi); };        // (of the wave's queries)
   // S of one tile
   auto product = [&](const u32x4 *k, f32x16 (&S)[2]) {
     int k_at = k_lane;
@@ -164,8 +171,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
       }
   };
   // keys that the query does not see score -inf
-  auto hide = [&](int n0, f32x16 (&S)[2]) {
-    const uint64_t seen = seen_keys(n0) >> (4 * h);
+  auto hide = [&](int t, f32x16 (&S)[2]) {
+    const uint64_t seen = seen_keys(t) >> (4 * h);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       const int word = (int)(uint32_t)(seen >> (32 * kt));
@@ -219,14 +226,19 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
   // a tile that not every query sees whole, with a value that is no number, or infinite
   auto odd_values = [&](int t, const u32x4 *v) {
     if (!masked(t)) return false;
-    uint32_t any = 0;
+    float z[4] = {0.f, 0.f, 0.f, 0.f};            // sums of 0 times the values: 0, or no number
+    const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
 #pragma unroll
     for (int m = 0; m < TK * CH / 64; ++m) {
       const u32x4 w = *(lds_u32x4)((lds_ptr)v + 16 * lane + 1024 * m);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) any |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = w[e];
+        z[e] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), none, z[e], false);
+      }
     }
-    return __builtin_amdgcn_ballot_w64(any != 0) != 0;
+    const float all = (z[0] + z[1]) + (z[2] + z[3]);
+    return __builtin_amdgcn_ballot_w64(all != 0.f) != 0;       // (true for what is no number)
   };
 
   // ---- The next tile's scores are worked out while this one's weights are: matrix and vector instructions of one wave, which do not wait
@@ -240,7 +252,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
     load(1, kbase, lds_k1, false);
     load(0, vbase, lds_v0, true);
     product(lds_k0, S);
-    if (masked(0)) hide(first_of(0), S);
+    if (masked(0)) hide(0, S);
     raise(highest(S));
     auto step = [&](int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
       arrived();
@@ -263,7 +275,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
       }
       later |= odd;
       if (t + 1 < tiles) {
-        if (masked(t + 1)) hide(first_of(t + 1), N);
+        if (masked(t + 1)) hide(t + 1, N);
         raise(highest(N));
       }
 #pragma unroll
@@ -287,9 +299,9 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
         if (!odd_values(t, lds_v0)) continue;
         u32x4 P[4];
         product(lds_k0, S);
-        hide(first_of(t), S);
+        hide(t, S);
         l_run += weights(S, P);
-        const uint64_t seen = seen_keys(first_of(t));
+        const uint64_t seen = seen_keys(t);
 #pragma unroll
         for (int s = 0; s < 4; ++s)
           for (int key = 0; key < 16; ++key) {
