@@ -164,7 +164,24 @@ sts_status plan_window(const sts_window_params *p, CachePlan &pl, bool &prompt) 
   }
   prompt = p->Tq > 16;
   memset(&pl, 0, sizeof(pl));
-  if (prompt) return STS_OK;
+  if (prompt) {
+    // Blocks of rows; where they leave compute units without work, several workgroups share a block's keys, four tiles each at least.
+    const int G = p->Hq / p->Hkv;
+    const int64_t blocks = ((int64_t)p->Tq * G + STS_WINDOW_ROWS - 1) / STS_WINDOW_ROWS * p->Hkv * p->B;
+    if ((int64_t)p->Tq * G > 0x7fffffffll - 65536 || blocks > 0x7fffffffll) return STS_EUNSUPPORTED;
+    const int64_t span = (int64_t)p->sinks + p->window + STS_WINDOW_ROWS / G + 1, keys = span < p->N ? span : p->N;
+    const int64_t tiles = (keys + STS_WINDOW_KEYS - 1) / STS_WINDOW_KEYS;
+    int64_t S = blocks > 0 ? 2 * sts_cu_count() / blocks : 1;
+    if (S > tiles / 4) S = tiles / 4;
+    if (S > 64) S = 64;
+    if (S < 1) S = 1;
+    pl.num_splits = (int)S;
+    if (S > 1) {
+      pl.part_o_bytes = align256((size_t)(blocks * S) * STS_WINDOW_ROWS * p->d * sizeof(float));
+      pl.part_ml_bytes = align256((size_t)(blocks * S) * STS_WINDOW_ROWS * 2 * sizeof(float));
+    }
+    return STS_OK;
+  }
   // no more tiles than the cache has, than the sinks and the window span (one more where the window begins inside a tile)
   const int64_t all = ((int64_t)p->N + STS_TILE_KEYS - 1) / STS_TILE_KEYS;
   const int64_t some = ((int64_t)p->sinks + STS_TILE_KEYS - 1) / STS_TILE_KEYS + ((int64_t)p->window + p->Tq + STS_TILE_KEYS - 1) / STS_TILE_KEYS + 1;
@@ -275,7 +292,15 @@ sts_status sts_window_attn(const sts_window_params *p, void *stream) {
     w.out = p->out;
     w.lse_out = p->lse_out;
     w.out_dtype = p->out_dtype;
-    return sts_run_kernel(STS_K_WINDOW, s, [&] { return launch_window_prompt(w, p->d, s); }) == hipSuccess ? STS_OK : STS_EHIP;
+    w.num_splits = pl.num_splits;
+    if (pl.num_splits > 1) {
+      if (!p->workspace || p->workspace_bytes < pl.part_o_bytes + pl.part_ml_bytes || !aligned(p->workspace, 256)) return STS_EWORKSPACE;
+      w.part_o = static_cast<float *>(p->workspace);
+      w.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(p->workspace) + pl.part_o_bytes);
+    }
+    hipError_t rc = sts_run_kernel(STS_K_WINDOW, s, [&] { return launch_window_prompt(w, p->d, s); });
+    if (rc == hipSuccess && pl.num_splits > 1) rc = sts_run_kernel(STS_K_ATTN_COMBINE, s, [&] { return launch_window_combine(w, p->d, s); });
+    return rc == hipSuccess ? STS_OK : STS_EHIP;
   }
   CacheAttnArgs c;
   memset(&c, 0, sizeof(c));

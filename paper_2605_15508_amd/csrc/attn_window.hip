@@ -15,7 +15,8 @@
 
 namespace {
 
-constexpr int WAVES = 4, ROWS = 32 * WAVES, TK = 64;
+constexpr int WAVES = 4, ROWS = STS_WINDOW_ROWS, TK = STS_WINDOW_KEYS;
+static_assert(ROWS == 32 * WAVES && TK == 64, "");
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -47,7 +48,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
   const int nb = (int)(((int64_t)A.Tq * A.G + ROWS - 1) / ROWS);
   const int total = gridDim.x, x = blockIdx.x % STS_XCDS;
   const int j = x * (total / STS_XCDS) + min(x, total % STS_XCDS) + blockIdx.x / STS_XCDS;
-  const int blk = nb - 1 - j % nb, g = j / nb % A.Hkv, bt = j / nb / A.Hkv;
+  const int split = j % A.num_splits, unit = j / A.num_splits;
+  const int blk = nb - 1 - unit % nb, g = unit / nb % A.Hkv, bt = unit / nb / A.Hkv;
 
   const int L = A.seq_lens ? min(max(A.seq_lens[bt], 0), A.N) : A.N;
   const int p_first = L - A.Tq;                                   // position of query 0
@@ -66,7 +68,9 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
   const int end = max(min(b_hi + 1, L), 0);
   const int lo = (int)min(max((int64_t)b_lo - A.window + 1, (int64_t)0), (int64_t)end);
   const int firsts = min(A.sinks, lo), skipped = lo - firsts;
-  const int places = end - skipped, tiles = (places + TK - 1) / TK;
+  const int places = end - skipped, all_tiles = (places + TK - 1) / TK;
+  // (few blocks: several workgroups to each, with a part of its tiles)
+  const int per_split = (all_tiles + A.num_splits - 1) / A.num_splits, begin = split * per_split, tiles = min(begin + per_split, all_tiles);
   // the key at a tile's first place, if that is none of the sinks
   auto first_of = [&](int t) { return t * TK + skipped; };
 
@@ -245,14 +249,14 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
   // for each other. K is a tile ahead of V.
   auto arrived = [] { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); };
   bool later = false;              // tiles left for the end: see below
-  if (tiles > 0) {
+  if (begin < tiles) {
     f32x16 S[2];
-    load(0, kbase, lds_k0, false);
+    load(begin, kbase, lds_k0, false);
     arrived();
-    load(1, kbase, lds_k1, false);
-    load(0, vbase, lds_v0, true);
+    load(begin + 1, kbase, lds_k1, false);
+    load(begin, vbase, lds_v0, true);
     product(lds_k0, S);
-    if (masked(0)) hide(0, S);
+    if (masked(begin)) hide(begin, S);
     raise(highest(S));
     auto step = [&](int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
       arrived();
@@ -281,7 +285,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) S[kt] = N[kt];
     };
-    for (int t = 0;; t += 2) {
+    for (int t = begin;; t += 2) {
       step(t, lds_k1, lds_k0, lds_v0, lds_v1);
       if (t + 1 >= tiles) break;
       step(t + 1, lds_k0, lds_k1, lds_v1, lds_v0);
@@ -291,7 +295,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
     // What is infinite or no number must not reach queries that do not see it, and 0 times it is not 0: such tiles come last, key by key, and
     // a key's row is taken in only where it is seen.
     if (__syncthreads_or(later)) {
-      for (int t = 0; t < tiles; ++t) {
+      for (int t = begin; t < tiles; ++t) {
         arrived();
         load(t, kbase, lds_k0, false);
         load(t, vbase, lds_v0, true);
@@ -333,6 +337,17 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
     const uint32_t q0 = q[0], q1 = q[1];
     l_run = __builtin_bit_cast(float, q0) + __builtin_bit_cast(float, q1);
   }
+  if (A.num_splits > 1) {            // a partial: the sums as they are, and what they are relative to
+    const size_t part = (size_t)unit * A.num_splits + split, row = part * ROWS + wave * 32 + col;
+    float *o = A.part_o + row * D + 4 * h;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4 *>(o + 32 * dt + 8 * e) = f32x4{acc[dt][4 * e], acc[dt][4 * e + 1], acc[dt][4 * e + 2], acc[dt][4 * e + 3]};
+    if (h == 0) *reinterpret_cast<f32x2 *>(A.part_ml + row * 2) = f32x2{m_run, l_run};
+    return;
+  }
   if (!ok) return;
   const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
   const size_t at = (((size_t)bt * A.Tq + qi) * A.Hq + head) * D + 4 * h;
@@ -353,12 +368,57 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
     A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + qi] = l_run == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_run)) * 0.69314718055994530942f;
 }
 
+// The parts of a block's rows put together, in order: D / 4 threads a row, four channels each.
+template <int D>
+__global__ void __launch_bounds__(256) window_combine_kernel(const WindowArgs A) {
+  constexpr int LANES = D / 4, AT_ONCE = 4;
+  const int nb = (int)(((int64_t)A.Tq * A.G + ROWS - 1) / ROWS);
+  const int64_t row_id = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;        // unit * ROWS + row of the block
+  const int64_t unit = row_id / ROWS;
+  const int row = (int)(row_id - unit * ROWS), chan = 4 * (threadIdx.x % LANES);
+  const int blk = nb - 1 - (int)(unit % nb), g = (int)(unit / nb % A.Hkv), bt = (int)(unit / nb / A.Hkv);
+  const int64_t r = (int64_t)blk * ROWS + row;
+  if (bt >= A.B || r >= (int64_t)A.Tq * A.G) return;
+  const int S = A.num_splits;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < S; s0 += AT_ONCE) {
+    f32x2 ml[AT_ONCE];
+    f32x4 x[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const size_t at = ((size_t)unit * S + min(s0 + j, S - 1)) * ROWS + row;
+      ml[j] = *reinterpret_cast<const f32x2 *>(A.part_ml + at * 2);
+      x[j] = *reinterpret_cast<const f32x4 *>(A.part_o + at * D + chan);
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      if (s0 + j >= S || ml[j][0] == -INFINITY) continue;
+      const float m_new = fmaxf(m, ml[j][0]);
+      const float fo = __builtin_amdgcn_exp2f(m - m_new), fn = __builtin_amdgcn_exp2f(ml[j][0] - m_new);
+      l = l * fo + ml[j][1] * fn;
+      o = o * fo + x[j] * fn;
+      m = m_new;
+    }
+  }
+  const int qi = (int)(r / A.G), head = g * A.G + (int)(r - (int64_t)qi * A.G);
+  o *= l == 0.f ? 0.f : 1.f / l;
+  const size_t at = (((size_t)bt * A.Tq + qi) * A.Hq + head) * D + chan;
+  if (A.out_dtype == STS_F32) {
+    *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at) = o;
+  } else {
+    const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[0], o[1]}), bf16x2)),
+                     __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[2], o[3]}), bf16x2))};
+    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at) = w;
+  }
+  if (A.lse_out && chan == 0)
+    A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+}
+
 }  // namespace
 
 hipError_t launch_window_prompt(const WindowArgs &a, int d, hipStream_t s) {
-  const int64_t blocks = ((int64_t)a.Tq * a.G + ROWS - 1) / ROWS * a.Hkv * a.B;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks), block(64 * WAVES);
+  const dim3 grid((unsigned)(((int64_t)a.Tq * a.G + ROWS - 1) / ROWS * a.Hkv * a.B * a.num_splits)), block(64 * WAVES);
   if (d == 128) {
     if (a.block_table) STS_LAUNCH((window_prompt_kernel<128, true>), grid, block, 0, s, a);
     else STS_LAUNCH((window_prompt_kernel<128, false>), grid, block, 0, s, a);
@@ -366,5 +426,13 @@ hipError_t launch_window_prompt(const WindowArgs &a, int d, hipStream_t s) {
     if (a.block_table) STS_LAUNCH((window_prompt_kernel<64, true>), grid, block, 0, s, a);
     else STS_LAUNCH((window_prompt_kernel<64, false>), grid, block, 0, s, a);
   }
+  return sts_take_launch_status();
+}
+
+hipError_t launch_window_combine(const WindowArgs &a, int d, hipStream_t s) {
+  const int64_t rows = ((int64_t)a.Tq * a.G + ROWS - 1) / ROWS * ROWS * a.Hkv * a.B;
+  const dim3 grid((unsigned)(rows / (256 / (d / 4)))), block(256);
+  if (d == 128) STS_LAUNCH(window_combine_kernel<128>, grid, block, 0, s, a);
+  else STS_LAUNCH(window_combine_kernel<64>, grid, block, 0, s, a);
   return sts_take_launch_status();
 }

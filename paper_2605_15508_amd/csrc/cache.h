@@ -33,13 +33,17 @@ struct WindowArgs {
   int32_t B, Tq, Hq, Hkv, G, N, window, sinks;
   int32_t page_shift, table_stride, num_pages;
   float scale, scale_log2;
+  int32_t num_splits;                // workgroups per block of rows, each with a part of its keys
+  float *part_o, *part_ml;           // [units][num_splits][STS_WINDOW_ROWS][d], [..][2]
   void *out;
   float *lse_out;
   int32_t out_dtype;
 };
+constexpr int STS_WINDOW_ROWS = 128, STS_WINDOW_KEYS = 64;      // query rows of a block, keys of a tile
 
 hipError_t launch_packed_store(const PackedRowsArgs &a, hipStream_t s);
 hipError_t launch_packed_load(const PackedRowsArgs &a, hipStream_t s);
 // far: rows at offsets of more than 32 bits, or pages
 hipError_t launch_cache_attn(const CacheAttnArgs &a, int d, int nq, bool four_bit, bool far, hipStream_t s);
 hipError_t launch_window_prompt(const WindowArgs &a, int d, hipStream_t s);
+hipError_t launch_window_combine(const WindowArgs &a, int d, hipStream_t s);
