@@ -185,50 +185,52 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
   u32x4 Q[QLDS ? 1 : NQ][QLDS ? 1 : QR];
   uint32_t qs[FOUR ? NQ : 1];
   int q_tq[NQ];
+  auto take_q = [&] {
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    const int r = nq * 16 + b;
-    const bool ok = r < rows_valid;
-    const int hsel = ok ? r / A.Tq : 0;
-    q_tq[nq] = ok ? r - hsel * A.Tq : 0;
-    const uint16_t *qp = A.q + (((size_t)bt * A.Tq + q_tq[nq]) * A.Hq + g * A.G + nth_member(mask, hsel)) * D;
-    auto put = [&](int i, u32x4 w) {
-      if (!QLDS) Q[QLDS ? 0 : nq][QLDS ? 0 : i] = w;
-      else lds_q[(nq * QR + i) * 64 + lane] = w;
-    };
-    if (QLDS && wave != nq % W) continue;        // (a query tile by each wave, for all of them)
-    auto get = [&](int chan) { return (*reinterpret_cast<const u32x4 *>(qp + chan) & (ok ? q_keep : 0u)) ^ q_flip; };
-    if constexpr (FOUR) {
-      // Channels 16 a .. of the first 64 and of the rest: the first and the second half of the operand. A group of 32 channels is in
-      // two neighbouring lane groups, and its scale goes to the lane group that has K's share of it.
-      uint32_t s[D / 64];
+    for (int nq = 0; nq < NQ; ++nq) {
+      const int r = nq * 16 + b;
+      const bool ok = r < rows_valid;
+      const int hsel = ok ? r / A.Tq : 0;
+      q_tq[nq] = ok ? r - hsel * A.Tq : 0;
+      const uint16_t *qp = A.q + (((size_t)bt * A.Tq + q_tq[nq]) * A.Hq + g * A.G + nth_member(mask, hsel)) * D;
+      auto put = [&](int i, u32x4 w) {
+        if (!QLDS) Q[QLDS ? 0 : nq][QLDS ? 0 : i] = w;
+        else lds_q[(nq * QR + i) * 64 + lane] = w;
+      };
+      if (QLDS && wave != nq % W) continue;        // (a query tile by each wave, for all of them)
+      auto get = [&](int chan) { return (*reinterpret_cast<const u32x4 *>(qp + chan) & (ok ? q_keep : 0u)) ^ q_flip; };
+      if constexpr (FOUR) {
+        // Channels 16 a .. of the first 64 and of the rest: the first and the second half of the operand. A group of 32 channels is in
+        // two neighbouring lane groups, and its scale goes to the lane group that has K's share of it.
+        uint32_t s[D / 64];
 #pragma unroll
-      for (int j = 0; j < D / 64; ++j) {
-        const u32x4 w0 = get(64 * j + 16 * a), w1 = get(64 * j + 16 * a + 8);
-        const uint32_t w[8] = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
-        uint32_t m = largest(w);
-        m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
-        s[j] = q_scale(m);
-        u32x4 hi, lo;
-        q_halves(w, s[j], hi, lo);
-        put(D == 128 ? j : 0, hi);
-        put(D == 128 ? 2 + j : 1, lo);
+        for (int j = 0; j < D / 64; ++j) {
+          const u32x4 w0 = get(64 * j + 16 * a), w1 = get(64 * j + 16 * a + 8);
+          const uint32_t w[8] = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
+          uint32_t m = largest(w);
+          m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+          s[j] = q_scale(m);
+          u32x4 hi, lo;
+          q_halves(w, s[j], hi, lo);
+          put(D == 128 ? j : 0, hi);
+          put(D == 128 ? 2 + j : 1, lo);
+        }
+        const uint32_t s0 = s[0], s1 = s[D / 64 - 1];
+        const uint32_t o0 = (uint32_t)__shfl_xor((int)s0, 48, 64), o1 = (uint32_t)__shfl_xor((int)s1, 48, 64);
+        qs[nq] = a == 0 ? s0 : a == 3 ? s1 : a == 1 ? o0 : o1;
+        if (QLDS) lds_qs[QLDS ? nq : 0][lane] = qs[nq];
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) put(kk, get(8 * (a + 4 * kk)));
       }
-      const uint32_t s0 = s[0], s1 = s[D / 64 - 1];
-      const uint32_t o0 = (uint32_t)__shfl_xor((int)s0, 48, 64), o1 = (uint32_t)__shfl_xor((int)s1, 48, 64);
-      qs[nq] = a == 0 ? s0 : a == 3 ? s1 : a == 1 ? o0 : o1;
-      if (QLDS) lds_qs[QLDS ? nq : 0][lane] = qs[nq];
-    } else {
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) put(kk, get(8 * (a + 4 * kk)));
     }
-  }
-  if (QLDS) {
-    __syncthreads();
-    if (FOUR)
+    if (QLDS) {
+      __syncthreads();
+      if (FOUR)
 #pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) qs[FOUR ? nq : 0] = lds_qs[FOUR ? nq : 0][lane];
-  }
+        for (int nq = 0; nq < NQ; ++nq) qs[FOUR ? nq : 0] = lds_qs[FOUR ? nq : 0][lane];
+    }
+  };
 
   float m_run[NQ], l_run[NQ];
   f32x4 acc[NQ][NT];
@@ -261,7 +263,11 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
 #pragma unroll
     for (int j = 0; j < KL; ++j) k[j] = *reinterpret_cast<const k_t *>(base + (off + (off_t)(64 * j)));
   };
-  auto load_v = [&](const unsigned char *base, off_t off) { return *reinterpret_cast<const v_t *>(base + off); };
+  // (V of a bf16 cache past the caches, where K's halves of a line meet: 16 sequences, window 4096, 55.4 us without, 49.3 so)
+  auto load_v = [&](const unsigned char *base, off_t off) {
+    const v_t *src = reinterpret_cast<const v_t *>(base + off);
+    return FOUR ? *src : __builtin_nontemporal_load(src);
+  };
 
   // contiguous: offsets of the lane's rows in a tile, which a tile's end and gap move to rows that are attended to (their weight is 0,
   // but 0 times what lies there may be NaN)
@@ -348,208 +354,181 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
   };
 
   // ---- one tile
-  auto consume = [&](const Tile &R, int t, uint32_t tile_mask) {
+  // S^T = K Q^T
+  auto scores = [&](const Tile &R, f32x4 (&St)[NQ][2]) {
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     auto q_at = [&](int nq, int i) { return QLDS ? lds_q[(nq * QR + i) * 64 + lane] : Q[QLDS ? 0 : nq][QLDS ? 0 : i]; };
+    if constexpr (FOUR) {
+#pragma unroll
+      for (int j = 0; j < NQ; ++j) {
+        const u32x4 q0 = q_at(j, 0), q1 = q_at(j, 1);
+        const uint32_t s = qs[FOUR ? j : 0];
+        f32x4 x[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[h] = scaled_product(R.k[h][0], ks[h], q0, q1, s, zero);
+        if constexpr (D == 128) {
+          const u32x4 l0 = q_at(j, 2), l1 = q_at(j, 3);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) St[j][h] = scaled_product(R.k[h][0], ks[h], l0, l1, s, x[h]);
+          // The instruction takes eight passes: a result in registers that are partly an operand's would be wrong, and the compiler
+          // sees to that for larger results only. So all operands are in use until the results are there.
+          asm volatile("" ::"v"(St[j][0]), "v"(St[j][1]), "v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(l0), "v"(l1), "v"(R.k[0][0]), "v"(R.k[1][0]));
+        } else {
+          St[j][0] = x[0];
+          St[j][1] = x[1];
+          asm volatile("" ::"v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(R.k[0][0]), "v"(R.k[1][0]));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+          const u32x4 Qb = q_at(j, kk);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const u32x4 Ka = R.k[h][FOUR ? 0 : kk];
+            St[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, Ka), __builtin_bit_cast(bf16x8, Qb), kk ? St[j][h] : zero, 0, 0, 0);
+          }
+        }
+    }
+  };
+  // a window: which of the keys from n0 on query row q_tq[nq] sees: those up to it, without those between the sinks and its window
+  auto seen_keys = [&](int n0, int nq) {
+    const int p = p0 + q_tq[nq];
+    return first_keys(min(p + 1, c) - n0) & (first_keys(C.sinks - n0) | ~first_keys((int)max((int64_t)p - C.window + 1, (int64_t)0) - n0));
+  };
+  // ... and whether some row does not see some of them
+  auto partly_seen = [&](int n0) {
+    return !(n0 + TK <= c && n0 + TK - 1 <= p0 && (n0 + TK <= C.sinks || p0 + A.Tq - 1 - n0 < C.window));
+  };
+  // keys that a row does not see score -inf
+  auto hide = [&](int n0, uint32_t tile_mask, f32x4 (&St)[NQ][2]) {
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      const int mine = (int)((WIN ? seen_keys(n0, j) : tile_mask) >> a);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(mine, 4 * i, 1);
+        const float x = St[j][i >> 2][i & 3];
+        St[j][i >> 2][i & 3] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) & keep) | (0xff800000u & ~keep));
+      }
+    }
+  };
+  // the weights exp(S - m) as the B operand of the second product: bf16 (half a step, 2^-9 of each); their sums in fp32
+  auto weights = [&](const f32x4 (&St)[NQ][2], u32x4 (&P)[NQ]) {
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      const float m_ref = WIN && m_run[j] == -INFINITY ? 0.f : m_run[j];
+      float p[8], sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(St[j][i >> 2][i & 3], sl2, -m_ref));
+        sum += p[i];
+      }
+      l_run[j] += sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) P[j][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p[2 * i], p[2 * i + 1]}), bf16x2));
+    }
+  };
+  // pair j of channels of the lane's 8 keys, and of those the keys of channel 2 j (hi: 2 j + 1) as pairs
+  auto v_pairs = [&](const Tile &R, int j, uint32_t (&w)[8]) {
+#pragma unroll
+    for (int m = 0; m < 8; ++m) {
+      if constexpr (FOUR) w[m] = pair_of(R.v[m], __builtin_bit_cast(float, vs[m]), j);
+      else w[m] = R.v[m][j];
+    }
+  };
+  auto v_keys = [&](const uint32_t (&w)[8], bool hi) {
+    u32x4 x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], hi ? 0x07060302u : 0x05040100u);
+    return x;
+  };
+  // values of the tile that are no numbers, or infinite: 0 times them is not 0
+  auto odd_values = [&](const Tile &R) {
+    float z = 0.f;
+    if constexpr (!FOUR) {
+      const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
+#pragma unroll
+      for (int m = 0; m < 8; ++m)
+#pragma unroll
+        for (int j = 0; j < NT / 2; ++j) {
+          const uint32_t x = R.v[m][j];
+          z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), none, z, false);
+        }
+    }
+    return __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
+  };
+  bool later = false;              // tiles left for the end: see below
+  auto consume = [&](const Tile &R, int t, uint32_t tile_mask) {
     const int n0 = first_of(t);
-    bool partly = false;                 // some row does not see some key
-    // which of the tile's keys query row q_tq[nq] sees: those up to it, without those between the sinks and its window
-    auto seen_keys = [&](int nq) {
-      const int p = p0 + q_tq[nq];
-      return first_keys(min(p + 1, c) - n0) & (first_keys(C.sinks - n0) | ~first_keys((int)max((int64_t)p - C.window + 1, (int64_t)0) - n0));
-    };
-    if constexpr (WIN) {
-      const int pl = p0 + A.Tq - 1;
-      partly = !(n0 + TK <= c && n0 + TK - 1 <= p0 && (n0 + TK <= C.sinks || pl - n0 < C.window));
+    f32x4 St[NQ][2];
+    scores(R, St);
+    // (V's conversions do not move up here, where their results would take the registers of the tiles on the way)
+    if (FOUR && NQ >= 2) __builtin_amdgcn_sched_barrier(0);
+    bool odd = false;
+    if (WIN ? partly_seen(n0) : tile_mask != 0xffffffffu) {
+      hide(n0, tile_mask, St);
+      if (WIN) odd = odd_values(R);
     }
-    u32x4 P[NQ];
-    {
-      f32x4 St[NQ][2];
-      if constexpr (FOUR) {
+    // Most tiles of a long list raise no row's maximum: it is put together from the four lanes of a row only where one of them does.
+    float mine[NQ];
+    bool grown = false;
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-          const u32x4 q0 = q_at(j, 0), q1 = q_at(j, 1);
-          const uint32_t s = qs[FOUR ? j : 0];
-          f32x4 x[2];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) x[h] = scaled_product(R.k[h][0], ks[h], q0, q1, s, zero);
-          if constexpr (D == 128) {
-            const u32x4 l0 = q_at(j, 2), l1 = q_at(j, 3);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) St[j][h] = scaled_product(R.k[h][0], ks[h], l0, l1, s, x[h]);
-            // The instruction takes eight passes: a result in registers that are partly an operand's would be wrong, and the compiler
-            // sees to that for larger results only. So all operands are in use until the results are there.
-            asm volatile("" ::"v"(St[j][0]), "v"(St[j][1]), "v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(l0), "v"(l1), "v"(R.k[0][0]), "v"(R.k[1][0]));
-          } else {
-            St[j][0] = x[0];
-            St[j][1] = x[1];
-            asm volatile("" ::"v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(R.k[0][0]), "v"(R.k[1][0]));
-          }
-        }
-      } else {
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-          for (int j = 0; j < NQ; ++j) {
-            const u32x4 Qb = q_at(j, kk);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const u32x4 Ka = R.k[h][FOUR ? 0 : kk];
-              St[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, Ka), __builtin_bit_cast(bf16x8, Qb), kk ? St[j][h] : zero, 0, 0, 0);
-            }
-          }
-      }
-      // (V's conversions do not move up here, where their results would take the registers of the tiles on the way)
-      if (FOUR && NQ >= 2) __builtin_amdgcn_sched_barrier(0);
-      // keys that a row does not see score -inf
-      if (WIN ? partly : tile_mask != 0xffffffffu) {
-#pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-          const int mine = (int)((WIN ? seen_keys(j) : tile_mask) >> a);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(mine, 4 * i, 1);
-            const float x = St[j][i >> 2][i & 3];
-            St[j][i >> 2][i & 3] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) & keep) | (0xff800000u & ~keep));
-          }
-        }
-      }
-      // Most tiles of a long list raise no row's maximum: it is put together from the four lanes of a row only where one of them does.
-      float mine[NQ];
-      bool grown = false;
+    for (int j = 0; j < NQ; ++j) {
+      const f32x4 s0 = St[j][0], s1 = St[j][1];
+      mine[j] = sl2 * top(top(top(s0[0], s0[1]), top(s0[2], s0[3])), top(top(s1[0], s1[1]), top(s1[2], s1[3])));
+      grown |= mine[j] > m_run[j];
+    }
+    if (__builtin_amdgcn_ballot_w64(grown) != 0) {
 #pragma unroll
       for (int j = 0; j < NQ; ++j) {
-        const f32x4 s0 = St[j][0], s1 = St[j][1];
-        mine[j] = sl2 * top(top(top(s0[0], s0[1]), top(s0[2], s0[3])), top(top(s1[0], s1[1]), top(s1[2], s1[3])));
-        grown |= mine[j] > m_run[j];
-      }
-      if (__builtin_amdgcn_ballot_w64(grown) != 0) {
+        const float m_new = larger(m_run[j], max_over_groups(mine[j]));
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[j] - m_new);
+        l_run[j] *= alpha;
+        m_run[j] = m_new;
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-          const int nq = j;
-          const float m_new = larger(m_run[nq], max_over_groups(mine[j]));
-          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[nq] - m_new);
-          l_run[nq] *= alpha;
-          m_run[nq] = m_new;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) acc[nq][nt] *= alpha;
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < NQ; ++j) {
-        const int nq = j;
-        const float m_ref = WIN && m_run[nq] == -INFINITY ? 0.f : m_run[nq];
-        float p[8], sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(St[j][i >> 2][i & 3], sl2, -m_ref));
-          sum += p[i];
-        }
-        l_run[nq] += sum;
-        // the weights enter the second product as bf16 (half a step, 2^-9 of each), the sum above in fp32
-#pragma unroll
-        for (int i = 0; i < 4; ++i) P[nq][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p[2 * i], p[2 * i + 1]}), bf16x2));
+        for (int nt = 0; nt < NT; ++nt) acc[j][nt] *= alpha;
       }
     }
-    // pair j of channels of the lane's 8 keys, and of those the keys of channel 2 j (hi: 2 j + 1) as pairs
-    auto v_pairs = [&](int j, uint32_t (&w)[8]) {
+    later |= odd;
+    if (!odd) {
+      u32x4 P[NQ];
+      weights(St, P);
 #pragma unroll
-      for (int m = 0; m < 8; ++m) {
-        if constexpr (FOUR) w[m] = pair_of(R.v[m], __builtin_bit_cast(float, vs[m]), j);
-        else w[m] = R.v[m][j];
-      }
-    };
-    auto v_keys = [&](const uint32_t (&w)[8], bool hi) {
-      u32x4 x;
+      for (int j = 0; j < NT / 2; ++j) {
+        uint32_t w[8];
+        v_pairs(R, j, w);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], hi ? 0x07060302u : 0x05040100u);
-      return x;
-    };
-    if constexpr (WIN) {
-      if (partly) {
-        // A value that is no number, or infinite, must not reach the rows that do not see it, and 0 times it is not 0: then key by key,
-        // and only where it is seen.
-        uint32_t odd = 0;
+        for (int hi = 0; hi < 2; ++hi) {
+          const bf16x8 Va = __builtin_bit_cast(bf16x8, v_keys(w, hi));
 #pragma unroll
-        for (int m = 0; m < 8; ++m)
-#pragma unroll
-          for (int j = 0; j < NT / 2; ++j) odd |= ((R.v[m][j] & 0x7f80u) == 0x7f80u) | ((R.v[m][j] & 0x7f800000u) == 0x7f800000u);
-        if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
-          for (int key = 0; key < TK; ++key) {
-#pragma unroll
-            for (int nq = 0; nq < NQ; ++nq) {
-              const bool see = (seen_keys(nq) >> key) & 1u;
-              u32x4 own;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) own[i] = (a + 8 * i == key ? 0xffffu : 0u) | (a + 8 * i + 4 == key ? 0xffff0000u : 0u);
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                uint32_t w[8];
-                v_pairs(nt >> 1, w);
-                const u32x4 Vk = v_keys(w, nt & 1) & own;
-                const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, Vk), __builtin_bit_cast(bf16x8, P[nq] & own), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[nq][nt][r] += see ? x[r] : 0.f;
-              }
-            }
-          }
-          return;
+          for (int nq = 0; nq < NQ; ++nq)
+            acc[nq][2 * j + hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Va, __builtin_bit_cast(bf16x8, P[nq]), acc[nq][2 * j + hi], 0, 0, 0);
         }
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < NT / 2; ++j) {
-      uint32_t w[8];
-      v_pairs(j, w);
-#pragma unroll
-      for (int hi = 0; hi < 2; ++hi) {
-        const bf16x8 Va = __builtin_bit_cast(bf16x8, v_keys(w, hi));
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq)
-          acc[nq][2 * j + hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Va, __builtin_bit_cast(bf16x8, P[nq]), acc[nq][2 * j + hi], 0, 0, 0);
       }
     }
   };
 
   // ---- main loop: PF tiles on the way, each asked for again when it has been used. One exit, and code of its own for what is left over, so
-  // that the loop's head knows which loads are in flight.
+  // that the loop's head knows which loads are in flight. Q comes while the first tiles are on their way.
+  // GATHER: a list entry is fetched 3 PF tiles ahead of its use, its page looked up 2 PF ahead, the offset placed PF + 1 ahead.
+  Tile R[PF];
+  uint32_t seen[PF], next_seen = 0;
+  int entry[PF], blk[PF], page[PF];
   if (nv > 0) {
-    Tile R[PF];
-    uint32_t seen[PF];
     if constexpr (!GATHER) {
 #pragma unroll
       for (int j = 0; j < PF; ++j) issue_near(tile_of(j), R[j]);
-      put_scales(R[0].sc, 0);
-      get_scales(0);
-      auto step = [&](int v, int j, bool more) {
-        const int t = tile_of(v), left = c - first_of(t);
-        put_scales(R[(j + 1) % PF].sc, (v + 1) & 1);
-        consume(R[j], t, left >= TK ? 0xffffffffu : (1u << left) - 1u);
-        get_scales((v + 1) & 1);
-        if (more) issue_near(tile_of(v + PF), R[j]);
-        __builtin_amdgcn_sched_barrier(0);
-      };
-      int v = 0;
-      for (; v + PF <= nv; v += PF) {
-#pragma unroll
-        for (int j = 0; j < PF; ++j) step(v + j, j, true);
-      }
-#pragma unroll
-      for (int j = 0; j < PF - 1; ++j)
-        if (v + j < nv) step(v + j, j, false);
     } else {
-      // tile j of the ring: a list entry fetched 3 PF tiles ahead of its use, its page looked up 2 PF ahead, the offset placed PF + 1
-      // ahead
-      int entry[PF], blk[PF], page[PF];
-      uint32_t next_seen = 0;
-      int e0[PF + 1];
+      int e0[PF + 1], pg0[PF + 1];
 #pragma unroll
       for (int j = 0; j <= PF; ++j) e0[j] = fetch(tile_of(j));
 #pragma unroll
       for (int j = 0; j < PF; ++j) blk[(j + 1) % PF] = fetch(tile_of(PF + 1 + j));
 #pragma unroll
       for (int j = 0; j < PF; ++j) entry[(j + 1) % PF] = fetch(tile_of(2 * PF + 1 + j));
-      int pg0[PF + 1];
 #pragma unroll
       for (int j = 0; j <= PF; ++j) e0[j] = block_of(e0[j]), pg0[j] = look_up(e0[j]);
 #pragma unroll
@@ -562,14 +541,22 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
           seen[j] = next_seen;
         }
       }
-      put_scales(R[0].sc, 0);
-      get_scales(0);
-      auto step = [&](int v, int j, bool more) {
-        const int t = tile_of(v), n = (j + 1) % PF;
-        put_scales(R[n].sc, (v + 1) & 1);
-        consume(R[j], t, seen[j]);
-        get_scales((v + 1) & 1);
-        if (more) {
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  take_q();
+  if (nv > 0) {
+    put_scales(R[0].sc, 0);
+    get_scales(0);
+    auto step = [&](int v, int j, bool more) {
+      const int t = tile_of(v), n = (j + 1) % PF, left = c - first_of(t);
+      put_scales(R[n].sc, (v + 1) & 1);
+      consume(R[j], t, GATHER ? seen[j] : left >= TK ? 0xffffffffu : (1u << left) - 1u);
+      get_scales((v + 1) & 1);
+      if (more) {
+        if constexpr (!GATHER) {
+          issue_near(tile_of(v + PF), R[j]);
+        } else {
           issue_far((v + PF) & 1, R[j]);
           seen[j] = next_seen;
           __builtin_amdgcn_sched_barrier(0);
@@ -578,16 +565,58 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
           page[n] = look_up(blk[n]);
           entry[n] = fetch(tile_of(v + 3 * PF + 1));
         }
-        __builtin_amdgcn_sched_barrier(0);
-      };
-      int v = 0;
-      for (; v + PF <= nv; v += PF) {
-#pragma unroll
-        for (int j = 0; j < PF; ++j) step(v + j, j, true);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int v = 0;
+    for (; v + PF <= nv; v += PF) {
 #pragma unroll
-      for (int j = 0; j < PF - 1; ++j)
-        if (v + j < nv) step(v + j, j, false);
+      for (int j = 0; j < PF; ++j) step(v + j, j, true);
+    }
+#pragma unroll
+    for (int j = 0; j < PF - 1; ++j)
+      if (v + j < nv) step(v + j, j, false);
+    if constexpr (WIN) {
+      // What is infinite or no number must not reach the rows that do not see it: such tiles come last, key by key, and a key's
+      // row of V is taken in only where it is seen.
+      if (later) {
+        for (v = 0; v < nv; ++v) {
+          const int t = tile_of(v), n0 = first_of(t);
+          if (!partly_seen(n0)) continue;
+          if constexpr (GATHER) {
+            const int e = block_of(fetch(t));
+            place(e, look_up(e), t, 0, next_seen);
+            issue_far(0, R[0]);
+          } else {
+            issue_near(t, R[0]);
+          }
+          if (!odd_values(R[0])) continue;
+          f32x4 St[NQ][2];
+          u32x4 P[NQ];
+          scores(R[0], St);
+          hide(n0, 0u, St);
+          weights(St, P);
+          for (int key = 0; key < TK; ++key) {
+            u32x4 own;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) own[i] = (a + 8 * i == key ? 0xffffu : 0u) | (a + 8 * i + 4 == key ? 0xffff0000u : 0u);
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+              const bool see = (seen_keys(n0, nq) >> key) & 1u;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                uint32_t w[8];
+                v_pairs(R[0], nt >> 1, w);
+                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v_keys(w, nt & 1) & own),
+                                                                        __builtin_bit_cast(bf16x8, P[nq] & own), zero, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[nq][nt][r] += see ? x[r] : 0.f;
+              }
+            }
+          }
+        }
+      }
     }
   }
 
