@@ -191,6 +191,7 @@ sts_status plan_window(const sts_window_params *p, CachePlan &pl, bool &prompt) 
 sts_status launch_short(CacheAttnArgs &c, const CachePlan &pl, int d, bool four_bit, bool far, int kind, void *ws, size_t ws_bytes, hipStream_t s) {
   if (!ws || ws_bytes < pl.part_o_bytes + pl.part_ml_bytes || !aligned(ws, 256)) return STS_EWORKSPACE;
   AttnArgs &a = c.a;
+  c.tq_inv = 65536 / a.Tq + 1;
   a.num_units = pl.num_units;
   a.num_splits = pl.num_splits;
   a.z_rounds = (a.B + STS_GRID_Z - 1) / STS_GRID_Z;

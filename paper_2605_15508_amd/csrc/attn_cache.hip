@@ -137,12 +137,19 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
   constexpr bool QLDS = NQ >= 2;
     __shared__ __attribute__((aligned(16))) float lds_o[W * 16 * OPITCH];
   __shared__ float lds_ml[W][NQ * 16][2];
-  __shared__ __attribute__((aligned(16))) u32x4 lds_q[QLDS ? NQ * QR * 64 : 1];
-  __shared__ uint32_t lds_qs[FOUR && QLDS ? NQ : 1][64];
+  __shared__ __attribute__((aligned(16))) u32x4 lds_q[NQ * QR * 64];
+  __shared__ uint32_t lds_qs[NQ][2][64];
   __shared__ __attribute__((aligned(16))) off_t lds_off[GATHER ? W : 1][2][TK];                // by (slot % 4) * 8 + slot / 4
   __shared__ __attribute__((aligned(16))) uint32_t lds_sc[FOUR ? W : 1][2][2][D / 32][TK];     // [tile parity][K, V][group], slots as above
 
   const AttnArgs &A = C.a;
+  // what the first loads need of the arguments, asked for together: waits for scalar loads cannot tell them apart
+  uint32_t unit = A.units.unit[blockIdx.y];
+  asm volatile("" ::"s"(unit), "s"(A.q), "s"(A.indices), "s"(A.counts), "s"(A.seq_lens), "s"(A.idx_stride_b), "s"(A.cnt_stride_b), "s"(A.Tq), "s"(A.Hq),
+               "s"(A.G), "s"(A.N), "s"(A.kmax), "s"(A.num_splits), "s"(A.z_rounds), "s"(A.page), "s"(A.page_shift), "s"(A.block_table), "s"(A.scale),
+               "s"(A.scale_log2), "s"(C.tq_inv));
+  if (FOUR) asm volatile("" ::"s"(C.codes), "s"(C.scales), "s"(C.code_b), "s"(C.code_h), "s"(C.code_n), "s"(C.scale_b), "s"(C.scale_h), "s"(C.scale_n));
+  else asm volatile("" ::"s"(A.k), "s"(A.v), "s"(A.stride_b), "s"(A.stride_h), "s"(A.stride_n), "s"(C.window), "s"(C.sinks), "s"(C.behind));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int a = lane >> 4, b = lane & 15;
   const int S = A.num_splits, U = A.num_units;
@@ -153,7 +160,6 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
     split %= S;
     if (bt >= A.B) return;
   }
-  const uint32_t unit = A.units.unit[u];
   const int g = unit & 0xff;
   const uint32_t mask = (unit >> 8) & 0xffff;
   const int nheads = (unit >> 24) & 0x1f;
@@ -183,53 +189,54 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
   const uint32_t q_keep = A.scale == 0.f ? 0u : 0xffffffffu, q_flip = A.scale < 0.f ? 0x80008000u : 0u;
   const float sl2 = A.scale == 0.f ? 1.f : fabsf(A.scale_log2);
   u32x4 Q[QLDS ? 1 : NQ][QLDS ? 1 : QR];
-  uint32_t qs[FOUR ? NQ : 1];
+  uint32_t qs[NQ];
   int q_tq[NQ];
+  auto row_of_lane = [&](int nq, bool &ok, int &hsel) {
+    const int r = nq * 16 + b;
+    ok = r < rows_valid;
+    hsel = ok ? (r * C.tq_inv) >> 16 : 0;              // r / Tq
+    q_tq[nq] = ok ? r - hsel * A.Tq : 0;
+  };
   auto take_q = [&] {
+    // The work is divided among the waves, which find the operands in LDS.
+    constexpr int PARTS = FOUR ? D / 64 : 1;
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
-      const int r = nq * 16 + b;
-      const bool ok = r < rows_valid;
-      const int hsel = ok ? r / A.Tq : 0;
-      q_tq[nq] = ok ? r - hsel * A.Tq : 0;
-      const uint16_t *qp = A.q + (((size_t)bt * A.Tq + q_tq[nq]) * A.Hq + g * A.G + nth_member(mask, hsel)) * D;
-      auto put = [&](int i, u32x4 w) {
-        if (!QLDS) Q[QLDS ? 0 : nq][QLDS ? 0 : i] = w;
-        else lds_q[(nq * QR + i) * 64 + lane] = w;
-      };
-      if (QLDS && wave != nq % W) continue;        // (a query tile by each wave, for all of them)
-      auto get = [&](int chan) { return (*reinterpret_cast<const u32x4 *>(qp + chan) & (ok ? q_keep : 0u)) ^ q_flip; };
-      if constexpr (FOUR) {
-        // Channels 16 a .. of the first 64 and of the rest: the first and the second half of the operand. A group of 32 channels is in
-        // two neighbouring lane groups, and its scale goes to the lane group that has K's share of it.
-        uint32_t s[D / 64];
+      bool ok;
+      int hsel;
+      row_of_lane(nq, ok, hsel);
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
+      for (int j = 0; j < PARTS; ++j) {
+        if (wave != (nq * PARTS + j) % W) continue;
+        const uint16_t *qp = A.q + (((size_t)bt * A.Tq + q_tq[nq]) * A.Hq + g * A.G + nth_member(mask, hsel)) * D;
+        auto get = [&](int chan) { return (*reinterpret_cast<const u32x4 *>(qp + chan) & (ok ? q_keep : 0u)) ^ q_flip; };
+        if constexpr (FOUR) {
+          // Channels 16 a .. of the first 64 (j = 0) or of the rest: the first or the second half of the operand. A group of 32 channels
+          // is in two neighbouring lane groups.
           const u32x4 w0 = get(64 * j + 16 * a), w1 = get(64 * j + 16 * a + 8);
           const uint32_t w[8] = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
           uint32_t m = largest(w);
           m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
-          s[j] = q_scale(m);
+          const uint32_t s = q_scale(m);
           u32x4 hi, lo;
-          q_halves(w, s[j], hi, lo);
-          put(D == 128 ? j : 0, hi);
-          put(D == 128 ? 2 + j : 1, lo);
-        }
-        const uint32_t s0 = s[0], s1 = s[D / 64 - 1];
-        const uint32_t o0 = (uint32_t)__shfl_xor((int)s0, 48, 64), o1 = (uint32_t)__shfl_xor((int)s1, 48, 64);
-        qs[nq] = a == 0 ? s0 : a == 3 ? s1 : a == 1 ? o0 : o1;
-        if (QLDS) lds_qs[QLDS ? nq : 0][lane] = qs[nq];
-      } else {
+          q_halves(w, s, hi, lo);
+          lds_q[(nq * QR + (D == 128 ? j : 0)) * 64 + lane] = hi;
+          lds_q[(nq * QR + (D == 128 ? 2 + j : 1)) * 64 + lane] = lo;
+          lds_qs[nq][j][lane] = s;
+        } else {
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) put(kk, get(8 * (a + 4 * kk)));
+          for (int kk = 0; kk < KK; ++kk) lds_q[(nq * QR + kk) * 64 + lane] = get(8 * (a + 4 * kk));
+        }
       }
     }
-    if (QLDS) {
-      __syncthreads();
-      if (FOUR)
+    __syncthreads();
+    // (the scale of a group goes to the lane group that has K's share of it)
+    if (FOUR)
 #pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) qs[FOUR ? nq : 0] = lds_qs[FOUR ? nq : 0][lane];
-    }
+      for (int nq = 0; nq < NQ; ++nq) qs[nq] = lds_qs[nq][D == 128 ? a >> 1 : 0][(a & 1) * 32 + b];
+    if (!QLDS)
+#pragma unroll
+      for (int i = 0; i < QR; ++i) Q[0][QLDS ? 0 : i] = lds_q[i * 64 + lane];
   };
 
   float m_run[NQ], l_run[NQ];
@@ -362,7 +369,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
 #pragma unroll
       for (int j = 0; j < NQ; ++j) {
         const u32x4 q0 = q_at(j, 0), q1 = q_at(j, 1);
-        const uint32_t s = qs[FOUR ? j : 0];
+        const uint32_t s = qs[j];
         f32x4 x[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) x[h] = scaled_product(R.k[h][0], ks[h], q0, q1, s, zero);
@@ -676,7 +683,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
       for (int e = 0; e < SEGF / 4; ++e) *reinterpret_cast<f32x4 *>(po + (size_t)r * D + seg * SEGF + 4 * e) = sum[e];
       if (seg == 0) *reinterpret_cast<f32x2 *>(pml + r * 2) = f32x2{m, L};
     } else if (r < rows_valid) {
-      const int hsel = r / A.Tq, tq = r - hsel * A.Tq, head = g * A.G + nth_member(mask, hsel);
+      const int hsel = (r * C.tq_inv) >> 16, tq = r - hsel * A.Tq, head = g * A.G + nth_member(mask, hsel);
       const float inv = L > 0.f ? 1.f / L : 0.f;
       const size_t at = (((size_t)bt * A.Tq + tq) * A.Hq + head) * D + seg * SEGF;
 #pragma unroll

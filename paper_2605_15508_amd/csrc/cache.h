@@ -10,6 +10,7 @@ struct CacheAttnArgs {
   const uint8_t *codes, *scales;     // 4-bit cache; strides in bytes
   int64_t code_b, code_h, code_n, code_page;
   int64_t scale_b, scale_h, scale_n, scale_page;
+  int32_t tq_inv;                    // r / Tq = r * tq_inv >> 16 for r < 64
   int32_t window, sinks;             // bf16 cache: see sts_window_attn
   int32_t behind;                    // bf16 cache: 1 = the block's own tokens are not in the cache (k_new)
 };
