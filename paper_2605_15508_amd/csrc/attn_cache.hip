@@ -15,7 +15,7 @@
 //     lane a has the a-th quarter, 16 bytes at head size 128 and one scale; of a bf16 row every fourth chunk of 16 bytes.
 // S over 4-bit codes: v_mfma_scale_f32_16x16x128_f8f6f4 takes K's codes and scales as they lie in memory, a lane 32 channels of a key
 // and their scale. Q, the other operand, is the sum of two e4m3 numbers, high and low, with a scale per 32 channels: four significant bits
-// each hold the eight of a bf16 exactly down to 2^-10 of the group's largest value, and what lies further down to 2^-18 of it.
+// each hold the eight of a bf16 exactly for values of at least 2^-9 of their group's largest, and others to 2^-17 of that largest.
 // At head size 64 both halves go into one instruction, K's row taken twice.
 // V's codes become bf16 pairs in the chip's conversion, scale included, exactly. The pairs are two channels of one key and have to
 // become two keys of one channel: two byte permutes per pair of registers, as for bf16.
@@ -379,11 +379,12 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
           for (int h = 0; h < 2; ++h) St[j][h] = scaled_product(R.k[h][0], ks[h], l0, l1, s, x[h]);
           // The instruction takes eight passes: a result in registers that are partly an operand's would be wrong, and the compiler
           // sees to that for larger results only. So all operands are in use until the results are there.
-          asm volatile("" ::"v"(St[j][0]), "v"(St[j][1]), "v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(l0), "v"(l1), "v"(R.k[0][0]), "v"(R.k[1][0]));
+          asm volatile("" ::"v"(St[j][0]), "v"(St[j][1]), "v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(l0), "v"(l1), "v"(R.k[0][0]), "v"(R.k[1][0]),
+                       "v"(ks[0]), "v"(ks[1]), "v"(s));
         } else {
           St[j][0] = x[0];
           St[j][1] = x[1];
-          asm volatile("" ::"v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(R.k[0][0]), "v"(R.k[1][0]));
+          asm volatile("" ::"v"(x[0]), "v"(x[1]), "v"(q0), "v"(q1), "v"(R.k[0][0]), "v"(R.k[1][0]), "v"(ks[0]), "v"(ks[1]), "v"(s));
         }
       }
     } else {
@@ -422,7 +423,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
       }
     }
   };
-  // the weights exp(S - m) as the B operand of the second product: bf16 (half a step, 2^-9 of each); their sums in fp32
+  // the weights exp(S - m) as the B operand of the second product: bf16 (half a step, 2^-8 of each); their sums in fp32
   auto weights = [&](const f32x4 (&St)[NQ][2], u32x4 (&P)[NQ]) {
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {

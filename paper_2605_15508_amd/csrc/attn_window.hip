@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
         for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
     }
   };
-  // exp(S - m), as the B operands of the second product (bf16, half a step, 2^-9 of each), and their sum in fp32
+  // exp(S - m), as the B operands of the second product (bf16, half a step, 2^-8 of each), and their sum in fp32
   auto weights = [&](const f32x16 (&S)[2], u32x4 (&P)[4]) {
     const float m_ref = m_run == -INFINITY ? 0.f : m_run;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
