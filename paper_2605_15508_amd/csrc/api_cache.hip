@@ -79,7 +79,7 @@ struct CachePlan {
 };
 
 // Units of a short block and how many parts their tiles are cut into: `tiles` at most per unit, `resident` workgroups at once.
-sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, const int32_t *head_map, bool whole, int64_t tiles, int64_t (*resident)(int nq, int d),
+sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, const int32_t *head_map, bool whole, int64_t tiles, int64_t (*resident)(int d),
                        CachePlan &pl) {
   int max_heads = most_rows / Tq;
   if (max_heads < 1) max_heads = 1;
@@ -88,9 +88,9 @@ sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, con
   const int nu = sts_group_units(Hq, Hkv, Tq, max_heads, head_map, whole, pl.units, rows);
   if (nu < 0) return STS_EUNSUPPORTED;
   pl.num_units = nu;
-  pl.nq = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  pl.nq = rows <= 16 ? 1 : 2;
   const int64_t total = (int64_t)B * nu;
-  int64_t S = total > 0 ? resident(pl.nq, d) / total : 1;
+  int64_t S = total > 0 ? resident(d) / total : 1;
   // two tiles for each of four waves at least, and lists of up to 16 tiles whole, as for the bf16 cache
   const int64_t cap = tiles <= 16 ? 1 : (tiles + 2 * STS_WG_WAVES - 1) / (2 * STS_WG_WAVES);
   if (S > cap) S = cap;
@@ -116,7 +116,7 @@ sts_status validate_heads(int B, int Tq, int Hq, int Hkv, int d, int out_dtype, 
   return STS_OK;
 }
 
-int64_t packed_resident(int nq, int d) { return (int64_t)sts_cu_count() * (nq == 4 ? 1 : 2); }
+int64_t packed_resident(int) { return (int64_t)sts_cu_count() * 2; }
 
 sts_status plan_packed(const sts_packed_attn_params *p, CachePlan &pl) {
   if (!p) return STS_EINVAL;
@@ -144,7 +144,7 @@ sts_status plan_packed(const sts_packed_attn_params *p, CachePlan &pl) {
   return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, p->head_map, !lists, (len + STS_TILE_KEYS - 1) / STS_TILE_KEYS, packed_resident, pl);
 }
 
-int64_t window_resident(int nq, int d) { return (int64_t)sts_cu_count() * (d == 128 ? 1 : 2); }
+int64_t window_resident(int d) { return (int64_t)sts_cu_count() * (d == 128 ? 1 : 2); }
 
 sts_status plan_window(const sts_window_params *p, CachePlan &pl, bool &prompt) {
   if (!p) return STS_EINVAL;
