@@ -21,6 +21,8 @@
 // become two keys of one channel: two byte permutes per pair of registers, as for bf16.
 // Scales: a lane loads the word of one token of the tile, K's in the lower half of the wave, V's in the upper, and
 // the lanes pick up those of their rows from LDS, one tile ahead of their use: bytes for K, the conversion's floats for V.
+#include <float.h>
+
 #include "cache.h"
 
 namespace {
@@ -135,7 +137,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
   constexpr int OPITCH = D + 4;
   constexpr bool WIN = !FOUR;
   constexpr bool QLDS = NQ >= 2;
-    __shared__ __attribute__((aligned(16))) float lds_o[W * 16 * OPITCH];
+  __shared__ __attribute__((aligned(16))) float lds_o[W * 16 * OPITCH];
   __shared__ float lds_ml[W][NQ * 16][2];
   __shared__ __attribute__((aligned(16))) u32x4 lds_q[NQ * QR * 64];
   __shared__ uint32_t lds_qs[NQ][2][64];
@@ -635,7 +637,8 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (a == 0) {
-      lds_ml[wave][nq * 16 + b][0] = m_run[nq];
+      // (scores that are no numbers raise no maximum: without one the part would be taken for an empty one)
+      lds_ml[wave][nq * 16 + b][0] = l != l ? top(m_run[nq], -FLT_MAX) : m_run[nq];
       lds_ml[wave][nq * 16 + b][1] = l;
     }
   }
@@ -650,8 +653,8 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
       for (int w = 0; w < W; ++w) m = fmaxf(m, lds_ml[w][r][0]);
       return m;
     };
-    const float top = top_of(nq * 16 + b);
-    const float f = m_run[nq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[nq] - top);
+    const float m_all = top_of(nq * 16 + b);
+    const float f = m_run[nq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[nq] - m_all);
     float *orow = lds_o + (wave * 16 + b) * OPITCH;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -685,7 +688,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
       if (seg == 0) *reinterpret_cast<f32x2 *>(pml + r * 2) = f32x2{m, L};
     } else if (r < rows_valid) {
       const int hsel = (r * C.tq_inv) >> 16, tq = r - hsel * A.Tq, head = g * A.G + nth_member(mask, hsel);
-      const float inv = L > 0.f ? 1.f / L : 0.f;
+      const float inv = L == 0.f ? 0.f : 1.f / L;
       const size_t at = (((size_t)bt * A.Tq + tq) * A.Hq + head) * D + seg * SEGF;
 #pragma unroll
       for (int e = 0; e < SEGF / 4; ++e) {
@@ -699,7 +702,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
         }
       }
       if (A.lse_out && seg == 0)
-        A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + tq] = L > 0.f ? (m + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
+        A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + tq] = L == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f;
     }
     __syncthreads();
   }

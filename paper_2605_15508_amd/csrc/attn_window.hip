@@ -11,6 +11,8 @@
 // LDS by the transposing read (four lanes have 16 channels of a key, lane i gets channel i of four keys).
 // LDS chunks of 16 bytes are permuted within a row so that neither K's reads (16 rows, one chunk each) nor V's (4 rows, 64
 // bytes each) meet in a bank.
+#include <float.h>
+
 #include "cache.h"
 
 namespace {
@@ -101,8 +103,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
 #pragma unroll
   for (int m = 0; m < NL; ++m) {
     const int row = row0 + RL * m;
-    k_off[m] = (uint32_t)(row * (int)row_bytes + 16 * k_chunk<D>(row, slot0));
-    v_off[m] = (uint32_t)(row * (int)row_bytes + 16 * v_chunk<D>(row, slot0));
+    k_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * k_chunk<D>(row, slot0);
+    v_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * v_chunk<D>(row, slot0);
   }
   // K's or V's tile t (past the last: the last again, which nobody reads)
   auto load = [&](int t, const unsigned char *from, u32x4 *to, bool is_v) {
@@ -247,7 +249,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
 
   // ---- The next tile's scores are worked out while this one's weights are: matrix and vector instructions of one wave, which do not wait
   // for each other. K is a tile ahead of V.
-  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); };
+  // What was asked for has come, and what was read is in registers: the tiles change hands.
+  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
   bool later = false;              // tiles left for the end: see below
   if (begin < tiles) {
     f32x16 S[2];
@@ -345,7 +348,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         *reinterpret_cast<f32x4 *>(o + 32 * dt + 8 * e) = f32x4{acc[dt][4 * e], acc[dt][4 * e + 1], acc[dt][4 * e + 2], acc[dt][4 * e + 3]};
-    if (h == 0) *reinterpret_cast<f32x2 *>(A.part_ml + row * 2) = f32x2{m_run, l_run};
+    // (scores that are no numbers raise no maximum: without one the part would be taken for an empty one)
+    if (h == 0) *reinterpret_cast<f32x2 *>(A.part_ml + row * 2) = f32x2{l_run != l_run ? top(m_run, -FLT_MAX) : m_run, l_run};
     return;
   }
   if (!ok) return;

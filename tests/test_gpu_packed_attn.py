@@ -321,3 +321,21 @@ def test_prepared_calls_do_not_share_scratch():
     torch.cuda.synchronize()
     for call, want in sets:
         assert all(torch.equal(a, b) for a, b in zip(call.result, want))
+
+
+@pytest.mark.parametrize("N", [40, 2000])
+def test_keys_that_are_no_numbers(N):
+    """One key, and all of them: their rows have no result, whatever the rest is split into."""
+    g = gen(12)
+    codes, scales, _, k, v = packed_cache(1, 2, N, 128, g)
+    q = queries(1, 2, 4, 128, g)
+    ref = attention(q, 0.1, all_tokens(k, v, 4, 2), q_halves=True)
+    for bad in (slice(N - 1, N), slice(0, N // 2), slice(0, N)):
+        sc = scales.clone()
+        sc[:, 1, bad, 0, 1] = 255
+        o, l = (x.cpu() for x in run(q, codes, sc, 0.1, out_dtype=torch.float32))
+        assert torch.isnan(o[:, :, 2:]).all() and not torch.isfinite(l[:, 2:]).any()
+        assert ((o[:, :, :2].double() - ref[0][:, :, :2]).abs() <= ref[2][:, :, :2]).all()
+    q[0, 1, 3, 5] = float("inf")
+    o = run(q, codes, scales, 0.1, out_dtype=torch.float32)[0].cpu()
+    assert torch.isnan(o[0, 1, 3]).all() and torch.isfinite(o[0, 0]).all() and torch.isfinite(o[0, 1, :3]).all()

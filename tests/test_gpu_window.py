@@ -266,3 +266,30 @@ def test_long_windows(Tq, N, window):
         sums = (N / 8 + 64) * 2.0 ** -24
         assert ((o[0, :, t].double() - want).abs() <= (2.0 ** -8 + 2.2 * d_s + 2.0 ** -20 + sums) * size).all()
         assert ((l[0, t].double() - z).abs() <= d_s + sums + 2.0 ** -20 + 2.0 ** -22 * z.abs()).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,Tq,N,window,sinks", [(1, 3, 900, 700, 4), (1, 1, 40, 40, 0), (2, 40, 900, 700, 4), (4, 300, 300, 90, 2)])
+def test_keys_that_are_no_numbers(B, Tq, N, window, sinks, d):
+    """One key, and all of them: who sees one has no result, whatever the rest is split into; who does not is as without."""
+    q, k, v, _, _ = data(B, Tq, 4, 2, N, d, 12)
+    see = visible(B, Tq, N, window, sinks, None, False)(0)
+    for bad in ([N - 2], list(range(N - min(window, N) // 2, N)), list(range(N))):
+        kk = k.clone()
+        kk[:, 1, bad] = float("nan")
+        o, _ = run(q, kk, v, 0.1, window, sinks, out_dtype=torch.float32)
+        hit = see[:, bad].any(1)
+        o = o.cpu()
+        assert torch.isnan(o[:, hit, 2:]).all()
+        ref = reference(q, k, v, 0.1, window, sinks)
+        assert ((o[:, :, :2].double() - ref[0][:, :, :2]).abs() <= ref[2][:, :, :2]).all()
+        assert ((o[:, ~hit, 2:].double() - ref[0][:, ~hit, 2:]).abs() <= ref[2][:, ~hit, 2:] + 1e-30).all()
+
+
+@pytest.mark.parametrize("Tq,window", [(1, 1), (4, 4), (1, 3)])
+def test_the_cache_is_not_looked_at_where_the_window_is_the_block(Tq, window):
+    """Own tokens fill the window, or nearly: the cached ones that nobody sees may be anything."""
+    q, k, v, kn, vn = data(1, Tq, 4, 2, 70, 128, 13, tail=True)
+    ref = reference(q, k, v, 0.1, window, 0, None, kn, vn)
+    k[:, :, : 70 - window + 1], v[:, :, : 70 - window + 1] = float("inf"), float("nan")
+    check(run(q, k, v, 0.1, window, 0, k_new=kn, v_new=vn, out_dtype=torch.float32), ref)
