@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(THREADS) packed_store_kernel(const PackedRowsA
   constexpr int LANES = D / 8;
   const int b = blockIdx.y, row = blockIdx.x * (THREADS / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
   const int t = row / A.Hkv, h = row - t * A.Hkv;
-  const int n = (A.pos ? A.pos[b] : 0) + t;
+  const int n = (int)((uint32_t)(A.pos ? A.pos[b] : 0) + (uint32_t)t);          // (past the largest int: negative)
   const bool live = t < (A.lens ? min(A.lens[b], A.T) : A.T) && n >= 0 && n < A.N;
   // (a quad's lanes all hold the same row; lanes of rows that are not stored take part in the exchange with zeros)
   u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(THREADS) packed_load_kernel(const PackedRowsAr
   const int b = blockIdx.y, row = blockIdx.x * (THREADS / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
   const int t = row / A.Hkv, h = row - t * A.Hkv;
   if (t >= (A.lens ? min(A.lens[b], A.T) : A.T)) return;
-  const int n = (A.pos ? A.pos[b] : 0) + t;
+  const int n = (int)((uint32_t)(A.pos ? A.pos[b] : 0) + (uint32_t)t);          // (past the largest int: negative)
   u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
   if (n >= 0 && n < A.N) {
     int64_t code, scale;

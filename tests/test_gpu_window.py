@@ -293,3 +293,13 @@ def test_the_cache_is_not_looked_at_where_the_window_is_the_block(Tq, window):
     ref = reference(q, k, v, 0.1, window, 0, None, kn, vn)
     k[:, :, : 70 - window + 1], v[:, :, : 70 - window + 1] = float("inf"), float("nan")
     check(run(q, k, v, 0.1, window, 0, k_new=kn, v_new=vn, out_dtype=torch.float32), ref)
+
+
+@pytest.mark.parametrize("Tq", [3, 60])
+def test_windows_and_sinks_beyond_any_cache(Tq):
+    q, k, v, _, _ = data(1, Tq, 4, 2, 90, 64, 14)
+    ref = reference(q, k, v, 0.1, 1000, 0)
+    for window, sinks in ((10 ** 12, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 10 ** 12)):
+        check(run(q, k, v, 0.1, window, sinks, out_dtype=torch.float32), ref, f"{window} {sinks}")
+    with pytest.raises(sts.StsError):
+        run(q, k, v, 0.1, -(2 ** 31), 0)
