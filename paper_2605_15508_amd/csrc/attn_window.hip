@@ -33,8 +33,10 @@ __device__ __forceinline__ uint64_t first_keys(int n) { return n <= 0 ? 0 : n >=
 
 __device__ __forceinline__ float top(float x, float y) { return __builtin_elementwise_maximum(x, y); }      // (a NaN wins)
 
-template <int D, bool PAGED>
-__global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const WindowArgs A) {
+// PAGES: 0 none; 1 with rows at up to 2^32 units of 16 bytes in the pool; 2 further away
+template <int D, int PAGES>
+// (head size 64: registers for three workgroups on a compute unit: 4000 rows, pages of one token 65 us, with two 71)
+__global__ void __launch_bounds__(64 * WAVES, D == 64 && PAGES < 2 ? 3 : 2) window_prompt_kernel(const WindowArgs A) {
   constexpr int KS = D / 16;             // contraction steps of S
   constexpr int DT = D / 32;             // 32-channel tiles of O
   constexpr int CH = D / 8;              // 16-byte chunks of a row
@@ -42,6 +44,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
   constexpr int RL = 64 / CH;                      // rows that a wave's load covers
   // (four arrays, not two of two: so the compiler can tell the loads that fill one from the reads of another)
   __shared__ __attribute__((aligned(16))) u32x4 lds_k0[TK * CH], lds_k1[TK * CH], lds_v0[TK * CH], lds_v1[TK * CH];
+  __shared__ __attribute__((aligned(16))) uint32_t lds_odd[2][WAVES];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
@@ -90,9 +93,9 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
   // row's chunks is in what a lane asks for. Rows that no query of the block sees are read from ones that some query does: their weight
   // is 0, but 0 times what lies there may be NaN.
   const int row0 = wave * NL * RL + lane / CH, slot0 = lane % CH;
-  const int64_t row_bytes = A.stride_n * 2, head_off = ((PAGED ? 0 : bt * A.stride_b) + g * A.stride_h) * 2;
+  const int64_t row_bytes = A.stride_n * 2, page_bytes = A.stride_page * 2, head_off = ((PAGES ? 0 : bt * A.stride_b) + g * A.stride_h) * 2;
   const unsigned char *kbase = reinterpret_cast<const unsigned char *>(A.k) + head_off, *vbase = reinterpret_cast<const unsigned char *>(A.v) + head_off;
-  const int32_t *table = PAGED ? A.block_table + (size_t)bt * A.table_stride : nullptr;
+  const int32_t *table = PAGES ? A.block_table + (size_t)bt * A.table_stride : nullptr;
   auto row_of = [&](int v) {           // (past the last place: the last key)
     v = min(v, places - 1);
     return v < firsts ? v : v + skipped;
@@ -106,12 +109,32 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
     k_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * k_chunk<D>(row, slot0);
     v_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * v_chunk<D>(row, slot0);
   }
+  // Pages: lane i looks up the page of row i % 16 of its wave's sixteen and tells the lanes that ask for the rows where they lie, a tile
+  // before they do (looked up when asked for, with offsets in 64 bits: 33001 tokens in pages of 16, 181 us; so 167; without pages 151).
+  struct Where {
+    uint32_t row[PAGES == 1 ? NL : 1];
+  };
+  const uint32_t page_mask = (1u << A.page_shift) - 1;
+  auto my_row = [&](int t) { return row_of(min(t, tiles - 1) * TK + wave * (NL * RL) + lane % (NL * RL)); };
+  auto page_of = [&](int t) { return PAGES ? min(max(table[my_row(t) >> A.page_shift], 0), A.num_pages - 1) : 0; };
+  auto where = [&](int t, int page) {
+    Where at;
+    if constexpr (PAGES == 1) {
+      const uint32_t mine = (uint32_t)page * (uint32_t)(A.stride_page / 8) + ((uint32_t)my_row(t) & page_mask) * (uint32_t)(A.stride_n / 8);
+#pragma unroll
+      for (int m = 0; m < NL; ++m) at.row[m] = (uint32_t)__shfl((int)mine, lane / CH + RL * m, 64);
+    } else {
+      at.row[0] = (uint32_t)page;
+    }
+    return at;
+  };
+  static_assert(NL * RL == 16, "");
   // K's or V's tile t (past the last: the last again, which nobody reads)
-  auto load = [&](int t, const unsigned char *from, u32x4 *to, bool is_v) {
+  auto load = [&](int t, const unsigned char *from, u32x4 *to, bool is_v, const Where &at) {
     const int v0 = min(t, tiles - 1) * TK, n0 = v0 + skipped;
     u32x4 *const mine = to + wave * NL * 64;
-    auto chunk = [&](int m) { return 16 * (is_v ? v_chunk<D>(row0 + RL * m, slot0) : k_chunk<D>(row0 + RL * m, slot0)); };
-    if (!PAGED && v0 >= firsts && v0 + TK <= places) {
+    auto chunk = [&](int m) { return is_v ? v_chunk<D>(row0 + RL * m, slot0) : k_chunk<D>(row0 + RL * m, slot0); };
+    if (!PAGES && v0 >= firsts && v0 + TK <= places) {
       const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(from + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
 #pragma unroll
       for (int m = 0; m < NL; ++m) __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_ptr)(mine + 64 * m), 16, (int)(is_v ? v_off[m] : k_off[m]), 0, 0, 0);
@@ -120,10 +143,16 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
       typedef const __attribute__((address_space(1))) unsigned char *global_ptr;
 #pragma unroll
       for (int m = 0; m < NL; ++m) {
-        const int n = row_of(v0 + row0 + RL * m);
-        int64_t at = n * row_bytes;
-        if (PAGED) at = (min(max(table[n >> A.page_shift], 0), A.num_pages - 1) * A.stride_page + (n & ((1 << A.page_shift) - 1)) * A.stride_n) * 2;
-        __builtin_amdgcn_global_load_lds((global_ptr)(from + at + chunk(m)), (lds_ptr)(mine + 64 * m), 16, 0, 0);
+        uint64_t off;            // (none of the factors is negative)
+        if constexpr (PAGES == 1) {
+          off = (uint64_t)(at.row[m] + chunk(m)) << 4;
+        } else if constexpr (PAGES == 2) {
+          const uint32_t page = (uint32_t)__shfl((int)at.row[0], lane / CH + RL * m, 64);
+          off = (uint64_t)page * (uint64_t)page_bytes + ((uint32_t)row_of(v0 + row0 + RL * m) & page_mask) * (uint32_t)row_bytes + 16 * chunk(m);
+        } else {
+          off = (uint64_t)(uint32_t)row_of(v0 + row0 + RL * m) * (uint64_t)row_bytes + 16 * chunk(m);
+        }
+        __builtin_amdgcn_global_load_lds((global_ptr)(from + off), (lds_ptr)(mine + 64 * m), 16, 0, 0);
       }
     }
   };
@@ -229,14 +258,18 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
       }
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
-  // a tile that not every query sees whole, with a value that is no number, or infinite
-  auto odd_values = [&](int t, const u32x4 *v) {
-    if (!masked(t)) return false;
+  // A tile that not every query of the block sees whole: has it a value that is no number, or infinite? Each wave looks through the rows
+  // that it asked for, in slot `at`; the answer is there after the next barrier.
+  auto partly_seen = [&](int t) {
+    const int n0 = first_of(t);
+    return !(n0 + TK - 1 <= b_lo && (n0 + TK <= A.sinks || b_hi - max(n0, lo) < A.window));
+  };
+  auto look_through = [&](const u32x4 *v, int at) {
     float z[4] = {0.f, 0.f, 0.f, 0.f};            // sums of 0 times the values: 0, or no number
     const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
 #pragma unroll
-    for (int m = 0; m < TK * CH / 64; ++m) {
-      const u32x4 w = *(lds_u32x4)((lds_ptr)v + 16 * lane + 1024 * m);
+    for (int m = 0; m < NL; ++m) {
+      const u32x4 w = *(lds_u32x4)((lds_ptr)v + 16 * (lane + 64 * (wave * NL + m)));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t x = w[e];
@@ -244,7 +277,15 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
       }
     }
     const float all = (z[0] + z[1]) + (z[2] + z[3]);
-    return __builtin_amdgcn_ballot_w64(all != 0.f) != 0;       // (true for what is no number)
+    const bool mine = __builtin_amdgcn_ballot_w64(all != 0.f) != 0;       // (true for what is no number)
+    if (lane == 0) lds_odd[at][wave] = mine;
+  };
+  auto odd_values = [&](int at) {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    uint32_t any = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) any |= lds_odd[at][w];
+    return __builtin_amdgcn_readfirstlane((int)any) != 0;
   };
 
   // ---- The next tile's scores are worked out while this one's weights are: matrix and vector instructions of one wave, which do not wait
@@ -254,18 +295,28 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
   bool later = false;              // tiles left for the end: see below
   if (begin < tiles) {
     f32x16 S[2];
-    load(begin, kbase, lds_k0, false);
+    const int page0 = page_of(begin), page1 = page_of(begin + 1), page2 = page_of(begin + 2);
+    Where at_v = where(begin, page0);
+    load(begin, kbase, lds_k0, false, at_v);
+    load(begin, vbase, lds_v0, true, at_v);
+    at_v = where(begin + 1, page1);
+    load(begin + 1, kbase, lds_k1, false, at_v);
+    Where at_k = where(begin + 2, page2);
     arrived();
-    load(begin + 1, kbase, lds_k1, false);
-    load(begin, vbase, lds_v0, true);
     product(lds_k0, S);
     if (masked(begin)) hide(begin, S);
     raise(highest(S));
     auto step = [&](int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
       arrived();
-      load(t + 2, kbase, k_free, false);
-      load(t + 1, vbase, v_free, true);
-      const bool odd = odd_values(t, v);
+      load(t + 2, kbase, k_free, false, at_k);
+      load(t + 1, vbase, v_free, true, at_v);
+      at_v = at_k;
+      at_k = where(t + 3, page_of(t + 3));
+      bool odd = false;
+      if (partly_seen(t)) {
+        look_through(v, t & 1);
+        odd = odd_values(t & 1);
+      }
       f32x16 N[2];
       u32x4 P[4];
       product(k_next, N);
@@ -300,10 +351,13 @@ __global__ void __launch_bounds__(64 * WAVES, 2) window_prompt_kernel(const Wind
     if (__syncthreads_or(later)) {
       for (int t = begin; t < tiles; ++t) {
         arrived();
-        load(t, kbase, lds_k0, false);
-        load(t, vbase, lds_v0, true);
+        const Where at = where(t, page_of(t));
+        load(t, kbase, lds_k0, false, at);
+        load(t, vbase, lds_v0, true, at);
         arrived();
-        if (!odd_values(t, lds_v0)) continue;
+        if (!partly_seen(t)) continue;
+        look_through(lds_v0, 0);
+        if (!odd_values(0)) continue;
         u32x4 P[4];
         product(lds_k0, S);
         hide(t, S);
@@ -423,12 +477,16 @@ __global__ void __launch_bounds__(256) window_combine_kernel(const WindowArgs A)
 
 hipError_t launch_window_prompt(const WindowArgs &a, int d, hipStream_t s) {
   const dim3 grid((unsigned)(((int64_t)a.Tq * a.G + ROWS - 1) / ROWS * a.Hkv * a.B * a.num_splits)), block(64 * WAVES);
+  // a pool whose rows lie within 64 GB: their offsets fit 32 bits in units of 16 bytes
+  const int pages = !a.block_table ? 0 : (a.num_pages + 1.0) * (double)a.stride_page + 32.0 * (double)a.stride_n < 8.0 * 4294967296.0 ? 1 : 2;
   if (d == 128) {
-    if (a.block_table) STS_LAUNCH((window_prompt_kernel<128, true>), grid, block, 0, s, a);
-    else STS_LAUNCH((window_prompt_kernel<128, false>), grid, block, 0, s, a);
+    if (pages == 2) STS_LAUNCH((window_prompt_kernel<128, 2>), grid, block, 0, s, a);
+    else if (pages) STS_LAUNCH((window_prompt_kernel<128, 1>), grid, block, 0, s, a);
+    else STS_LAUNCH((window_prompt_kernel<128, 0>), grid, block, 0, s, a);
   } else {
-    if (a.block_table) STS_LAUNCH((window_prompt_kernel<64, true>), grid, block, 0, s, a);
-    else STS_LAUNCH((window_prompt_kernel<64, false>), grid, block, 0, s, a);
+    if (pages == 2) STS_LAUNCH((window_prompt_kernel<64, 2>), grid, block, 0, s, a);
+    else if (pages) STS_LAUNCH((window_prompt_kernel<64, 1>), grid, block, 0, s, a);
+    else STS_LAUNCH((window_prompt_kernel<64, 0>), grid, block, 0, s, a);
   }
   return sts_take_launch_status();
 }

@@ -303,3 +303,22 @@ def test_windows_and_sinks_beyond_any_cache(Tq):
         check(run(q, k, v, 0.1, window, sinks, out_dtype=torch.float32), ref, f"{window} {sinks}")
     with pytest.raises(sts.StsError):
         run(q, k, v, 0.1, -(2 ** 31), 0)
+
+
+@pytest.mark.parametrize("apart", [2 ** 29, 2 ** 32])
+@pytest.mark.parametrize("Tq", [5, 40])
+def test_pages_that_lie_far_apart(Tq, apart):
+    """Pages 1 GB apart and 8 GB apart: offsets of more than 32 bits, and of more than 32 bits of 16 bytes."""
+    N, d, page, Hkv = 70, 64, 8, 2
+    q, k, v, _, _ = data(1, Tq, 4, Hkv, N, d, 15)
+    ref = reference(q, k, v, 0.1, 45, 3)
+    kp, vp = (to_pages(t, page, None, 1) for t in (k, v))
+    pool = torch.empty((kp.shape[0] - 1) * apart + 2 * kp[0].numel(), dtype=torch.bfloat16, device=DEV)
+    far = [pool[j * kp[0].numel():].as_strided(kp.shape, (apart, page * d, d, 1)) for j in range(2)]
+    for t, rows in zip(far, (kp, vp)):
+        t.copy_(rows)
+    try:
+        check(run(q, *far, 0.1, 45, 3, page_size=page, N=N, block_table=table_of(1, N, page, None, 1), out_dtype=torch.float32), ref)
+    finally:
+        del far, pool
+        torch.cuda.empty_cache()
