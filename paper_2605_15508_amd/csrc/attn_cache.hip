@@ -364,13 +364,21 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
 
   // ---- one tile
   // S^T = K Q^T
+  // (Q's first quads are read from LDS while the tile before is worked on)
+  u32x4 q_next[2];
+  auto next_q = [&] {
+    if (FOUR && QLDS) {
+      q_next[0] = lds_q[lane];
+      q_next[1] = lds_q[64 + lane];
+    }
+  };
   auto scores = [&](const Tile &R, f32x4 (&St)[NQ][2]) {
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     auto q_at = [&](int nq, int i) { return QLDS ? lds_q[(nq * QR + i) * 64 + lane] : Q[QLDS ? 0 : nq][QLDS ? 0 : i]; };
     if constexpr (FOUR) {
 #pragma unroll
       for (int j = 0; j < NQ; ++j) {
-        const u32x4 q0 = q_at(j, 0), q1 = q_at(j, 1);
+        const u32x4 q0 = QLDS && j == 0 ? q_next[0] : q_at(j, 0), q1 = QLDS && j == 0 ? q_next[1] : q_at(j, 1);
         const uint32_t s = qs[j];
         f32x4 x[2];
 #pragma unroll
@@ -430,13 +438,10 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
       const float m_ref = WIN && m_run[j] == -INFINITY ? 0.f : m_run[j];
-      float p[8], sum = 0.f;
+      float p[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(St[j][i >> 2][i & 3], sl2, -m_ref));
-        sum += p[i];
-      }
-      l_run[j] += sum;
+      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(St[j][i >> 2][i & 3], sl2, -m_ref));
+      l_run[j] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 #pragma unroll
       for (int i = 0; i < 4; ++i) P[j][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p[2 * i], p[2 * i + 1]}), bf16x2));
     }
@@ -558,11 +563,13 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) 
   if (nv > 0) {
     put_scales(R[0].sc, 0);
     get_scales(0);
+    next_q();
     auto step = [&](int v, int j, bool more) {
       const int t = tile_of(v), n = (j + 1) % PF, left = c - first_of(t);
       put_scales(R[n].sc, (v + 1) & 1);
       consume(R[j], t, GATHER ? seen[j] : left >= TK ? 0xffffffffu : (1u << left) - 1u);
       get_scales((v + 1) & 1);
+      next_q();
       if (more) {
         if constexpr (!GATHER) {
           issue_near(tile_of(v + PF), R[j]);
