@@ -302,6 +302,11 @@ sts_status sts_window_attn(const sts_window_params *p, void *stream) {
     w.lse_out = p->lse_out;
     w.out_dtype = p->out_dtype;
     w.num_splits = pl.num_splits;
+    w.blocks = (int32_t)(((int64_t)w.Tq * w.G + STS_WINDOW_ROWS - 1) / STS_WINDOW_ROWS);
+    w.by_splits = divide_by(w.num_splits);
+    w.by_blocks = divide_by(w.blocks);
+    w.by_heads = divide_by(w.Hkv);
+    w.by_group = divide_by(w.G);
     if (pl.num_splits > 1) {
       if (!p->workspace || p->workspace_bytes < pl.part_o_bytes + pl.part_ml_bytes || !aligned(p->workspace, 256)) return STS_EWORKSPACE;
       w.part_o = static_cast<float *>(p->workspace);

@@ -48,25 +48,28 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 && PAGES < 2 ? 3 : 2) wind
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
+  // what the first loads need of the arguments, asked for together: waits for scalar loads cannot tell them apart
+  asm volatile("" ::"s"(A.q), "s"(A.k), "s"(A.v), "s"(A.stride_b), "s"(A.stride_h), "s"(A.stride_n), "s"(A.seq_lens), "s"(A.block_table), "s"(A.Tq), "s"(A.Hq), "s"(A.Hkv),
+               "s"(A.G), "s"(A.N), "s"(A.window), "s"(A.sinks), "s"(A.scale), "s"(A.scale_log2), "s"(A.num_splits), "s"(A.blocks), "s"(A.by_splits.mul),
+               "s"(A.by_splits.shift), "s"(A.by_blocks.mul), "s"(A.by_blocks.shift), "s"(A.by_heads.mul), "s"(A.by_heads.shift), "s"(A.by_group.mul),
+               "s"(A.by_group.shift));
   // Blocks of one KV head next to each other on one die (workgroup i runs on die i % 8), the later positions, which may have
   // more keys, first.
-  const int nb = (int)(((int64_t)A.Tq * A.G + ROWS - 1) / ROWS);
   const int total = gridDim.x, x = blockIdx.x % STS_XCDS;
   const int j = x * (total / STS_XCDS) + min(x, total % STS_XCDS) + blockIdx.x / STS_XCDS;
-  const int split = j % A.num_splits, unit = j / A.num_splits;
-  const int blk = nb - 1 - unit % nb, g = unit / nb % A.Hkv, bt = unit / nb / A.Hkv;
+  const int unit = A.by_splits.of(j), split = j - unit * A.num_splits;
+  const int head_unit = A.by_blocks.of(unit), blk = A.blocks - 1 - (unit - head_unit * A.blocks);
+  const int bt = A.by_heads.of(head_unit), g = head_unit - bt * A.Hkv;
 
   const int L = A.seq_lens ? min(max(A.seq_lens[bt], 0), A.N) : A.N;
   const int p_first = L - A.Tq;                                   // position of query 0
-  const int64_t rows = (int64_t)A.Tq * A.G;
-  const int64_t r_mine = (int64_t)blk * ROWS + wave * 32 + col;
-  const bool ok = r_mine < rows;
-  const int r = (int)min(r_mine, rows - 1);
-  const int qi = r / A.G, head = g * A.G + r - qi * A.G;
+  const int rows = A.Tq * A.G, row_0 = blk * ROWS, row_w = row_0 + wave * 32;
+  const bool ok = row_w + col < rows;
+  const int r = min(row_w + col, rows - 1);
+  const int qi = A.by_group.of(r), head = g * A.G + r - qi * A.G;
   const int p = p_first + qi;                                     // this lane's query
-  const int b_lo = p_first + blk * ROWS / A.G, b_hi = p_first + (int)min((int64_t)blk * ROWS + ROWS - 1, rows - 1) / A.G;       // the workgroup's
-  const int w_lo = p_first + (int)(min((int64_t)blk * ROWS + wave * 32, rows - 1)) / A.G;                                       // the wave's
-  const int w_hi = p_first + (int)(min((int64_t)blk * ROWS + wave * 32 + 31, rows - 1)) / A.G;
+  const int b_lo = p_first + A.by_group.of(row_0), b_hi = p_first + A.by_group.of(min(row_0 + ROWS - 1, rows - 1));          // the workgroup's
+  const int w_lo = p_first + A.by_group.of(min(row_w, rows - 1)), w_hi = p_first + A.by_group.of(min(row_w + 31, rows - 1)); // the wave's
 
   // The keys that some query of the block sees, one after the other: those of `firsts` sinks before lo, then lo .. end - 1. Place v holds key v, or
   // v + skipped from `firsts` on.

@@ -26,6 +26,18 @@ struct PackedRowsArgs {
   int32_t B, T, Hkv, d;
 };
 
+// n / d for 0 <= n < 2^31 as a product (Granlund and Montgomery, "Division by invariant integers using multiplication"): with 2^l >= d > 2^(l-1)
+// and mul = floor(2^(31+l) / d) + 1, n * mul >> 31 + l is exact. A division takes a wave some forty instructions.
+struct Divisor {
+  uint32_t mul, shift;
+  __host__ __device__ __forceinline__ int of(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
+};
+inline Divisor divide_by(int d) {
+  uint32_t l = 0;
+  while ((1ll << l) < d) ++l;
+  return {(uint32_t)(((uint64_t)1 << (31 + l)) / (uint64_t)d + 1), 31 + l};
+}
+
 // Attention with a window over many query rows (attn_window.hip)
 struct WindowArgs {
   const uint16_t *q, *k, *v;
@@ -35,6 +47,8 @@ struct WindowArgs {
   int32_t page_shift, table_stride, num_pages;
   float scale, scale_log2;
   int32_t num_splits;                // workgroups per block of rows, each with a part of its keys
+  int32_t blocks;                    // blocks of STS_WINDOW_ROWS rows of a KV head
+  Divisor by_splits, by_blocks, by_heads, by_group;
   float *part_o, *part_ml;           // [units][num_splits][STS_WINDOW_ROWS][d], [..][2]
   void *out;
   float *lse_out;

@@ -72,6 +72,7 @@ hipError_t launch_attn_combine(const AttnArgs &a, int d, int nq, hipStream_t) {
   return hipSuccess;
 }
 static void check_window(const WindowArgs &a, int d) {
+  if (a.blocks != (a.Tq * (int64_t)a.G + STS_WINDOW_ROWS - 1) / STS_WINDOW_ROWS || a.by_blocks.of(a.blocks) != 1 || a.by_heads.of(a.Hkv) != 1) fail("window: divisors");
   if (a.num_splits < 1 || a.num_splits > 64 || a.Tq <= 16 || a.window < 1 || a.sinks < 0) fail("window: args");
   if (a.num_splits > 1) {
     const size_t blocks = ((size_t)a.Tq * a.G + STS_WINDOW_ROWS - 1) / STS_WINDOW_ROWS * a.Hkv * a.B, rows = blocks * a.num_splits * STS_WINDOW_ROWS;
@@ -109,8 +110,23 @@ static bool with_workspace(P &p, Q query, F call, bool always) {
   return rc == STS_OK;
 }
 
+// the divisions by multiplication: small divisors and next to powers of two, dividends next to multiples and at the ends
+static void check_divisors() {
+  auto one = [](int64_t d) {
+    if (d < 1 || d > 0x7fffffff) return;
+    const Divisor by = divide_by((int)d);
+    const int64_t most = 0x7fffffff / d * d;
+    for (int64_t n : {(int64_t)0, (int64_t)1, d - 1, d, d + 1, 2 * d - 1, 2 * d, 977 * d - 1, 977 * d, most - 1, most, (int64_t)0x7fffffff})
+      if (n >= 0 && n <= 0x7fffffff && by.of((int)n) != n / d) fail("division by multiplication");
+  };
+  for (int d = 1; d <= 100000; ++d) one(d);
+  for (int s = 0; s <= 31; ++s)
+    for (int64_t k = -3; k <= 3; ++k) one((1ll << s) + k);
+}
+
 int main() {
   long calls = 0, accepted = 0;
+  check_divisors();
   const int Bs[] = {0, 1, 4, 33, 70000}, Tqs[] = {1, 3, 5, 8, 16, 17, 300, 8192}, Ns[] = {0, 1, 31, 4096, 131072, 0x7fffffff - 65536};
   for (int B : Bs) for (int Tq : Tqs) for (int N : Ns) for (int d : {64, 128})
     for (int Hkv : {1, 2, 8, 16}) for (int G : {1, 3, 4, 8, 16}) {
