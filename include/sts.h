@@ -289,12 +289,12 @@ sts_status sts_dense_attn(const sts_attn_params *p, void *stream);
 sts_status sts_sparse_attn_static(const sts_attn_params *p, void *stream);
 
 /* ----------------------------------------------------------------------------------------
- * A cache held in 4 bits (paper Section 2.3 keeps the full cache, whose size Section 6.2 has to move to
- * host memory: at 4.25 bits a value it takes 0.27 of the bf16 cache's bytes). Per token and KV head `codes` hold d/2
+ * A cache held in 4 bits (the paper keeps the full cache, Section 2.3; at 4.25 bits a value it takes 0.27 of
+ * the bf16 cache's bytes). Per token and KV head `codes` hold d/2
  * bytes for K, then d/2 for V, two values to a byte (the even channel in the low half): a sign in
  * the top bit and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6. `scales` hold one byte s for every 32
  * neighbouring channels, d/32 for K, then d/32 for V: the codes stand for their number times 2^(s-127), and all 32
- * for NaN where s is 255. (These are the e2m1 and e8m0 types of the OCP microscaling formats.)
+ * for NaN where s is 255; the store writes 2 <= s <= 252, and other s up to 252 are read as they say. (These are the e2m1 and e8m0 types of the OCP microscaling formats.)
  *
  * Token n of batch element b and KV head g lies at b*stride_b + g*stride_h + n*stride_n of either
  * array (byte strides); with block_table, at page*stride_page + g*stride_h + (n % page_size)*stride_n with
@@ -302,7 +302,7 @@ sts_status sts_sparse_attn_static(const sts_attn_params *p, void *stream);
  *
  * Supported: d in {64,128}; page_size 1, 2, 4, 8, 16 or 32; codes 16-byte aligned with strides that are
  * multiples of 16, scales aligned to d/16 with strides that are multiples of it, stride_n at least a token's
- * bytes (d codes, d/16 scales). Tokens, heads, batch elements and pages must not overlap where the cache is
+ * bytes (d codes, d/16 scales) and at most 2^26. Tokens, heads, batch elements and pages must not overlap where the cache is
  * written to.
  */
 typedef struct {
@@ -322,10 +322,12 @@ typedef struct {
  * is off by more than half a step, saturation at 6 included) and rounds x / 2^e to the nearest code, ties to the even
  * one. A group with a NaN or an infinity becomes NaN as a whole. Rows i >= lens[b], and positions outside
  * [0, N), are not stored; nothing else of the cache is written to. Two rows of one call must not name the same
- * place (pages shared between batch elements, for instance).
+ * place (pages shared between batch elements, for instance): what is then kept there is not defined.
  *
  * sts_packed_load -- the same rows of the cache as the bf16 values they stand for (exact). Rows i >= lens[b] of the
  * outputs stay as they were; rows at positions outside [0, N) become 0.
+ *
+ * Supported: B <= 65535, T * Hkv < 2^31 - 65536; k and v 16-byte aligned.
  */
 typedef struct {
   int32_t B, T, Hkv, d;
@@ -337,7 +339,12 @@ typedef struct {
 
 /* sts_packed_attn -- sts_sparse_attn (indices given) or sts_dense_attn (indices NULL) over the 4-bit cache: the formulas,
  * lists, blocks, pages and the block's own tokens of sts_attn_params with K and V the values that the cache stands for.
- * The products are bf16 with fp32 sums; the cached values are exact in bf16. Fields as there.
+ * Sums and softmax statistics are fp32; the cached values enter the products exactly, a query's value to 2^-17 of the
+ * largest of its 32 channels, a weight as bf16. Fields as there.
+ * A group of K that is NaN makes the rows that see its token NaN, one of V their 32 channels; the logarithm lse_out is then no finite
+ * number. Tokens that no list names and tokens behind a sequence's end never reach a result, whatever lies there.
+ *
+ * Supported: Tq <= 16; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; q, out, k_new and v_new 16-byte aligned; scale finite.
  */
 typedef struct {
   int32_t B, Tq, Hq, Hkv, d;
@@ -361,18 +368,21 @@ typedef struct {
 
 /* ----------------------------------------------------------------------------------------
  * sts_window_attn -- attention with a sliding window and a few first tokens that stay visible
- * (attention sinks; the paper compares with such a policy in Section 6.1, and layers whose sparsity it
- * finds too low for lists need one that no draft decides), over a bf16 cache.
+ * (attention sinks), over a bf16 cache: for layers that no draft's lists decide, and as the fixed policy that the
+ * method is compared with.
  *
  * Query row i of batch element b stands at position p_i: without k_new the block's own tokens are the
  * cache's last, p_i = L_b - Tq + i; with k_new they are not in the cache yet, p_i = L_b + i, and
  * row i also attends to the new tokens 0..i. A cached token n < L_b is visible to row i iff
  *     n <= p_i  and  (n < sinks  or  n > p_i - window).
  * Otherwise the formulas of sts_dense_attn. Rows at negative positions (a padded batch: L_b < Tq) and rows that see
- * nothing give out = 0 and lse = -inf. Tq may be a whole prompt; window >= L_b is plain causal attention.
+ * nothing give out = 0 and lse = -inf. Tq may be a whole prompt; window >= L_b is plain causal attention. What a row does
+ * not see never reaches its result, NaN and infinities included, and pages of which no row sees a token are not looked up
+ * at addresses of their own (their entries may be anything); a row that sees a key with NaN is NaN.
  *
  * Supported: d in {64,128}; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; Tq >= 1, with k_new Tq <= 16 and window >= Tq;
- * window >= 1, sinks >= 0; kv strides as in sts_attn_params; page_size 1, 2, 4, 8, 16 or 32.
+ * Tq * Hq/Hkv < 2^31 - 65536; window >= 1, sinks >= 0; kv strides multiples of 8 elements, kv_stride_n at least d and at most 2^25;
+ * q, k, v, out, k_new and v_new 16-byte aligned; page_size 1, 2, 4, 8, 16 or 32.
  */
 typedef struct {
   int32_t B, Tq, Hq, Hkv, d, N;
