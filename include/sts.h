@@ -327,7 +327,7 @@ typedef struct {
  * sts_packed_load -- the same rows of the cache as the bf16 values they stand for (exact). Rows i >= lens[b] of the
  * outputs stay as they were; rows at positions outside [0, N) become 0.
  *
- * Supported: B <= 65535, T * Hkv < 2^31 - 65536; k and v 16-byte aligned.
+ * Supported: B <= 65535, T * Hkv <= 2^28 - 65536; k and v 16-byte aligned.
  */
 typedef struct {
   int32_t B, T, Hkv, d;
@@ -344,7 +344,7 @@ typedef struct {
  * A group of K that is NaN makes the rows that see its token NaN, one of V their 32 channels; the logarithm lse_out is then no finite
  * number. Tokens that no list names and tokens behind a sequence's end never reach a result, whatever lies there.
  *
- * Supported: Tq <= 16; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; q, out, k_new and v_new 16-byte aligned; scale finite.
+ * Supported: Tq <= 16; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; q, out, k_new and v_new 16-byte aligned; scale * log2(e) finite.
  */
 typedef struct {
   int32_t B, Tq, Hq, Hkv, d;
@@ -381,8 +381,8 @@ typedef struct {
  * at addresses of their own (their entries may be anything); a row that sees a key with NaN is NaN.
  *
  * Supported: d in {64,128}; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; Tq >= 1, with k_new Tq <= 16 and window >= Tq;
- * Tq * Hq/Hkv < 2^31 - 65536; window >= 1, sinks >= 0; kv strides multiples of 8 elements, kv_stride_n at least d and at most 2^25;
- * q, k, v, out, k_new and v_new 16-byte aligned; page_size 1, 2, 4, 8, 16 or 32.
+ * Tq * Hq/Hkv < 2^31 - 65536, fewer than 2^24 blocks of 128 rows of a KV head in a call with Tq > 16; window >= 1, sinks >= 0; kv strides multiples of 8 elements, kv_stride_n at least d and at most 2^25;
+ * q, k, v, out, k_new and v_new 16-byte aligned; scale * log2(e) finite; page_size 1, 2, 4, 8, 16 or 32.
  */
 typedef struct {
   int32_t B, Tq, Hq, Hkv, d, N;

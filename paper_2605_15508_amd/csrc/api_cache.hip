@@ -42,7 +42,8 @@ sts_status rows_call(const sts_packed_rows_params *p, bool store, hipStream_t s)
   if (!p || p->B < 0 || p->T < 0 || p->Hkv < 1) return STS_EINVAL;
   const sts_status v = validate_cache(p->cache, p->d);
   if (v != STS_OK) return v;
-  if (p->B > 65535 || (int64_t)p->T * p->Hkv > 0x7fffffffll - 65536) return STS_EUNSUPPORTED;
+  // (a grid's dimension holds 2^32 threads, of which a row takes up to 16)
+  if (p->B > 65535 || (int64_t)p->T * p->Hkv > (1 << 28) - 65536) return STS_EUNSUPPORTED;
   if (p->B == 0 || p->T == 0) return STS_OK;
   if (store && p->cache.N == 0) return STS_OK;       // no place for any row
   if (!p->k || !p->v || (p->cache.N > 0 && (!p->cache.codes || !p->cache.scales))) return STS_EINVAL;
@@ -117,7 +118,7 @@ sts_status validate_heads(int B, int Tq, int Hq, int Hkv, int d, int out_dtype, 
   if (d != 64 && d != 128) return STS_EUNSUPPORTED;
   if (Hq > STS_MAX_HEADS || Hq / Hkv > STS_MAX_GROUP) return STS_EUNSUPPORTED;
   if (out_dtype != STS_BF16 && out_dtype != STS_F32) return STS_EINVAL;
-  if (!isfinite(scale)) return STS_EINVAL;
+  if (!isfinite(scale * 1.44269504088896340736f)) return STS_EINVAL;         // (of which the kernels take the product with log2(e))
   if ((k_new == nullptr) != (v_new == nullptr)) return STS_EINVAL;
   if (!aligned(k_new, 16) || !aligned(v_new, 16)) return STS_EUNSUPPORTED;
   return STS_OK;
@@ -175,7 +176,7 @@ sts_status plan_window(const sts_window_params *p, CachePlan &pl, bool &prompt) 
     // Blocks of rows; where they leave compute units without work, several workgroups share a block's keys, four tiles each at least.
     const int G = p->Hq / p->Hkv;
     const int64_t blocks = ((int64_t)p->Tq * G + STS_WINDOW_ROWS - 1) / STS_WINDOW_ROWS * p->Hkv * p->B;
-    if ((int64_t)p->Tq * G > 0x7fffffffll - 65536 || blocks > 0x7fffffffll) return STS_EUNSUPPORTED;
+    if ((int64_t)p->Tq * G > 0x7fffffffll - 65536 || blocks >= 1 << 24) return STS_EUNSUPPORTED;      // (256 threads each: see above)
     const int64_t span = (int64_t)p->sinks + p->window + STS_WINDOW_ROWS / G + 1, keys = span < p->N ? span : p->N;
     const int64_t tiles = (keys + STS_WINDOW_KEYS - 1) / STS_WINDOW_KEYS;
     int64_t S = blocks > 0 ? 2 * sts_cu_count() / blocks : 1;

@@ -89,7 +89,7 @@ def test_caches_that_are_refused(lib, change, status):
 
 @pytest.mark.parametrize("change,status", [(dict(B=-1), EINVAL), (dict(T=-1), EINVAL), (dict(Hkv=0), EINVAL), (dict(k=None), EINVAL), (dict(v=None), EINVAL),
                                            (dict(k=FAR + 8), EUNSUPPORTED), (dict(v=FAR + 2), EUNSUPPORTED), (dict(B=65536), EUNSUPPORTED),
-                                           (dict(T=1 << 30, Hkv=8), EUNSUPPORTED)])
+                                           (dict(T=1 << 30, Hkv=8), EUNSUPPORTED), (dict(T=1 << 25, Hkv=8), EUNSUPPORTED)])
 def test_rows_that_are_refused(lib, change, status):
     for f in (lib.sts_packed_store, lib.sts_packed_load):
         assert f(ctypes.byref(rows(**change)), None) == status
@@ -105,7 +105,7 @@ def test_row_calls_without_rows_and_data(lib):
 
 
 HEADS = [(dict(B=-1), EINVAL), (dict(Tq=0), EINVAL), (dict(Hq=30), EINVAL), (dict(Hkv=0), EINVAL), (dict(Hq=512, Hkv=256), EUNSUPPORTED),
-         (dict(Hq=32, Hkv=1), EUNSUPPORTED), (dict(out_dtype=2), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL),
+         (dict(Hq=32, Hkv=1), EUNSUPPORTED), (dict(out_dtype=2), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(scale=-3e38), EINVAL),
          (dict(k_new=FAR), EINVAL), (dict(v_new=FAR), EINVAL), (dict(k_new=FAR + 8, v_new=FAR), EUNSUPPORTED), (dict(q=None), EINVAL), (dict(out=None), EINVAL),
          (dict(q=FAR + 8), EUNSUPPORTED), (dict(out=FAR + 4), EUNSUPPORTED), (dict(), EWORKSPACE), (dict(workspace=FAR, workspace_bytes=100), EWORKSPACE),
          (dict(workspace=FAR + 128, workspace_bytes=1 << 30), EWORKSPACE)]
@@ -140,7 +140,7 @@ def test_packed_attention_without_a_batch_or_a_map(lib):
                                                    (dict(block_table=FAR, page_size=16, num_pages=9, kv_stride_page=0), EINVAL),
                                                    (dict(block_table=FAR, page_size=16, num_pages=9, kv_stride_page=132, table_stride=256), EUNSUPPORTED),
                                                    (dict(block_table=FAR, page_size=16, num_pages=9, kv_stride_page=128, table_stride=255), EINVAL),
-                                                   (dict(Tq=1 << 30, Hq=64, Hkv=8), EUNSUPPORTED), (dict(Tq=64, workspace=FAR, workspace_bytes=64), EWORKSPACE)])
+                                                   (dict(Tq=1 << 30, Hq=64, Hkv=8), EUNSUPPORTED), (dict(Tq=4096, B=1 << 17), EUNSUPPORTED), (dict(Tq=64, workspace=FAR, workspace_bytes=64), EWORKSPACE)])
 def test_window_attention_that_is_refused(lib, change, status):
     assert lib.sts_window_attn(ctypes.byref(window(**change)), None) == status
 

@@ -339,3 +339,79 @@ def test_keys_that_are_no_numbers(N):
     q[0, 1, 3, 5] = float("inf")
     o = run(q, codes, scales, 0.1, out_dtype=torch.float32)[0].cpu()
     assert torch.isnan(o[0, 1, 3]).all() and torch.isfinite(o[0, 0]).all() and torch.isfinite(o[0, 1, :3]).all()
+
+
+def test_a_batch_over_one_cache_and_calls_without_results_of_their_own():
+    """One cache for the whole batch (a stride of 0), no lse asked for, no batch and no rows at all."""
+    g = gen(13)
+    codes, scales, _, k, v = packed_cache(1, 2, 150, 128, g)
+    c, s = (t.to(DEV).expand(3, -1, -1, -1, -1) for t in (codes, scales))
+    q = queries(3, 4, 8, 128, g)
+    got = sts.sts_packed_attn(q.to(DEV), c, s, 0.1, out_dtype=torch.float32)
+    check(got, attention(q, 0.1, all_tokens(k.expand(3, -1, -1, -1), v.expand(3, -1, -1, -1), 8, 4), q_halves=True))
+    o, none = sts.sts_packed_attn(q.to(DEV), c, s, 0.1, out_dtype=torch.float32, want_lse=False)
+    assert none is None and torch.equal(o, got[0])
+    o, l = sts.sts_packed_attn(q[:0].to(DEV), c[:0], s[:0], 0.1)
+    assert o.shape == (0, 4, 8, 128) and l.shape == (0, 8, 4)
+    a, b = sts.sts_packed_load(c, s, 0)
+    assert a.shape == b.shape == (3, 0, 2, 128)
+    sts.sts_packed_store(a, b, codes.to(DEV).expand(3, -1, -1, -1, -1), s)
+    a, b = sts.sts_packed_load(c[:0], s[:0], 7)
+    assert a.shape == (0, 7, 2, 128)
+
+
+def test_shapes_and_types_that_the_binding_refuses():
+    g = gen(14)
+    codes, scales, _, _, _ = packed_cache(1, 2, 40, 128, g)
+    codes, scales = codes.to(DEV), scales.to(DEV)
+    q = queries(1, 2, 4, 128, g).to(DEV)
+    rows = torch.zeros(1, 3, 2, 128, dtype=torch.bfloat16, device=DEV)
+    one = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for call in (lambda: sts.sts_packed_attn(q.float(), codes, scales, 0.1), lambda: sts.sts_packed_attn(q, codes.view(torch.int8), scales, 0.1),
+                 lambda: sts.sts_packed_attn(q, codes, scales[:, :, :39], 0.1), lambda: sts.sts_packed_attn(q[..., :64].contiguous(), codes, scales, 0.1),
+                 lambda: sts.sts_packed_attn(q, codes, scales, 0.1, N=41), lambda: sts.sts_packed_attn(q, codes, scales, 0.1, counts=one),
+                 lambda: sts.sts_packed_attn(q, codes, scales, 0.1, seq_lens=one.long()), lambda: sts.sts_packed_attn(q, codes, scales, 0.1, k_new=rows),
+                 lambda: sts.sts_packed_store(rows.half(), rows, codes, scales), lambda: sts.sts_packed_store(rows[:, :, :1], rows, codes, scales),
+                 lambda: sts.sts_packed_store(rows, rows, codes, scales, pos=one.cpu()), lambda: sts.sts_packed_load(codes, scales, 3, out=(rows, rows[:, :2])),
+                 lambda: sts.sts_packed_load(codes, scales, 3, block_table=one.view(1, 1)), lambda: sts.sts_packed_load(codes.transpose(3, 4), scales, 3)):
+        with pytest.raises(AssertionError):
+            call()
+    for call in (lambda: sts.sts_packed_store(rows.cpu(), rows.cpu(), codes.cpu(), scales.cpu()), lambda: sts.sts_packed_attn(q, codes, scales, float("nan")),
+                 lambda: sts.sts_packed_attn(torch.zeros(1, 17, 4, 128, dtype=torch.bfloat16, device=DEV), codes, scales, 0.1),
+                 lambda: sts.sts_packed_attn(q, codes, scales, 0.1, workspace=torch.empty(0, dtype=torch.uint8, device=DEV)),
+                 lambda: sts.sts_packed_store(rows, rows, codes, scales, page_size=3)):
+        with pytest.raises(sts.StsError):
+            call()
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0])
+def test_own_tokens_at_scales_of_both_signs(scale):
+    g = gen(15)
+    codes, scales, _, k, v = packed_cache(2, 2, 90, 128, g)
+    q = queries(2, 5, 8, 128, g)
+    kn, vn = (torch.randn(2, 5, 2, 128, generator=g).to(torch.bfloat16) for _ in range(2))
+    check(run(q, codes, scales, scale, k_new=kn, v_new=vn, out_dtype=torch.float32), attention(q, scale, all_tokens(k, v, 8, 5), kn, vn, q_halves=True))
+
+
+@pytest.mark.parametrize("Tq,Hq,Hkv,listed_heads", [(2, 256, 256, False), (16, 256, 16, False), (1, 256, 32, True), (3, 240, 16, True)])
+def test_many_heads(Tq, Hq, Hkv, listed_heads):
+    g = gen(16)
+    codes, scales, _, k, v = packed_cache(1, Hkv, 70, 64, g)
+    q = queries(1, Tq, Hq, 64, g)
+    idx = lists(1, Hq, 70, 40, g) if listed_heads else None
+    ref = attention(q, 0.1, listed(k, v, Hq, Tq, idx, None) if listed_heads else all_tokens(k, v, Hq, Tq), q_halves=True)
+    check(run(q, codes, scales, 0.1, indices=idx, out_dtype=torch.float32), ref)
+
+
+def test_large_batches():
+    """More sequences than a grid's last dimension has, of one token each: the output is its value."""
+    B, d = 40001, 64
+    g = gen(17)
+    rows = torch.randn(2, B, 1, 1, d, generator=g).to(torch.bfloat16).to(DEV)
+    codes, scales = torch.zeros(B, 1, 1, 2, d // 2, dtype=torch.uint8, device=DEV), torch.zeros(B, 1, 1, 2, d // 32, dtype=torch.uint8, device=DEV)
+    sts.sts_packed_store(rows[0], rows[1], codes, scales)
+    back = sts.sts_packed_load(codes, scales, 1)
+    q = torch.randn(B, 1, 1, d, generator=g).to(torch.bfloat16).to(DEV)
+    for kw in ({}, {"indices": torch.zeros(B, 1, 1, dtype=torch.int32, device=DEV)}):
+        assert torch.equal(sts.sts_packed_attn(q, codes, scales, 0.1, **kw)[0], back[1])
+    assert torch.equal(sts.sts_packed_attn(q, codes, scales, 0.0, k_new=rows[0], v_new=back[1])[0], back[1])

@@ -322,3 +322,49 @@ def test_pages_that_lie_far_apart(Tq, apart):
     finally:
         del far, pool
         torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("Tq", [4, 50])
+def test_a_batch_over_one_cache_and_calls_without_results_of_their_own(Tq):
+    """One cache for the whole batch (a stride of 0), no lse asked for, no batch at all; and what the measurement aid counts."""
+    q, k, v, _, _ = data(3, Tq, 4, 2, 200, 128, 16)
+    k, v = (t[:1].expand(3, -1, -1, -1) for t in (k, v))
+    ref = reference(q, k, v, 0.1, 60, 3)
+    kd, vd = (t[:1].to(DEV).expand(3, -1, -1, -1) for t in (k, v))
+    got = sts.sts_window_attn(q.to(DEV), kd, vd, 0.1, 60, sinks=3, out_dtype=torch.float32)
+    check(got, ref)
+    sts.prof_enable(True)
+    sts.prof_reset()
+    try:
+        o, none = sts.sts_window_attn(q.to(DEV), kd, vd, 0.1, 60, sinks=3, out_dtype=torch.float32, want_lse=False)
+        assert sts.prof_read()["window"][0] == 1
+    finally:
+        sts.prof_enable(False)
+        sts.prof_reset()
+    assert none is None and torch.equal(o, got[0])
+    o, l = sts.sts_window_attn(q[:0].to(DEV), kd[:0], vd[:0], 0.1, 60, sinks=3)
+    assert o.shape == (0, Tq, 4, 128) and l.shape == (0, 4, Tq)
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0])
+def test_own_tokens_at_scales_of_both_signs(scale):
+    q, k, v, kn, vn = data(2, 5, 4, 2, 90, 128, 17, tail=True)
+    check(run(q, k, v, scale, 40, 2, k_new=kn, v_new=vn, out_dtype=torch.float32), reference(q, k, v, scale, 40, 2, None, kn, vn))
+
+
+@pytest.mark.parametrize("Tq,Hq,Hkv", [(2, 256, 256), (16, 256, 16), (1, 256, 32), (20, 256, 256), (30, 240, 16)])
+def test_many_heads(Tq, Hq, Hkv):
+    q, k, v, _, _ = data(1, Tq, Hq, Hkv, 70, 64, 18)
+    check(run(q, k, v, 0.1, 33, 2, out_dtype=torch.float32), reference(q, k, v, 0.1, 33, 2))
+
+
+@pytest.mark.parametrize("Tq", [1, 17])
+def test_large_batches(Tq):
+    """More sequences than a grid's last dimension has; the first row that sees a key sees the first alone."""
+    B, d = 40001, 64
+    q, k, v = (torch.randn(*s, generator=gen(19)).to(torch.bfloat16).to(DEV) for s in ((B, Tq, 1, d), (B, 1, 1, d), (B, 1, 1, d)))
+    o, l = sts.sts_window_attn(q, k, v, 0.1, 5)
+    assert torch.equal(o[:, -1], v[:, :, 0]) and (o[:, :-1] == 0).all()
+    s = 0.1 * (q[:, -1, 0].double() * k[:, 0, 0].double()).sum(-1)
+    # one key: lse is its score, 64 products in fp32 of |q||k| under 10 each at 0.1, and two conversions between base 2 and e
+    assert ((l[:, 0, -1].double() - s).abs() <= 64 * 2.0 ** -24 * 64 + 2.0 ** -22 * s.abs()).all() and torch.isneginf(l[:, 0, :-1]).all()
