@@ -81,14 +81,15 @@ struct CachePlan {
 
 // Units of a short block and how many parts their tiles are cut into, `tiles` of them at most per unit: so many that `resident` workgroups run
 // at once, with two tiles for each of their four waves at least, or one (one_each) as long as every workgroup has a compute unit
-// of its own. Lists of up to 16 tiles stay whole, as for the bf16 cache: a second launch takes as long as they do.
-sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, const int32_t *head_map, bool whole, int64_t tiles, bool one_each,
+// of its own. Lists of up to 16 tiles stay whole, as for the bf16 cache: a second launch takes as long as they do. With own tokens (tail) there
+// is one anyway.
+sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, const int32_t *head_map, bool whole_groups, int64_t tiles, bool one_each, bool tail,
                        int64_t (*resident)(int d), CachePlan &pl) {
   int max_heads = most_rows / Tq;
   if (max_heads < 1) max_heads = 1;
   if (max_heads > STS_MAX_GROUP) max_heads = STS_MAX_GROUP;
   int rows = 0;
-  const int nu = sts_group_units(Hq, Hkv, Tq, max_heads, head_map, whole, pl.units, rows);
+  const int nu = sts_group_units(Hq, Hkv, Tq, max_heads, head_map, whole_groups, pl.units, rows);
   if (nu < 0) return STS_EUNSUPPORTED;
   pl.num_units = nu;
   pl.nq = rows <= 16 ? 1 : 2;
@@ -97,8 +98,9 @@ sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, con
     const int64_t most = (tiles + wave_tiles * STS_WG_WAVES - 1) / (wave_tiles * STS_WG_WAVES), S = total > 0 ? workgroups / total : 1;
     return S < most ? S : most;
   };
-  int64_t S = tiles <= 16 ? 1 : parts_of(resident(d), 2);
-  if (one_each && tiles > 16) {
+  const bool whole = tiles <= 16 && !tail;
+  int64_t S = whole ? 1 : parts_of(resident(d), 2);
+  if (one_each && !whole) {
     const int64_t more = parts_of(sts_cu_count(), 1);
     if (more > S) S = more;
   }
@@ -149,7 +151,7 @@ sts_status plan_packed(const sts_packed_attn_params *p, CachePlan &pl) {
     return STS_EINVAL;
   }
   const int64_t len = lists ? (int64_t)p->kmax * page : p->cache.N;
-  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, p->head_map, !lists, (len + STS_TILE_KEYS - 1) / STS_TILE_KEYS, false, packed_resident, pl);
+  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, p->head_map, !lists, (len + STS_TILE_KEYS - 1) / STS_TILE_KEYS, false, p->k_new != nullptr, packed_resident, pl);
 }
 
 int64_t window_resident(int d) { return (int64_t)sts_cu_count() * (d == 128 ? 1 : 2); }
@@ -194,7 +196,7 @@ sts_status plan_window(const sts_window_params *p, CachePlan &pl, bool &prompt) 
   // One for a wave: 5 rows, window 1024, pages 13.2 us, with two 15.3 (over 4 bits 4096 tokens 9.2 us, with two 8.6).
   const int64_t all = ((int64_t)p->N + STS_TILE_KEYS - 1) / STS_TILE_KEYS;
   const int64_t some = ((int64_t)p->sinks + STS_TILE_KEYS - 1) / STS_TILE_KEYS + ((int64_t)p->window + p->Tq + STS_TILE_KEYS - 1) / STS_TILE_KEYS + 1;
-  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, nullptr, true, all < some ? all : some, true, window_resident, pl);
+  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, nullptr, true, all < some ? all : some, true, p->k_new != nullptr, window_resident, pl);
 }
 
 sts_status launch_short(CacheAttnArgs &c, const CachePlan &pl, int d, bool four_bit, bool far, int kind, void *ws, size_t ws_bytes, hipStream_t s) {
