@@ -83,8 +83,8 @@ struct CachePlan {
 // at once, with two tiles for each of their four waves at least, or one (one_each) as long as every workgroup has a compute unit
 // of its own. Lists of up to 16 tiles stay whole, as for the bf16 cache: a second launch takes as long as they do. With own tokens (tail) there
 // is one anyway.
-sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, const int32_t *head_map, bool whole_groups, int64_t tiles, bool one_each, bool tail,
-                       int64_t (*resident)(int d), CachePlan &pl) {
+sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, const int32_t *head_map, bool whole_groups, int64_t tiles, int row_bytes,
+                       bool one_each, bool tail, int64_t (*resident)(int d), CachePlan &pl) {
   int max_heads = most_rows / Tq;
   if (max_heads < 1) max_heads = 1;
   if (max_heads > STS_MAX_GROUP) max_heads = STS_MAX_GROUP;
@@ -104,8 +104,18 @@ sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, con
     const int64_t more = parts_of(sts_cu_count(), 1);
     if (more > S) S = more;
   }
-  if (S > 256) S = 256;
   if (S < 1) S = 1;
+  // Between one and two units for each compute unit some would have two to work on and most one. Parts even that out, where a unit is a
+  // megabyte of the cache or more: 33 sequences, window 4096 138 us whole, 118 in parts; 16000 tokens of 4 bits 146 and 124; 4000 of them 42 and 43.
+  const int64_t cus = sts_cu_count();
+  if (total > cus && total < 2 * cus && tiles * STS_TILE_KEYS * row_bytes >= 1 << 20) {
+    int64_t rounds = 2;                    // with S parts; the shortest is that of the least rounds / S
+    for (int64_t s = 2; s <= 4; ++s) {
+      const int64_t r = (total * s + cus - 1) / cus;
+      if (r * S < rounds * s) rounds = r, S = s;
+    }
+  }
+  if (S > 256) S = 256;
   pl.num_splits = (int)S;
   const size_t parts = (size_t)total * (size_t)S;
   if (parts > 0x7fffffffull) return STS_EUNSUPPORTED;
@@ -151,7 +161,8 @@ sts_status plan_packed(const sts_packed_attn_params *p, CachePlan &pl) {
     return STS_EINVAL;
   }
   const int64_t len = lists ? (int64_t)p->kmax * page : p->cache.N;
-  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, p->head_map, !lists, (len + STS_TILE_KEYS - 1) / STS_TILE_KEYS, false, p->k_new != nullptr, packed_resident, pl);
+  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, p->head_map, !lists, (len + STS_TILE_KEYS - 1) / STS_TILE_KEYS, p->d + p->d / 16, false, p->k_new != nullptr,
+                     packed_resident, pl);
 }
 
 int64_t window_resident(int d) { return (int64_t)sts_cu_count() * (d == 128 ? 1 : 2); }
@@ -196,7 +207,7 @@ sts_status plan_window(const sts_window_params *p, CachePlan &pl, bool &prompt) 
   // One for a wave: 5 rows, window 1024, pages 13.2 us, with two 15.3 (over 4 bits 4096 tokens 9.2 us, with two 8.6).
   const int64_t all = ((int64_t)p->N + STS_TILE_KEYS - 1) / STS_TILE_KEYS;
   const int64_t some = ((int64_t)p->sinks + STS_TILE_KEYS - 1) / STS_TILE_KEYS + ((int64_t)p->window + p->Tq + STS_TILE_KEYS - 1) / STS_TILE_KEYS + 1;
-  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, nullptr, true, all < some ? all : some, true, p->k_new != nullptr, window_resident, pl);
+  return plan_splits(p->B, p->Tq, p->Hq, p->Hkv, p->d, 32, nullptr, true, all < some ? all : some, 4 * p->d, true, p->k_new != nullptr, window_resident, pl);
 }
 
 sts_status launch_short(CacheAttnArgs &c, const CachePlan &pl, int d, bool four_bit, bool far, int kind, void *ws, size_t ws_bytes, hipStream_t s) {

@@ -27,7 +27,8 @@
 // head are two units, each of which converts V (123 MB in 55 us; units of 64 rows do not fit the registers). Lists: rows of
 // 136 bytes are a line of codes and a piece of one of scales (121 MB in 29 us). The bf16 window: memory (16 sequences, window 4096: 269 MB in
 // 45 us, 6.0 TB/s). Few keys: the chain length -> page -> row -> product -> merge, 6 to 9 us, and 3.5 to 5 of the combine kernel.
-// Three tiles of 4 bits are on the way in each wave, two of bf16, which take all registers; two workgroups on a compute unit (4 bits), one (bf16).
+// Three tiles of 4 bits are on the way in each wave, of bf16 two at head size 64 and one at 128: so two workgroups fit a compute unit, one where there
+// are few (with two tiles on the way one fits: 40 sequences of 5 rows, window 600 53 us, so 43; 16 of one row, window 4096 the same).
 #include <float.h>
 
 #include "cache.h"
@@ -74,7 +75,7 @@ template <> struct Share<64, false> { typedef u32x4 k; typedef u32x2 v; };
 // bits 0 .. n - 1 of a word, none for n <= 0
 __device__ __forceinline__ uint32_t first_keys(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
-template <int D, int NQ, bool FOUR> constexpr int tiles_ahead() { return FOUR ? 3 : 2; }
+template <int D, bool FOUR> constexpr int tiles_ahead() { return FOUR ? 3 : D == 128 ? 1 : 2; }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
@@ -133,11 +134,11 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale, int byt
 // FOUR: a 4-bit cache without a window, else a bf16 cache with one. GATHER: the rows come from a list or a page
 // table, at offsets of 64 bits (FAR) or 32.
 template <int D, int NQ, bool FOUR, bool GATHER, bool FAR>
-__global__ void __launch_bounds__(64 * STS_WG_WAVES, !FOUR && D == 128 ? 1 : 2) cache_attn_kernel(const CacheAttnArgs C) {
+__global__ void __launch_bounds__(64 * STS_WG_WAVES, 2) cache_attn_kernel(const CacheAttnArgs C) {
   typedef typename Share<D, FOUR>::k k_t;
   typedef typename Share<D, FOUR>::v v_t;
   typedef typename std::conditional<FAR, uint64_t, uint32_t>::type off_t;
-  constexpr int W = STS_WG_WAVES, TK = STS_TILE_KEYS, PF = tiles_ahead<D, NQ, FOUR>();
+  constexpr int W = STS_WG_WAVES, TK = STS_TILE_KEYS, PF = tiles_ahead<D, FOUR>();
   constexpr int NT = D / 16, KK = D / 32;
   constexpr int KL = FOUR ? 1 : KK;              // loads of K per lane and half tile
   constexpr int QR = FOUR ? D / 32 : KK;         // quads of registers of Q per lane and query tile: bf16, or halves in e4m3
