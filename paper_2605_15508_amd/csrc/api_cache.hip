@@ -81,8 +81,9 @@ struct CachePlan {
 
 // Units of a short block and how many parts their tiles are cut into, `tiles` of them at most per unit: so many that `resident` workgroups run
 // at once, with two tiles for each of their four waves at least, or one (one_each) as long as every workgroup has a compute unit
-// of its own. Lists of up to 16 tiles stay whole, as for the bf16 cache: a second launch takes as long as they do. With own tokens (tail) there
-// is one anyway.
+// of its own. Lists of up to 16 tiles stay whole, as for the bf16 cache: a second launch takes as long as they do. Not so with own tokens (tail)
+// and two tiles of query rows, which a whole unit's workgroup takes in one after the other, as long as there are few units (500 tokens of 4 bits,
+// 5 rows, one sequence: 11.1 us in parts, 12.4 whole; 64 heads of 16 rows, 4 sequences: 20.3 and 18.1).
 sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, const int32_t *head_map, bool whole_groups, int64_t tiles, int row_bytes,
                        bool one_each, bool tail, int64_t (*resident)(int d), CachePlan &pl) {
   int max_heads = most_rows / Tq;
@@ -98,7 +99,7 @@ sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, con
     const int64_t most = (tiles + wave_tiles * STS_WG_WAVES - 1) / (wave_tiles * STS_WG_WAVES), S = total > 0 ? workgroups / total : 1;
     return S < most ? S : most;
   };
-  const bool whole = tiles <= 16 && !tail;
+  const bool whole = tiles <= 16 && !(tail && pl.nq == 2 && 4 * total <= sts_cu_count());
   int64_t S = whole ? 1 : parts_of(resident(d), 2);
   if (one_each && !whole) {
     const int64_t more = parts_of(sts_cu_count(), 1);
@@ -221,7 +222,7 @@ sts_status launch_short(CacheAttnArgs &c, const CachePlan &pl, int d, bool four_
   a.scale_log2 = a.scale * 1.44269504088896340736f;
   a.part_o = static_cast<float *>(ws);
   a.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + pl.part_o_bytes);
-  a.direct = pl.num_splits == 1 && !a.k_new;
+  a.direct = pl.num_splits == 1;
   hipError_t rc = sts_run_kernel(kind, s, [&] { return launch_cache_attn(c, d, pl.nq, four_bit, far, s); });
   if (rc == hipSuccess && !a.direct) rc = sts_run_kernel(STS_K_ATTN_COMBINE, s, [&] { return launch_attn_combine(a, d, pl.nq, s); });
   return rc == hipSuccess ? STS_OK : STS_EHIP;

@@ -2,7 +2,7 @@
 // (sts_packed_attn: all tokens, or index lists), or bf16 with a sliding window and sinks (sts_window_attn).
 //
 // Units, splits and partials are those of the bf16 kernels (attn.hip), whose combine kernel merges the splits and appends
-// the block's own tokens. One workgroup of four waves per (batch, unit, split); waves take alternating tiles of 32 keys
+// the block's own tokens. A workgroup that has a unit whole appends them itself (64 sequences of 1500 tokens, 5 rows: 34 us, with the combine kernel 56). One workgroup of four waves per (batch, unit, split); waves take alternating tiles of 32 keys
 // and keep an online softmax of their own, with maximum, sum and accumulators in fp32.
 //
 // Tiles in the transposed orientation, S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x32_bf16, lane (a, b) =
@@ -63,6 +63,17 @@ __device__ __forceinline__ float max_over_groups(float x) {
   const uint32_t v = __builtin_bit_cast(uint32_t, y);
   const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   return larger(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
+}
+
+// sum over the 16 lanes of a row, the same in each of them
+__device__ __forceinline__ float row_sum(float x) {
+  auto turned = [](float y, auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, y), decltype(ctrl)::value, 0xf, 0xf, false));
+  };
+  x += turned(x, std::integral_constant<int, 0x128>());          // row_ror: 8, 4, 2, 1
+  x += turned(x, std::integral_constant<int, 0x124>());
+  x += turned(x, std::integral_constant<int, 0x122>());
+  return x + turned(x, std::integral_constant<int, 0x121>());
 }
 
 // a lane's share of a row: K's quarter and V's D / 16 channels
@@ -681,7 +692,13 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, 2) cache_attn_kernel(const 
         *reinterpret_cast<f32x4 *>(orow + NT * (4 * a + r) + 4 * v4) = o;
       }
     __syncthreads();
-    constexpr int SEGF = D / 16;
+    constexpr int SEGF = D / 16, OWN = 4;
+    typedef typename std::conditional<D == 128, u32x4, u32x2>::type seg_t;
+    auto widen = [](const uint16_t *from, float (&to)[SEGF]) {
+      const seg_t w = *reinterpret_cast<const seg_t *>(from);
+#pragma unroll
+      for (int e = 0; e < SEGF; ++e) to[e] = __builtin_bit_cast(float, e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+    };
     const int row = threadIdx.x >> 4, seg = threadIdx.x & 15, r = nq * 16 + row;
     f32x4 sum[SEGF / 4];
 #pragma unroll
@@ -703,8 +720,40 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, 2) cache_attn_kernel(const 
       if (seg == 0) *reinterpret_cast<f32x2 *>(pml + r * 2) = f32x2{m, L};
     } else if (r < rows_valid) {
       const int hsel = (r * C.tq_inv) >> 16, tq = r - hsel * A.Tq, head = g * A.G + nth_member(mask, hsel);
-      const float inv = L == 0.f ? 0.f : 1.f / L;
       const size_t at = (((size_t)bt * A.Tq + tq) * A.Hq + head) * D + seg * SEGF;
+      float m_all = m;
+      if (A.k_new) {
+        // The block's own tokens 0 .. tq (all of them, if not causal), in order, each like one more part; the 16 threads of a row have
+        // D / 16 channels each.
+        const int mine = A.causal ? tq + 1 : A.Tq;
+        float q[SEGF], k[SEGF], v[SEGF];
+        widen(A.q + at, q);
+        for (int j0 = 0; j0 < A.Tq; j0 += OWN) {
+          seg_t kw[OWN], vw[OWN];
+#pragma unroll
+          for (int j = 0; j < OWN; ++j) {
+            const size_t from = (((size_t)bt * A.Tq + min(j0 + j, A.Tq - 1)) * A.Hkv + g) * D + seg * SEGF;
+            kw[j] = *reinterpret_cast<const seg_t *>(A.k_new + from);
+            vw[j] = *reinterpret_cast<const seg_t *>(A.v_new + from);
+          }
+#pragma unroll
+          for (int j = 0; j < OWN; ++j) {
+            widen(reinterpret_cast<const uint16_t *>(&kw[j]), k);
+            widen(reinterpret_cast<const uint16_t *>(&vw[j]), v);
+            float dot = 0.f;
+#pragma unroll
+            for (int e = 0; e < SEGF; ++e) dot += q[e] * k[e];
+            const float s = row_sum(dot) * A.scale_log2;
+            if (j0 + j >= mine) continue;
+            const float m_new = fmaxf(m_all, s), fo = __builtin_amdgcn_exp2f(m_all - m_new), fn = __builtin_amdgcn_exp2f(s - m_new);
+            L = L * fo + fn;
+#pragma unroll
+            for (int e = 0; e < SEGF; ++e) sum[e >> 2][e & 3] = sum[e >> 2][e & 3] * fo + v[e] * fn;
+            m_all = m_new;
+          }
+        }
+      }
+      const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
       for (int e = 0; e < SEGF / 4; ++e) {
         const f32x4 x = sum[e] * inv;
@@ -717,7 +766,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, 2) cache_attn_kernel(const 
         }
       }
       if (A.lse_out && seg == 0)
-        A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + tq] = L == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f;
+        A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + tq] = L == 0.f ? -INFINITY : (m_all + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f;
     }
     __syncthreads();
   }

@@ -39,7 +39,7 @@ hipError_t launch_packed_load(const PackedRowsArgs &a, hipStream_t) {
 }
 static void check_parts(const AttnArgs &a, int d, int nq) {
   if (a.num_splits < 1 || a.num_splits > 256 || a.num_units < 1 || a.num_units > STS_MAX_HEADS) fail("split: grid");
-  if (a.direct != (a.num_splits == 1 && !a.k_new)) fail("split: where results go");
+  if (a.direct != (a.num_splits == 1)) fail("split: where results go");
   const size_t parts = (size_t)a.B * a.num_units * a.num_splits;
   in_ws(a.part_o, parts * nq * 16 * d * 4, "split: part_o");
   in_ws(a.part_ml, parts * nq * 16 * 2 * 4, "split: part_ml");

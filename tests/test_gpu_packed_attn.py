@@ -415,3 +415,34 @@ def test_large_batches():
     for kw in ({}, {"indices": torch.zeros(B, 1, 1, dtype=torch.int32, device=DEV)}):
         assert torch.equal(sts.sts_packed_attn(q, codes, scales, 0.1, **kw)[0], back[1])
     assert torch.equal(sts.sts_packed_attn(q, codes, scales, 0.0, k_new=rows[0], v_new=back[1])[0], back[1])
+
+
+@pytest.mark.parametrize("Tq,causal", [(1, True), (4, False), (5, True), (9, False), (16, True)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_own_tokens_after_short_lists(Tq, causal, d):
+    """Lists that one workgroup has whole, with own tokens: one launch, no other kernel merges anything. Own tokens that a row does not see
+    may be anything."""
+    g = gen(18 + Tq)
+    codes, scales, _, k, v = packed_cache(3, 2, 300, d, g)
+    q = queries(3, Tq, 8, d, g)
+    idx = lists(3, 8, 300, 70, g)
+    cnt = torch.randint(0, 71, (3, 8), generator=g, dtype=torch.int32)
+    cnt[0] = 0
+    kn, vn = (torch.randn(3, Tq, 2, d, generator=g).to(torch.bfloat16) for _ in range(2))
+    ref = attention(q, 0.1, listed(k, v, 8, Tq, idx, cnt), kn, vn, causal, q_halves=True)
+    got = run(q, codes, scales, 0.1, indices=idx, counts=cnt, k_new=kn, v_new=vn, causal=causal, out_dtype=torch.float32)
+    check(got, ref)
+    if causal and Tq > 1:
+        kn[:, -1], vn[:, -1] = float("nan"), float("inf")
+        bad = run(q, codes, scales, 0.1, indices=idx, counts=cnt, k_new=kn, v_new=vn, out_dtype=torch.float32)
+        assert torch.equal(bad[0][:, :-1], got[0][:, :-1]) and torch.equal(bad[1][..., :-1], got[1][..., :-1])
+        assert torch.isnan(bad[0][:, -1]).all()
+    sts.prof_enable(True)
+    sts.prof_reset()
+    try:
+        run(q, codes, scales, 0.1, indices=idx, counts=cnt, k_new=kn, v_new=vn, causal=causal)
+        counts = sts.prof_read()
+        assert counts["packed_attn"][0] == 1 and counts["attn_combine"][0] == 0
+    finally:
+        sts.prof_enable(False)
+        sts.prof_reset()
