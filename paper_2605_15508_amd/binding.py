@@ -300,6 +300,15 @@ def sts_select(scores, head_map, k: int, lse=None, seq_lens=None, kind: int = ST
     return indices, counts, agg
 
 
+def _batch_stride(t) -> int:
+    """Elements from one batch element's part of a list to the next's, 0 where there is one alone. The library takes 0 for "not
+    given": a list that the whole batch shares by a stride of 0 would be read behind its end."""
+    if t.shape[0] <= 1:
+        return 0
+    assert t.stride(0) > 0 or t.numel() == 0, "one list for the whole batch (a stride of 0): make it contiguous()"
+    return t.stride(0)
+
+
 def _attn_params(q, k, v, scale, indices, counts, head_map, seq_lens, out, lse_out, logits_out,
                  page_size=1, block_table=None, N=None, k_new=None, v_new=None, causal=True, row_mask=None):
     import torch
@@ -328,11 +337,11 @@ def _attn_params(q, k, v, scale, indices, counts, head_map, seq_lens, out, lse_o
         assert indices.is_cuda and indices.dtype == torch.int32 and indices.shape[:2] == (B, Hq)
         kmax = indices.shape[2]
         assert kmax == 0 or (indices.stride(2) == 1 and (Hq == 1 or indices.stride(1) == kmax))
-        isb = indices.stride(0) if B > 1 else 0
+        isb = _batch_stride(indices)
     if counts is not None:
         assert counts.is_cuda and counts.dtype == torch.int32 and counts.shape == (B, Hq)
         assert Hq == 1 or counts.stride(1) == 1
-        csb = counts.stride(0) if B > 1 else 0
+        csb = _batch_stride(counts)
     if seq_lens is not None:
         assert seq_lens.is_cuda and seq_lens.dtype == torch.int32 and seq_lens.shape == (B,)
     hm = _host_i32(head_map) if head_map is not None else None
@@ -415,7 +424,7 @@ def _run_attn(sparse: bool, q, k, v, scale, indices=None, counts=None, head_map=
 def sts_sparse_attn(q, k, v, indices, scale, counts=None, head_map=None, out=None, out_dtype=None,
                     want_lse=True, workspace=None, lse_out=None, page_size=1, block_table=None, N=None,
                     k_new=None, v_new=None, causal=True, row_mask=None, prepare=False):
-    """Attention over the gathered rows indices[b,t,:counts[b,t]] of the full cache.
+    """Attention over the gathered rows indices[b,t,:counts[b,t]] of the full cache (a list of its own for every batch element).
     q [B,Tq,Hq,d] bf16, k/v [B,Hkv,N,d] bf16 (strided ok) -> (out [B,Tq,Hq,d], lse [B,Hq,Tq]).
     row_mask (16-bit words shaped like indices): query row i attends only to entries with bit i.
     prepare=True returns a PreparedCall instead of launching."""
@@ -635,7 +644,7 @@ def sts_packed_attn(q, codes, scales, scale, indices=None, counts=None, head_map
                     want_lse=True, workspace=None, lse_out=None, page_size=1, block_table=None, N=None, k_new=None, v_new=None,
                     causal=True, prepare=False):
     """Attention over a 4-bit cache (see sts_packed_store): all tokens, or the rows that indices [B,Hq,kmax] name, as in
-    sts_dense_attn and sts_sparse_attn -> (out [B,Tq,Hq,d], lse [B,Hq,Tq]). prepare=True returns a PreparedCall."""
+    sts_dense_attn and sts_sparse_attn (a list of its own for every batch element) -> (out [B,Tq,Hq,d], lse [B,Hq,Tq]). prepare=True returns a PreparedCall."""
     import torch
 
     lib = load_library()
@@ -650,7 +659,7 @@ def sts_packed_attn(q, codes, scales, scale, indices=None, counts=None, head_map
         assert indices.device == q.device and indices.dtype == torch.int32 and indices.dim() == 3 and tuple(indices.shape[:2]) == (B, Hq)
         kmax = indices.shape[2]
         assert kmax == 0 or (indices.stride(2) == 1 and (Hq == 1 or indices.stride(1) == kmax))
-        isb = indices.stride(0) if B > 1 else 0
+        isb = _batch_stride(indices)
         if kmax == 0:           # empty lists: a tensor without elements has no address, and none is read
             indices, isb = out, 0
     else:
@@ -658,7 +667,7 @@ def sts_packed_attn(q, codes, scales, scale, indices=None, counts=None, head_map
     if counts is not None:
         assert counts.device == q.device and counts.dtype == torch.int32 and tuple(counts.shape) == (B, Hq)
         assert Hq == 1 or counts.stride(1) == 1
-        csb = counts.stride(0) if B > 1 else 0
+        csb = _batch_stride(counts)
     hm = _host_i32(head_map) if head_map is not None else None
     assert hm is None or len(hm) == Hq
     p = PackedAttnParams(B=B, Tq=Tq, Hq=Hq, Hkv=Hkv, d=d, q=_ptr(q), cache=cache, indices=_ptr(indices), counts=_ptr(counts), kmax=kmax,
