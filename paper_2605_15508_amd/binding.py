@@ -282,7 +282,7 @@ def sts_select(scores, head_map, k: int, lse=None, seq_lens=None, kind: int = ST
     if lse is not None:
         assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (B, Hd, Tq)
     if seq_lens is not None:
-        assert seq_lens.is_cuda and seq_lens.dtype == torch.int32 and seq_lens.shape == (B,)
+        assert seq_lens.is_cuda and seq_lens.dtype == torch.int32 and seq_lens.shape == (B,) and seq_lens.is_contiguous()
     p = SelectParams(B=B, Hd=Hd, Tq=Tq, N=N, Hq=Hq, k=int(k), scores=_ptr(scores), lse=_ptr(lse),
                      head_map=ctypes.cast(hm, ctypes.c_void_p), seq_lens=_ptr(seq_lens),
                      indices=_ptr(indices), counts=_ptr(counts), agg_out=_ptr(agg), kind=kind,
@@ -343,7 +343,7 @@ def _attn_params(q, k, v, scale, indices, counts, head_map, seq_lens, out, lse_o
         assert Hq == 1 or counts.stride(1) == 1
         csb = _batch_stride(counts)
     if seq_lens is not None:
-        assert seq_lens.is_cuda and seq_lens.dtype == torch.int32 and seq_lens.shape == (B,)
+        assert seq_lens.is_cuda and seq_lens.dtype == torch.int32 and seq_lens.shape == (B,) and seq_lens.is_contiguous()
     hm = _host_i32(head_map) if head_map is not None else None
     out_dtype = STS_BF16 if out.dtype == torch.bfloat16 else STS_F32
     if k_new is not None:

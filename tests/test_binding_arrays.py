@@ -92,3 +92,31 @@ def test_one_list_for_the_whole_batch_is_refused(blocks, B, prepare):
     for call in with_lists(B, indices=dev(torch.zeros(1, 4, 0, dtype=torch.int32)).expand(B, -1, -1)):          # lists without entries are not read
         call()
     assert len(blocks) == 6
+
+
+@pytest.mark.parametrize("B", [1, 2, 5])
+def test_lengths_with_gaps_are_refused(blocks, B):
+    """The library reads B neighbouring words."""
+    q, k, v, codes, scales = arrays(B)
+    scores = dev(torch.zeros(B, 4, 3, 40))
+    pages, table = (dev(torch.zeros(5 * B, 2, 8, 64, dtype=torch.bfloat16)) for _ in range(2)), dev(torch.zeros(B, 5, dtype=torch.int32))
+    kp, vp = pages
+    calls = [lambda n, **kw: binding.sts_select(scores, [0, 1, 2, 3], 5, seq_lens=n, **kw),
+             lambda n, **kw: binding.sts_dense_attn(q, k, v, 0.1, seq_lens=n, want_lse=False, **kw),
+             lambda n, **kw: binding.sts_dense_attn(q, kp, vp, 0.1, seq_lens=n, want_lse=False, page_size=8, block_table=table, N=40, **kw),
+             lambda n, **kw: binding.sts_packed_attn(q, codes, scales, 0.1, seq_lens=n, want_lse=False, **kw),
+             lambda n, **kw: binding.sts_window_attn(q, k, v, 0.1, 9, seq_lens=n, want_lse=False, **kw)]
+    plain = dev(torch.zeros(B, dtype=torch.int32))
+    for call in calls:
+        for kw in ({}, {"prepare": True}):
+            r = call(plain, **kw)
+            if kw:
+                r()
+            assert blocks.pop().seq_lens == plain.data_ptr() and not blocks
+            for n in (dev(torch.zeros(1, dtype=torch.int32)).expand(B), dev(torch.zeros(2 * B, dtype=torch.int32))[::2]):
+                if B == 1:           # one length has no gaps
+                    call(n, **kw)
+                    continue
+                with pytest.raises(AssertionError):
+                    call(n, **kw)
+            blocks.clear()
