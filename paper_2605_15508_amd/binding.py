@@ -309,6 +309,12 @@ def _batch_stride(t) -> int:
     return t.stride(0)
 
 
+def _list_ptr(t) -> Optional[int]:
+    """Pointer of lists where NULL means a call without lists: lists without elements have no address, and any other one will do, which
+    nothing reads."""
+    return None if t is None else t.data_ptr() or 16
+
+
 def _attn_params(q, k, v, scale, indices, counts, head_map, seq_lens, out, lse_out, logits_out,
                  page_size=1, block_table=None, N=None, k_new=None, v_new=None, causal=True, row_mask=None):
     import torch
@@ -659,9 +665,7 @@ def sts_packed_attn(q, codes, scales, scale, indices=None, counts=None, head_map
         assert indices.device == q.device and indices.dtype == torch.int32 and indices.dim() == 3 and tuple(indices.shape[:2]) == (B, Hq)
         kmax = indices.shape[2]
         assert kmax == 0 or (indices.stride(2) == 1 and (Hq == 1 or indices.stride(1) == kmax))
-        isb = _batch_stride(indices)
-        if kmax == 0:           # empty lists: a tensor without elements has no address, and none is read
-            indices, isb = out, 0
+        isb = _batch_stride(indices) if kmax else 0
     else:
         assert counts is None and head_map is None
     if counts is not None:
@@ -670,7 +674,7 @@ def sts_packed_attn(q, codes, scales, scale, indices=None, counts=None, head_map
         csb = _batch_stride(counts)
     hm = _host_i32(head_map) if head_map is not None else None
     assert hm is None or len(hm) == Hq
-    p = PackedAttnParams(B=B, Tq=Tq, Hq=Hq, Hkv=Hkv, d=d, q=_ptr(q), cache=cache, indices=_ptr(indices), counts=_ptr(counts), kmax=kmax,
+    p = PackedAttnParams(B=B, Tq=Tq, Hq=Hq, Hkv=Hkv, d=d, q=_ptr(q), cache=cache, indices=_list_ptr(indices), counts=_ptr(counts), kmax=kmax,
                          head_map=ctypes.cast(hm, ctypes.c_void_p) if hm is not None else None, seq_lens=_per_batch(seq_lens, B, q.device),
                          scale=float(scale), out=_ptr(out), out_dtype=STS_BF16 if out.dtype == torch.bfloat16 else STS_F32, lse_out=_ptr(lse),
                          k_new=_ptr(k_new), v_new=_ptr(v_new), causal=1 if causal else 0, idx_stride_b=isb, cnt_stride_b=csb)

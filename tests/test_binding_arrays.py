@@ -1,11 +1,13 @@
 """What the binding hands to the library for arrays of the batch that are no plain rows of memory: the calls run on CPU tensors against a
 library that keeps their parameter blocks and enqueues nothing."""
+import ctypes
+import os
 import types
 
 import pytest
 import torch
 
-from paper_2605_15508_amd import binding
+from paper_2605_15508_amd import binding, build
 
 
 class Device(torch.Tensor):
@@ -15,6 +17,13 @@ class Device(torch.Tensor):
 
 def dev(t):
     return t.as_subclass(Device)
+
+
+@pytest.fixture(scope="module")
+def library():
+    if not os.path.exists(binding.library_path()):
+        build.build(force=True)
+    return binding.load_library()
 
 
 @pytest.fixture
@@ -120,3 +129,21 @@ def test_lengths_with_gaps_are_refused(blocks, B):
                 with pytest.raises(AssertionError):
                     call(n, **kw)
             blocks.clear()
+
+
+@pytest.mark.parametrize("prepare", [False, True])
+def test_lists_of_an_empty_batch_and_lists_without_entries(library, blocks, prepare):
+    """A tensor without elements has no address; the call is one with lists all the same."""
+    lists = dev(torch.zeros(0, 4, 7, dtype=torch.int32)), dev(torch.zeros(0, 4, dtype=torch.int32))
+    calls = [*with_lists(0, indices=lists[0]), *with_lists(0, indices=lists[0], counts=lists[1], head_map=[0, 0, 1, 1])]
+    for B in (0, 2):
+        calls += with_lists(B, indices=dev(torch.zeros(B, 4, 0, dtype=torch.int32)), head_map=[0, 0, 1, 1])
+    for call in calls:
+        r = call(prepare=prepare)
+        if prepare:
+            r()
+        p = blocks.pop()
+        assert not blocks and (p.indices or isinstance(p, binding.AttnParams))           # sts_sparse_attn is one by its name
+        if p.B == 0:           # and what the library makes of it: nothing to do
+            f = library.sts_sparse_attn if isinstance(p, binding.AttnParams) else library.sts_packed_attn
+            assert f(ctypes.byref(p), None) == 0
