@@ -41,6 +41,8 @@
 //   - loop exits that made the compiler wait for all loads in flight in every second tile: see the main loop.
 #include "common.h"
 
+#include <float.h>
+
 #include <mutex>
 #include <type_traits>
 
@@ -957,7 +959,8 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(const AttnArgs A, con
     if (s0 < S) load_batch(s0);
   }
   if (seg == 0) {
-    sm_ml[wave][row4][0] = mstar;
+    // (scores that are no numbers raise no maximum: without one a share of nothing else would be taken for an empty one)
+    sm_ml[wave][row4][0] = L != L ? fmaxf(mstar, -FLT_MAX) : mstar;
     sm_ml[wave][row4][1] = L;
   }
 #pragma unroll
