@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsts.so")
 SOURCES = ["api.hip", "attn.hip", "select.hip", "select_sampled.hip", "select_row.hip", "headmap.hip", "scratch.hip", "union.hip",
            "api_cache.hip", "packed.hip", "attn_cache.hip", "attn_window.hip"]
-HEADERS = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "cache.h"), os.path.join(CSRC, "select_util.h"), os.path.join(HERE, "..", "include", "sts.h")]
+HEADERS = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "cache.h"), os.path.join(CSRC, "attn_util.h"), os.path.join(CSRC, "select_util.h"), os.path.join(HERE, "..", "include", "sts.h")]
 
 # -packed-fp32-ops is switched off on purpose: packed fp32 instructions are not to be
 # generated for this hardware.

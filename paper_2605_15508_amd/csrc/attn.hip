@@ -39,7 +39,7 @@
 //   - maxima across lanes by LDS permutes: the swaps of rows and halves;
 //   - accumulators rescaled for every tile: only where some row's maximum has grown;
 //   - loop exits that made the compiler wait for all loads in flight in every second tile: see the main loop.
-#include "common.h"
+#include "attn_util.h"
 
 #include <float.h>
 
@@ -51,35 +51,6 @@ namespace {
 template <int D> struct Chunk;
 template <> struct Chunk<128> { typedef u32x4 type; };
 template <> struct Chunk<64> { typedef u32x2 type; };
-
-// position of the n-th set bit (n < popcount)
-__device__ __forceinline__ int nth_member(uint32_t mask, int n) {
-  const int first = __builtin_ctz(mask);
-  const uint32_t run = mask >> first;
-  if ((run & (run + 1)) == 0) return first + n;      // (mask is the same for all lanes; nearly always one run of bits)
-  int pos = 0;
-#pragma unroll
-  for (int i = 0; i < STS_MAX_GROUP; ++i) {
-    const bool set = (mask >> i) & 1u;
-    if (set && n == 0) pos = i;
-    n -= set ? 1 : 0;
-  }
-  return pos;
-}
-
-// The larger of two numbers, one instruction: the median with +infinity (fmaxf first turns signalling NaNs into quiet ones, an
-// instruction per operand that the compiler cannot vouch for).
-__device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
-
-// maximum over the four lanes 16 apart (the row-of-16 swaps of this chip: no LDS round trip)
-__device__ __forceinline__ float max_over_groups(float x) {
-  const uint32_t w = __builtin_bit_cast(uint32_t, x);
-  const auto p = __builtin_amdgcn_permlane16_swap(w, w, false, false);       // rows 0, 0, 2, 2 and 1, 1, 3, 3
-  const float y = larger(__builtin_bit_cast(float, (uint32_t)p[0]), __builtin_bit_cast(float, (uint32_t)p[1]));
-  const uint32_t v = __builtin_bit_cast(uint32_t, y);
-  const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);       // the lower and the upper half
-  return larger(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
-}
 
 // waves per workgroup, and whether they keep one tile's K and V on the way instead of two's
 constexpr bool one_buffer(int D, int NQ, bool cached) { return cached && D == 128 && NQ == 2; }
@@ -820,18 +791,6 @@ attn_split_kernel(const AttnArgs A) {
   }
 }
 
-// The sum over a row's 16 lanes, in every one of them: pairs, quads, halves, all.
-__device__ __forceinline__ float row_sum16(float x) {
-  auto add = [&](auto ctrl) {
-    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, false));
-  };
-  add(std::integral_constant<int, 0xb1>());     // quad_perm: lane ^ 1
-  add(std::integral_constant<int, 0x4e>());     // quad_perm: lane ^ 2
-  add(std::integral_constant<int, 0x141>());    // row_half_mirror: the other quad of the eight
-  add(std::integral_constant<int, 0x140>());    // row_mirror: the other eight
-  return x;
-}
-
 // Combine the per-split partials and write the final rows. One workgroup of 256 threads per
 // (batch, unit, query tile, group of 4 rows): wave w merges the splits w, w+4, w+8, ... of its
 // 4 rows (thread = row, D/16 channels; loads in independent batches), the four waves are then
@@ -889,16 +848,7 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(const AttnArgs A, con
   float o[SEGF];
 #pragma unroll
   for (int e = 0; e < SEGF; ++e) o[e] = 0.f;
-  auto merge = [&](float ms, float ls, const float *x) {
-    if (ms == -INFINITY) return;
-    const float mnew = fmaxf(mstar, ms);
-    const float fo = __builtin_amdgcn_exp2f(mstar - mnew);   // 0 while nothing is accumulated
-    const float fn = __builtin_amdgcn_exp2f(ms - mnew);
-    L = L * fo + ls * fn;
-#pragma unroll
-    for (int e = 0; e < SEGF; ++e) o[e] = o[e] * fo + x[e] * fn;
-    mstar = mnew;
-  };
+  auto merge = [&](float ms, float ls, const float *x) { merge_part(mstar, L, o, ms, ls, x); };
   // The speculative block's own tokens: candidate tq also attends to candidates 0..tq (all of
   // them when not causal). They are the first entries of the last wave's share, so their loads
   // go out together with the partials' and add no latency of their own. The 16 threads of a row

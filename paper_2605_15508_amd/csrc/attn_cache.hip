@@ -31,50 +31,10 @@
 // are few (with two tiles on the way one fits: 40 sequences of 5 rows, window 600 53 us, so 43; 16 of one row, window 4096 the same).
 #include <float.h>
 
+#include "attn_util.h"
 #include "cache.h"
 
 namespace {
-
-// position of the n-th set bit (n < popcount) of a mask that is the same for all lanes, nearly always one run of bits
-__device__ __forceinline__ int nth_member(uint32_t mask, int n) {
-  const int first = __builtin_ctz(mask);
-  const uint32_t run = mask >> first;
-  if ((run & (run + 1)) == 0) return first + n;
-  int pos = 0;
-#pragma unroll
-  for (int i = 0; i < STS_MAX_GROUP; ++i) {
-    const bool set = (mask >> i) & 1u;
-    if (set && n == 0) pos = i;
-    n -= set ? 1 : 0;
-  }
-  return pos;
-}
-
-// the larger of two numbers in one instruction (see attn.hip)
-__device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
-
-__device__ __forceinline__ float top(float x, float y) { return __builtin_elementwise_maximum(x, y); }
-
-// maximum over the four lanes 16 apart
-__device__ __forceinline__ float max_over_groups(float x) {
-  const uint32_t w = __builtin_bit_cast(uint32_t, x);
-  const auto p = __builtin_amdgcn_permlane16_swap(w, w, false, false);
-  const float y = larger(__builtin_bit_cast(float, (uint32_t)p[0]), __builtin_bit_cast(float, (uint32_t)p[1]));
-  const uint32_t v = __builtin_bit_cast(uint32_t, y);
-  const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return larger(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
-}
-
-// sum over the 16 lanes of a row, the same in each of them
-__device__ __forceinline__ float row_sum(float x) {
-  auto turned = [](float y, auto ctrl) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, y), decltype(ctrl)::value, 0xf, 0xf, false));
-  };
-  x += turned(x, std::integral_constant<int, 0x128>());          // row_ror: 8, 4, 2, 1
-  x += turned(x, std::integral_constant<int, 0x124>());
-  x += turned(x, std::integral_constant<int, 0x122>());
-  return x + turned(x, std::integral_constant<int, 0x121>());
-}
 
 // a lane's share of a row: K's quarter and V's D / 16 channels
 template <int D, bool FOUR> struct Share;
@@ -700,13 +660,17 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, 2) cache_attn_kernel(const 
       for (int e = 0; e < SEGF; ++e) to[e] = __builtin_bit_cast(float, e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
     };
     const int row = threadIdx.x >> 4, seg = threadIdx.x & 15, r = nq * 16 + row;
-    f32x4 sum[SEGF / 4];
+    float sum[SEGF];
 #pragma unroll
-    for (int e = 0; e < SEGF / 4; ++e) sum[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int e = 0; e < SEGF; ++e) sum[e] = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w)
 #pragma unroll
-      for (int e = 0; e < SEGF / 4; ++e) sum[e] += *reinterpret_cast<const f32x4 *>(lds_o + (w * 16 + row) * OPITCH + seg * SEGF + 4 * e);
+      for (int e = 0; e < SEGF; e += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(lds_o + (w * 16 + row) * OPITCH + seg * SEGF + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[e + i] += x[i];
+      }
     const float m = top_of(r);
     float L = 0.f;
 #pragma unroll
@@ -716,7 +680,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, 2) cache_attn_kernel(const 
     }
     if (!A.direct) {
 #pragma unroll
-      for (int e = 0; e < SEGF / 4; ++e) *reinterpret_cast<f32x4 *>(po + (size_t)r * D + seg * SEGF + 4 * e) = sum[e];
+      for (int e = 0; e < SEGF; e += 4) *reinterpret_cast<f32x4 *>(po + (size_t)r * D + seg * SEGF + e) = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
       if (seg == 0) *reinterpret_cast<f32x2 *>(pml + r * 2) = f32x2{m, L};
     } else if (r < rows_valid) {
       const int hsel = (r * C.tq_inv) >> 16, tq = r - hsel * A.Tq, head = g * A.G + nth_member(mask, hsel);
@@ -743,26 +707,21 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, 2) cache_attn_kernel(const 
             float dot = 0.f;
 #pragma unroll
             for (int e = 0; e < SEGF; ++e) dot += q[e] * k[e];
-            const float s = row_sum(dot) * A.scale_log2;
-            if (j0 + j >= mine) continue;
-            const float m_new = fmaxf(m_all, s), fo = __builtin_amdgcn_exp2f(m_all - m_new), fn = __builtin_amdgcn_exp2f(s - m_new);
-            L = L * fo + fn;
-#pragma unroll
-            for (int e = 0; e < SEGF; ++e) sum[e >> 2][e & 3] = sum[e >> 2][e & 3] * fo + v[e] * fn;
-            m_all = m_new;
+            const float s = row_sum16(dot) * A.scale_log2;
+            merge_part(m_all, L, sum, j0 + j < mine ? s : -INFINITY, 1.f, v);
           }
         }
       }
       const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
-      for (int e = 0; e < SEGF / 4; ++e) {
-        const f32x4 x = sum[e] * inv;
+      for (int e = 0; e < SEGF; e += 4) {
+        const f32x4 x = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]} * inv;
         if (A.out_dtype == STS_F32) {
-          *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 4 * e) = x;
+          *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + e) = x;
         } else {
           const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2)),
                            __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2], x[3]}), bf16x2))};
-          *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at + 4 * e) = w;
+          *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at + e) = w;
         }
       }
       if (A.lse_out && seg == 0)

@@ -18,6 +18,7 @@
 // Head size 64 (4000 rows, window 512): 53 to 56 us, 430 to 460, the exponentials.
 #include <float.h>
 
+#include "attn_util.h"
 #include "cache.h"
 
 namespace {
@@ -35,8 +36,6 @@ template <int D> __device__ __forceinline__ int v_chunk(int r, int c) { return D
 
 // bits 0 .. n - 1, none for n <= 0
 __device__ __forceinline__ uint64_t first_keys(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
-
-__device__ __forceinline__ float top(float x, float y) { return __builtin_elementwise_maximum(x, y); }      // (a NaN wins)
 
 // PAGES: 0 none; 1 with rows at up to 2^32 units of 16 bytes in the pool; 2 further away
 template <int D, int PAGES>
