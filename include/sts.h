@@ -290,11 +290,12 @@ sts_status sts_sparse_attn_static(const sts_attn_params *p, void *stream);
 
 /* ----------------------------------------------------------------------------------------
  * A cache held in 4 bits (the paper keeps the full cache, Section 2.3; at 4.25 bits a value it takes 0.27 of
- * the bf16 cache's bytes). Per token and KV head `codes` hold d/2
- * bytes for K, then d/2 for V, two values to a byte (the even channel in the low half): a sign in
- * the top bit and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6. `scales` hold one byte s for every 32
- * neighbouring channels, d/32 for K, then d/32 for V: the codes stand for their number times 2^(s-127), and all 32
- * for NaN where s is 255; the store writes 2 <= s <= 252, and other s up to 252 are read as they say. (These are the e2m1 and e8m0 types of the OCP microscaling formats.)
+ * the bf16 cache's bytes). Per token and KV head `codes` hold d/2 bytes for K, then d/2 for V, two values to
+ * a byte (the even channel in the low half): a sign in the top bit and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ * `scales` hold one byte s for every 32 neighbouring channels, d/32 for K, then d/32 for V: the codes stand
+ * for their number times 2^(s-127), and all 32 for NaN where s is 255; the store writes 2 <= s <= 252 and 255,
+ * and s of 0 and 1 are read as they say; 253 and 254 are not defined. (These are the e2m1 and e8m0 types of
+ * the OCP microscaling formats.)
  *
  * Token n of batch element b and KV head g lies at b*stride_b + g*stride_h + n*stride_n of either
  * array (byte strides); with block_table, at page*stride_page + g*stride_h + (n % page_size)*stride_n with
@@ -302,8 +303,8 @@ sts_status sts_sparse_attn_static(const sts_attn_params *p, void *stream);
  *
  * Supported: d in {64,128}; page_size 1, 2, 4, 8, 16 or 32; codes 16-byte aligned with strides that are
  * multiples of 16, scales aligned to d/16 with strides that are multiples of it, stride_n at least a token's
- * bytes (d codes, d/16 scales) and at most 2^26. Tokens, heads, batch elements and pages must not overlap where the cache is
- * written to.
+ * bytes (d codes, d/16 scales) and at most 2^26. Tokens, heads, batch elements and pages must not overlap
+ * where the cache is written to.
  */
 typedef struct {
   uint8_t *codes;           /* [dev] */
@@ -318,9 +319,11 @@ typedef struct {
 } sts_packed_cache;
 
 /* sts_packed_store -- T rows of K and V per batch element into the cache, at positions pos[b] .. pos[b] + T - 1.
- * Every group of 32 channels takes the smallest power of two 2^e, -125 <= e <= 125, with max|x| <= 7 * 2^e (so no value
- * is off by more than half a step, saturation at 6 included) and rounds x / 2^e to the nearest code, ties to the even
- * one. A group with a NaN or an infinity becomes NaN as a whole. Rows i >= lens[b], and positions outside
+ * Every group of 32 channels takes the smallest power of two 2^e, e >= -125, with max|x| <= 7 * 2^e (so no
+ * value is off by more than half a step, saturation at 6 included) and rounds x / 2^e to the nearest code, ties
+ * to the even one. No e above 125 is used: a group whose largest exceeds 7 * 2^125 (a bf16 next to the end of
+ * its range, which is 7.97 * 2^125) takes e = 125, and values beyond 7 * 2^125 become 6 * 2^125, up to two half
+ * steps off. A group with a NaN or an infinity becomes NaN as a whole. Rows i >= lens[b], and positions outside
  * [0, N), are not stored; nothing else of the cache is written to. Two rows of one call must not name the same
  * place (pages shared between batch elements, for instance): what is then kept there is not defined.
  *
@@ -337,14 +340,19 @@ typedef struct {
   sts_packed_cache cache;
 } sts_packed_rows_params;
 
-/* sts_packed_attn -- sts_sparse_attn (indices given) or sts_dense_attn (indices NULL) over the 4-bit cache: the formulas,
- * lists, blocks, pages and the block's own tokens of sts_attn_params with K and V the values that the cache stands for.
- * Sums and softmax statistics are fp32; the cached values enter the products exactly, a query's value to 2^-17 of the
- * largest of its 32 channels, a weight as bf16. Fields as there.
- * A group of K that is NaN makes the rows that see its token NaN, one of V their 32 channels; the logarithm lse_out is then no finite
- * number. Tokens that no list names and tokens behind a sequence's end never reach a result, whatever lies there.
+/* sts_packed_attn -- sts_sparse_attn (indices given) or sts_dense_attn (indices NULL) over the 4-bit cache: the
+ * formulas, lists, blocks, pages and the block's own tokens of sts_attn_params with K and V the values that the
+ * cache stands for; no row bits, logits or sums of weights. Fields as there.
+ * Sums and softmax statistics are fp32; the cached values enter the products exactly, a query's value to 2^-17
+ * of the largest of its 32 channels (to 2^-136 where that is more), a weight as bf16. A row's q . k has to stay
+ * within fp32's range for every cached token that it sees: its result is not defined otherwise. An own token
+ * that scores below the range has no weight.
+ * A group of K that is NaN makes the rows that see its token NaN, one of V their 32 channels; the logarithm
+ * lse_out is then no finite number. Tokens that no list names and tokens behind a sequence's end never reach a
+ * result, whatever lies there.
  *
- * Supported: Tq <= 16; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; q, out, k_new and v_new 16-byte aligned; scale * log2(e) finite.
+ * Supported: Tq <= 16; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; q, out, k_new and v_new 16-byte aligned;
+ * scale * log2(e) finite.
  */
 typedef struct {
   int32_t B, Tq, Hq, Hkv, d;
@@ -367,21 +375,23 @@ typedef struct {
 } sts_packed_attn_params;
 
 /* ----------------------------------------------------------------------------------------
- * sts_window_attn -- attention with a sliding window and a few first tokens that stay visible
- * (attention sinks), over a bf16 cache: for layers that no draft's lists decide, and as the fixed policy that the
- * method is compared with.
+ * sts_window_attn -- attention with a sliding window and a few first tokens that stay visible (attention
+ * sinks), over a bf16 cache: for layers that no draft's lists decide, and as the fixed policy that the method is
+ * compared with.
  *
  * Query row i of batch element b stands at position p_i: without k_new the block's own tokens are the
  * cache's last, p_i = L_b - Tq + i; with k_new they are not in the cache yet, p_i = L_b + i, and
  * row i also attends to the new tokens 0..i. A cached token n < L_b is visible to row i iff
  *     n <= p_i  and  (n < sinks  or  n > p_i - window).
- * Otherwise the formulas of sts_dense_attn. Rows at negative positions (a padded batch: L_b < Tq) and rows that see
- * nothing give out = 0 and lse = -inf. Tq may be a whole prompt; window >= L_b is plain causal attention. What a row does
- * not see never reaches its result, NaN and infinities included, and pages of which no row sees a token are not looked up
- * at addresses of their own (their entries may be anything); a row that sees a key with NaN is NaN.
+ * Otherwise the formulas of sts_dense_attn. Rows at negative positions (a padded batch: L_b < Tq) and rows that
+ * see nothing give out = 0 and lse = -inf. Tq may be a whole prompt; window >= L_b is plain causal attention.
+ * What a row does not see never reaches its result, NaN and infinities included, and pages of which no row sees
+ * a token are not looked up at addresses of their own (their entries may be anything); a row that sees a key
+ * with NaN is NaN.
  *
  * Supported: d in {64,128}; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; Tq >= 1, with k_new Tq <= 16 and window >= Tq;
- * Tq * Hq/Hkv < 2^31 - 65536, fewer than 2^24 blocks of 128 rows of a KV head in a call with Tq > 16; window >= 1, sinks >= 0; kv strides multiples of 8 elements, kv_stride_n at least d and at most 2^25;
+ * Tq * Hq/Hkv < 2^31 - 65536, fewer than 2^24 blocks of 128 rows of a KV head in a call with Tq > 16;
+ * window >= 1, sinks >= 0; kv strides multiples of 8 elements, kv_stride_n at least d and at most 2^25;
  * q, k, v, out, k_new and v_new 16-byte aligned; scale * log2(e) finite; page_size 1, 2, 4, 8, 16 or 32.
  */
 typedef struct {

@@ -207,9 +207,10 @@ def _stream() -> int:
 class PreparedCall:
     """A library call with its parameter block built once: calling the object enqueues the call
     again on torch's current stream with the same pointers (the tensors it was built from are kept
-    alive here; the workspace is the one that was current when it was built, so use it on the
-    stream it was prepared on). For serving loops that repeat a call on fixed buffers: the
-    per-call cost on the host is one ctypes call."""
+    alive here). For serving loops that repeat a call on fixed buffers: the per-call cost on the host
+    is one ctypes call. Calls of sts_packed_attn and sts_window_attn have a workspace of their own and
+    run on any stream, one at a time each; those of the other functions share the workspace of the stream they were
+    prepared on, unless one was given, and belong on that stream."""
 
     def __init__(self, fn, params, what, result, keep):
         self._fn, self._p, self._what, self.result, self._keep = fn, params, what, result, keep
@@ -576,8 +577,6 @@ def sts_packed_store(k, v, codes, scales, pos=None, lens=None, page_size=1, bloc
     """Rows k, v [B,T,Hkv,d] bf16 into the 4-bit cache (codes [B,Hkv,N,2,d/2], scales [B,Hkv,N,2,d/32] uint8, or pools of pages
     with a block table), at positions pos[b] + 0 .. T-1 (pos None: 0); only the first lens[b] rows. See sts_packed_store
     in include/sts.h."""
-    import torch
-
     lib = load_library()
     B, T, Hkv, d = k.shape
     cache, ch, cd, _ = _packed_cache(codes, scales, page_size, block_table, N, B)

@@ -79,11 +79,12 @@ struct CachePlan {
   }
 };
 
-// Units of a short block and how many parts their tiles are cut into, `tiles` of them at most per unit: so many that `resident` workgroups run
-// at once, with two tiles for each of their four waves at least, or one (one_each) as long as every workgroup has a compute unit
-// of its own. Lists of up to 16 tiles stay whole, as for the bf16 cache: a second launch takes as long as they do. Not so with own tokens (tail)
-// and two tiles of query rows, which a whole unit's workgroup takes in one after the other, as long as there are few units (500 tokens of 4 bits,
-// 5 rows, one sequence: 11.1 us in parts, 12.4 whole; 64 heads of 16 rows, 4 sequences: 20.3 and 18.1).
+// Units of a short block and how many parts their tiles are cut into, `tiles` of them at most per unit: so many that `resident`
+// workgroups run at once, with two tiles for each of their four waves at least, or one (one_each) as long as every workgroup has a
+// compute unit of its own. Lists of up to 16 tiles stay whole, as for the bf16 cache: a second launch takes as long as they do. Not
+// so with own tokens (tail) and two tiles of query rows, which a whole unit's workgroup takes in one after the other, as long as
+// there are few units (500 tokens of 4 bits, 5 rows, one sequence: 11.1 us in parts, 12.4 whole; 64 heads of 16 rows, 4 sequences:
+// 20.3 and 18.1).
 sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, const int32_t *head_map, bool whole_groups, int64_t tiles, int row_bytes,
                        bool one_each, bool tail, int64_t (*resident)(int d), CachePlan &pl) {
   int max_heads = most_rows / Tq;
@@ -107,7 +108,8 @@ sts_status plan_splits(int B, int Tq, int Hq, int Hkv, int d, int most_rows, con
   }
   if (S < 1) S = 1;
   // Between one and two units for each compute unit some would have two to work on and most one. Parts even that out, where a unit is a
-  // megabyte of the cache or more: 33 sequences, window 4096 138 us whole, 118 in parts; 16000 tokens of 4 bits 146 and 124; 4000 of them 42 and 43.
+  // megabyte of the cache or more: 33 sequences, window 4096 138 us whole, 118 in parts; 16000 tokens of 4 bits 146 and 124; 4000
+  // of them 42 and 43.
   const int64_t cus = sts_cu_count();
   if (total > cus && total < 2 * cus && tiles * STS_TILE_KEYS * row_bytes >= 1 << 20) {
     int64_t rounds = 2;                    // with S parts; the shortest is that of the least rounds / S
@@ -184,6 +186,10 @@ sts_status plan_window(const sts_window_params *p, CachePlan &pl, bool &prompt) 
     if (p->kv_stride_page % 8) return STS_EUNSUPPORTED;
     if ((int64_t)p->table_stride * page < p->N) return STS_EINVAL;
   }
+  // Which kernel: by the number of query rows. 16 rows in units of up to 32 rows of a KV head, and 17 in blocks of 128, over 8 KV heads, window
+  // 4096 of 32768 tokens: 1, 2, 4, 8 query heads each and one sequence 13.2 and 19.6 us, 15.3 and 20.6, 15.8 and 20.8, 18.8 and 22.4; 16
+  // sequences 47 and 64, 50 and 64, 80 and 67, 159 and 99. (With 64 rows and more on a KV head, where several units read the same
+  // window, the second would be ahead in large batches.)
   prompt = p->Tq > 16;
   memset(&pl, 0, sizeof(pl));
   if (prompt) {

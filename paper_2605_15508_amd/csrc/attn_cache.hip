@@ -2,8 +2,9 @@
 // (sts_packed_attn: all tokens, or index lists), or bf16 with a sliding window and sinks (sts_window_attn).
 //
 // Units, splits and partials are those of the bf16 kernels (attn.hip), whose combine kernel merges the splits and appends
-// the block's own tokens. A workgroup that has a unit whole appends them itself (64 sequences of 1500 tokens, 5 rows: 34 us, with the combine kernel 56). One workgroup of four waves per (batch, unit, split); waves take alternating tiles of 32 keys
-// and keep an online softmax of their own, with maximum, sum and accumulators in fp32.
+// the block's own tokens. A workgroup that has a unit whole appends them itself (64 sequences of 1500 tokens, 5 rows: 34 us, with the
+// combine kernel 56). One workgroup of four waves per (batch, unit, split); waves take alternating tiles of 32 keys and keep an online
+// softmax of their own, with maximum, sum and accumulators in fp32.
 //
 // Tiles in the transposed orientation, S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x32_bf16, lane (a, b) =
 // (lane / 16, lane % 16). Which key a row of K's operand holds is free, so row 4a + i of half h is the tile's key
@@ -14,21 +15,24 @@
 //   - K's operand is loaded as it is used, a lane's share of one key's row: no LDS, no exchange. Of a row of 4-bit codes
 //     lane a has the a-th quarter, 16 bytes at head size 128 and one scale; of a bf16 row every fourth chunk of 16 bytes.
 // S over 4-bit codes: v_mfma_scale_f32_16x16x128_f8f6f4 takes K's codes and scales as they lie in memory, a lane 32 channels of a key
-// and their scale. Q, the other operand, is the sum of two e4m3 numbers, high and low, with a scale per 32 channels: four significant bits
-// each hold the eight of a bf16 exactly for values of at least 2^-9 of their group's largest, and others to 2^-17 of that largest.
+// and their scale. Q, the other operand, is the sum of two e4m3 numbers, high and low, with a scale per 32 channels: four
+// significant bits each hold the eight of a bf16 exactly for values of at least 2^-9 of their group's largest, and others to 2^-17
+// of that largest (to 2^-136 where the scale is at its smallest).
 // At head size 64 both halves go into one instruction, K's row taken twice.
 // V's codes become bf16 pairs in the chip's conversion, scale included, exactly. The pairs are two channels of one key and have to
 // become two keys of one channel: two byte permutes per pair of registers, as for bf16.
 // Scales: a lane loads the word of one token of the tile, K's in the lower half of the wave, V's in the upper, and
 // the lanes pick up those of their rows from LDS, one tile ahead of their use: bytes for K, the conversion's floats for V.
 //
-// What bounds it. 4 bits, 20 query rows on a KV head (128K tokens, batch 4): 571 MB in 107 us, 5.3 TB/s, vector instructions 65% and matrix
-// instructions 31% of the time: converting V takes as many as the softmax does. 16 rows and fewer: memory (one row 4.2 TB/s); 64 rows on a KV
-// head are two units, each of which converts V (123 MB in 55 us; units of 64 rows do not fit the registers). Lists: rows of
-// 136 bytes are a line of codes and a piece of one of scales (121 MB in 29 us). The bf16 window: memory (16 sequences, window 4096: 269 MB in
-// 45 us, 6.0 TB/s). Few keys: the chain length -> page -> row -> product -> merge, 6 to 9 us, and 3.5 to 5 of the combine kernel.
-// Three tiles of 4 bits are on the way in each wave, of bf16 two at head size 64 and one at 128: so two workgroups fit a compute unit, one where there
-// are few (with two tiles on the way one fits: 40 sequences of 5 rows, window 600 53 us, so 43; 16 of one row, window 4096 the same).
+// What bounds it. 4 bits, 20 query rows on a KV head (128K tokens, batch 4): 571 MB in 107 us, 5.3 TB/s, vector instructions 65%
+// and matrix instructions 31% of the time: converting V takes as many as the softmax does. 16 rows and fewer: memory (one row 4.2
+// TB/s); 64 rows on a KV head are two units, each of which converts V (123 MB in 55 us; units of 64 rows do not fit the registers).
+// Lists: rows of 136 bytes are a line of codes and a piece of one of scales (121 MB in 29 us). The bf16 window: memory (16
+// sequences, window 4096: 269 MB in 45 us, 6.0 TB/s). Few keys: the chain length -> page -> row -> product -> merge, 6 to 9 us, and
+// 3.5 to 5 of the combine kernel.
+// Three tiles of 4 bits are on the way in each wave, of bf16 two at head size 64 and one at 128: so two workgroups fit a compute
+// unit, one where there are few (with two tiles on the way one fits: 40 sequences of 5 rows, window 600 53 us, so 43; 16 of one
+// row, window 4096 the same).
 #include <float.h>
 
 #include "attn_util.h"
@@ -63,8 +67,8 @@ __device__ __forceinline__ uint32_t largest(const uint32_t (&w)[8]) {
   return max(lo, hi);
 }
 
-// 16 bf16 values as e4m3 numbers hi + lo, each times 2^(s - 127); s puts a group's largest value, of magnitude bits m, at 2^7 .. 2^8 (255 for one
-// that is no number, or infinite: the products are NaN then)
+// 16 bf16 values as e4m3 numbers hi + lo, each times 2^(s - 127); s puts a group's largest value, of magnitude bits m, at 2^7 ..
+// 2^8 (255 for one that is no number, or infinite: the products are NaN then)
 __device__ __forceinline__ uint32_t q_scale(uint32_t m) { return m >= 0x7f80u ? 255u : (uint32_t)max((int)(m >> 7) - 7, 1); }
 __device__ __forceinline__ void q_halves(const uint32_t (&w)[8], uint32_t s, u32x4 &hi, u32x4 &lo) {
   typedef short s16x2 __attribute__((ext_vector_type(2)));
@@ -505,8 +509,8 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, 2) cache_attn_kernel(const 
     }
   };
 
-  // ---- main loop: PF tiles on the way, each asked for again when it has been used. One exit, and code of its own for what is left over, so
-  // that the loop's head knows which loads are in flight. Q comes while the first tiles are on their way.
+  // ---- main loop: PF tiles on the way, each asked for again when it has been used. One exit, and code of its own for what is left
+  // over, so that the loop's head knows which loads are in flight. Q comes while the first tiles are on their way.
   // GATHER: a list entry is fetched 3 PF tiles ahead of its use, its page looked up 2 PF ahead, the offset placed PF + 1 ahead.
   Tile R[PF];
   uint32_t seen[PF], next_seen = 0;

@@ -47,8 +47,9 @@ __device__ __forceinline__ float row_sum16(float x) {
   return x;
 }
 
-// One more part of a row, of maximum ms (in powers of two), sum ls and weighted sums x relative to it, joined to the row's m, l and o. What has no
-// maximum, an empty part or a token whose score is -infinity, has no weight and is left out: -inf - -inf is no number.
+// One more part of a row, of maximum ms (in powers of two), sum ls and weighted sums x relative to it, joined to the row's m, l and
+// o. What has no maximum, an empty part or a token whose score is -infinity, has no weight and is left out: -inf - -inf is no
+// number.
 template <int N>
 __device__ __forceinline__ void merge_part(float &m, float &l, float (&o)[N], float ms, float ls, const float *x) {
   if (ms == -INFINITY) return;

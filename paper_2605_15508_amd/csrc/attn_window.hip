@@ -12,10 +12,13 @@
 // LDS chunks of 16 bytes are permuted within a row so that neither K's reads (16 rows, one chunk each) nor V's (4 rows, 64
 // bytes each) meet in a bank.
 //
-// What bounds it: matrix and vector instructions of two waves on a SIMD (three at head size 64) that wait for each other at a barrier per tile.
-// 8192 rows, all causal: 555 us, 990 TFLOP/s, where this card's 8192^3 product reaches 1270; window 1024: 173 to 184 us, 700 to 750 (17
-// tiles a block, the first wait for which and the masked ends do not shrink with the window); 1999 rows behind 33001 tokens, window 4096: 148 us, 907.
-// Head size 64 (4000 rows, window 512): 53 to 56 us, 430 to 460, the exponentials.
+// What bounds it: matrix and vector instructions of two waves on a SIMD (three at head size 64) that wait for each other at a barrier
+// per tile. 8192 rows, all causal: 555 us, 990 TFLOP/s, where this card's 8192^3 product reaches 1270. Window 1024: 171 to 180 us, 720 to
+// 757 (17 tiles a block, the first wait for which and the masked ends do not shrink with the window; vector instructions take 51% of the
+// cycles, matrix instructions 39%, and a wave waits for 28% of its time). 1999 rows behind 33001 tokens, window 4096: 148 us, 907
+// (49%, 44%, 30%). Head size 64 (two prompts of up to 4000 rows, window 512): 47 to 58 us, by their lengths: vector instructions,
+// 61% of the cycles and 17 for every matrix instruction (25%), an eighth of them exponentials; ten tiles a block, and a wave waits
+// for 34% of its time.
 #include <float.h>
 
 #include "attn_util.h"
@@ -75,8 +78,8 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 && PAGES < 2 ? 3 : 2) wind
   const int b_lo = p_first + A.by_group.of(row_0), b_hi = p_first + A.by_group.of(min(row_0 + ROWS - 1, rows - 1));          // the workgroup's
   const int w_lo = p_first + A.by_group.of(min(row_w, rows - 1)), w_hi = p_first + A.by_group.of(min(row_w + 31, rows - 1)); // the wave's
 
-  // The keys that some query of the block sees, one after the other: those of `firsts` sinks before lo, then lo .. end - 1. Place v holds key v, or
-  // v + skipped from `firsts` on.
+  // The keys that some query of the block sees, one after the other: those of `firsts` sinks before lo, then lo .. end - 1. Place v
+  // holds key v, or v + skipped from `firsts` on.
   const int end = max(min(b_hi + 1, L), 0);
   const int lo = (int)min(max((int64_t)b_lo - A.window + 1, (int64_t)0), (int64_t)end);
   const int firsts = min(A.sinks, lo), skipped = lo - firsts;
@@ -193,7 +196,8 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 && PAGES < 2 ? 3 : 2) wind
     return w;
   };
 
-  // which keys of tile t the lane's query sees, a bit each: the sinks, then those up to it, without those between the sinks and its window
+  // which keys of tile t the lane's query sees, a bit each: the sinks, then those up to it, without those between the sinks and its
+  // window
   auto seen_keys = [&](int t) {
     const int n0 = first_of(t);
     return first_keys(firsts - t * TK) |
@@ -295,8 +299,8 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 && PAGES < 2 ? 3 : 2) wind
     return __builtin_amdgcn_readfirstlane((int)any) != 0;
   };
 
-  // ---- The next tile's scores are worked out while this one's weights are: matrix and vector instructions of one wave, which do not wait
-  // for each other. K is a tile ahead of V.
+  // ---- The next tile's scores are worked out while this one's weights are: matrix and vector instructions of one wave, which do
+  // not wait for each other. K is a tile ahead of V.
   // What was asked for has come, and what was read is in registers: the tiles change hands.
   auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
   bool later = false;              // tiles left for the end: see below
@@ -353,8 +357,8 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 && PAGES < 2 ? 3 : 2) wind
       if (t + 2 >= tiles) break;
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);              // all that was asked for has come
-    // What is infinite or no number must not reach queries that do not see it, and 0 times it is not 0: such tiles come last, key by key, and
-    // a key's row is taken in only where it is seen.
+    // What is infinite or no number must not reach queries that do not see it, and 0 times it is not 0: such tiles come last, key
+    // by key, and a key's row is taken in only where it is seen.
     if (__syncthreads_or(later)) {
       for (int t = begin; t < tiles; ++t) {
         arrived();

@@ -26,8 +26,8 @@ struct PackedRowsArgs {
   int32_t B, T, Hkv, d;
 };
 
-// n / d for 0 <= n < 2^31 as a product (Granlund and Montgomery, "Division by invariant integers using multiplication"): with 2^l >= d > 2^(l-1)
-// and mul = floor(2^(31+l) / d) + 1, n * mul >> 31 + l is exact. A division takes a wave some forty instructions.
+// n / d for 0 <= n < 2^31 as a product (Granlund and Montgomery, "Division by invariant integers using multiplication"): with 2^l
+// >= d > 2^(l-1) and mul = floor(2^(31+l) / d) + 1, n * mul >> 31 + l is exact. A division takes a wave some forty instructions.
 struct Divisor {
   uint32_t mul, shift;
   __host__ __device__ __forceinline__ int of(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }

@@ -1,13 +1,13 @@
 // The 4-bit cache: rows of K and V in, and the values that it holds for them out (gfx950).
 //
 // A group of 32 channels takes s = floor(log2(max|x|)) - 2 + 127, one more where max|x| > 1.75 * 2^floor(log2(max|x|)); in the
-// bits of a bf16 magnitude m (exponent e, 7 bits of fraction f) that is ((m + 31) >> 7) - 2: f > 96 carries into the exponent. The codes are
-// what the chip's own conversion gives for x * 2^(127 - s): the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, ties to the even code,
-// at most 6. With max|x| <= 7 * 2^(s - 127) the limit is the nearest code, too. Nothing here rounds but that conversion.
+// bits of a bf16 magnitude m (exponent e, 7 bits of fraction f) that is ((m + 31) >> 7) - 2: f > 96 carries into the exponent. The
+// codes are what the chip's own conversion gives for x * 2^(127 - s): the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, ties to the even
+// code, at most 6. With max|x| <= 7 * 2^(s - 127) the limit is the nearest code, too. Nothing here rounds but that conversion.
 //
 // What bounds both: memory. A lane holds 8 channels, 16 bytes of bf16 and 4 of codes, so that a wave's accesses are whole rows; K's
-// and V's row are under way together. 100003 tokens of 8 KV heads out of the cache: 518 MB in 100 us, 5.2 TB/s read and written, where a copy
-// of 512 MB reaches 5.3; 2 x 8191 rows into a pool of pages 16.5 us. A step's few rows take a launch, 3 us.
+// and V's row are under way together. 100003 tokens of 8 KV heads out of the cache: 518 MB in 100 us, 5.2 TB/s read and written,
+// where a copy of 512 MB reaches 5.3; 2 x 8191 rows into a pool of pages 16.5 us. A step's few rows take a launch, 3 us.
 #include "cache.h"
 
 namespace {
