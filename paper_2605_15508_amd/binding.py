@@ -301,6 +301,11 @@ def sts_select(scores, head_map, k: int, lse=None, seq_lens=None, kind: int = ST
     return indices, counts, agg
 
 
+def _i32(x) -> int:
+    """A number for a 32-bit field; what lies beyond (which a field would cut to other numbers) becomes the field's own end."""
+    return max(-0x80000000, min(int(x), 0x7fffffff))
+
+
 def _batch_stride(t) -> int:
     """Elements from one batch element's part of a list to the next's, 0 where there is one alone. The library takes 0 for "not
     given": a list that the whole batch shares by a stride of 0 would be read behind its end."""
@@ -544,7 +549,7 @@ def _packed_cache(codes, scales, page_size, block_table, N, B=None):
         B, ts = block_table.shape
         table, pages, cb, cp, sb, sp = block_table.data_ptr(), rooms, 0, cb, 0, sb
     # (by position, in the order of the header's fields: a third of the time of names)
-    return PackedCache(codes.data_ptr(), scales.data_ptr(), cb, ch, cn, cp, sb, sh, sn, sp, table, ts, pages, page_size, N), Hkv, 2 * dh, B
+    return PackedCache(codes.data_ptr(), scales.data_ptr(), cb, ch, cn, cp, sb, sh, sn, sp, table, ts, pages, _i32(page_size), N), Hkv, 2 * dh, B
 
 
 def _current(dev):
@@ -707,8 +712,8 @@ def sts_window_attn(q, k, v, scale, window: int, sinks: int = 0, seq_lens=None, 
         sb, sp, pages, ts = 0, k.stride(0), rooms, block_table.shape[1]
     _new_rows(q, Hkv, k_new, v_new)
     p = WindowParams(B=B, Tq=Tq, Hq=Hq, Hkv=Hkv, d=d, N=int(N), q=_ptr(q), k=_ptr(k), v=_ptr(v), kv_stride_b=sb, kv_stride_h=k.stride(1),
-                     kv_stride_n=k.stride(2), seq_lens=_per_batch(seq_lens, B, q.device), window=min(int(window), 0x7fffffff), sinks=min(int(sinks), 0x7fffffff), scale=float(scale),
-                     out=_ptr(out), out_dtype=STS_BF16 if out.dtype == torch.bfloat16 else STS_F32, lse_out=_ptr(lse), page_size=int(page_size),
+                     kv_stride_n=k.stride(2), seq_lens=_per_batch(seq_lens, B, q.device), window=_i32(window), sinks=_i32(sinks), scale=float(scale),
+                     out=_ptr(out), out_dtype=STS_BF16 if out.dtype == torch.bfloat16 else STS_F32, lse_out=_ptr(lse), page_size=_i32(page_size),
                      block_table=_ptr(block_table), table_stride=ts, num_pages=pages, kv_stride_page=sp, k_new=_ptr(k_new), v_new=_ptr(v_new))
     return _run_with_workspace(lib.sts_window_attn, lib.sts_window_attn_workspace_bytes, p, "sts_window_attn", "attn", workspace, q.device, (out, lse),
                                (q, k, v, seq_lens, block_table, k_new, v_new), prepare)

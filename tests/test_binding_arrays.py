@@ -147,3 +147,23 @@ def test_lists_of_an_empty_batch_and_lists_without_entries(library, blocks, prep
         if p.B == 0:           # and what the library makes of it: nothing to do
             f = library.sts_sparse_attn if isinstance(p, binding.AttnParams) else library.sts_packed_attn
             assert f(ctypes.byref(p), None) == 0
+
+
+@pytest.mark.parametrize("big", [2 ** 31, 2 ** 32, 2 ** 32 + 16, 10 ** 12, 2 ** 64])
+def test_numbers_beyond_32_bits_do_not_wrap(library, blocks, big):
+    """A window or sinks beyond any cache mean all of it; negative ones, and page sizes, are refused as smaller ones are."""
+    q, k, v, codes, scales = arrays(2)
+    rows = dev(torch.zeros(2, 3, 2, 64, dtype=torch.bfloat16))
+    binding.sts_window_attn(q, k, v, 0.1, big, sinks=big, want_lse=False)
+    assert (blocks[-1].window, blocks[-1].sinks) == (2 ** 31 - 1, 2 ** 31 - 1)
+    binding.sts_window_attn(q, k, v, 0.1, -big, sinks=-big, want_lse=False)
+    assert blocks[-1].window < 0 and blocks[-1].sinks < 0
+    calls = [(lambda: binding.sts_window_attn(q, k, v, 0.1, 9, page_size=big, want_lse=False), library.sts_window_attn),
+             (lambda: binding.sts_packed_attn(q, codes, scales, 0.1, page_size=big, want_lse=False), library.sts_packed_attn),
+             (lambda: binding.sts_packed_store(rows, rows, codes, scales, page_size=big), library.sts_packed_store),
+             (lambda: binding.sts_packed_load(codes, scales, 3, page_size=big, out=(rows, rows)), library.sts_packed_load)]
+    for call, f in calls:
+        call()
+        p = blocks.pop()
+        assert (p.cache if hasattr(p, "cache") else p).page_size == 2 ** 31 - 1
+        assert f(ctypes.byref(p), None) == -2          # not supported: found before anything is enqueued
