@@ -643,6 +643,7 @@ def _run_with_workspace(fn, size, p, what, tag, workspace, dev, result, keep, pr
             ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
         else:
             ws = _workspace(tag, need, dev)
+    assert ws.device == dev and ws.is_contiguous()
     p.workspace, p.workspace_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
     if prepare:       # build once, launch many times (see PreparedCall)
         return PreparedCall(fn, p, what, result, (keep, ws))

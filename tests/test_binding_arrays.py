@@ -167,3 +167,16 @@ def test_numbers_beyond_32_bits_do_not_wrap(library, blocks, big):
         p = blocks.pop()
         assert (p.cache if hasattr(p, "cache") else p).page_size == 2 ** 31 - 1
         assert f(ctypes.byref(p), None) == -2          # not supported: found before anything is enqueued
+
+
+def test_scratch_that_is_not_on_the_device_is_refused(blocks):
+    q, k, v, codes, scales = arrays(2)
+    elsewhere = torch.empty(1 << 20, dtype=torch.uint8, device="meta")
+    gaps = torch.empty(1 << 20, dtype=torch.uint8)[::2]
+    for ws in (elsewhere, gaps):
+        for prepare in (False, True):
+            with pytest.raises(AssertionError):
+                binding.sts_window_attn(q, k, v, 0.1, 9, want_lse=False, workspace=ws, prepare=prepare)
+            with pytest.raises(AssertionError):
+                binding.sts_packed_attn(q, codes, scales, 0.1, want_lse=False, workspace=ws, prepare=prepare)
+    assert not blocks
