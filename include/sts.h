@@ -347,9 +347,8 @@ typedef struct {
  * of the largest of its 32 channels (to 2^-136 where that is more), a weight as bf16. A row's q . k has to stay
  * within fp32's range for every cached token that it sees: its result is not defined otherwise. An own token
  * that scores below the range has no weight.
- * A group of K that is NaN makes the rows that see its token NaN, one of V their 32 channels; the logarithm
- * lse_out is then no finite number. Tokens that no list names and tokens behind a sequence's end never reach a
- * result, whatever lies there.
+ * A group of K that is NaN makes the rows that see its token NaN and their lse -inf, one of V their 32 channels.
+ * Tokens that no list names and tokens behind a sequence's end never reach a result, whatever lies there.
  *
  * Supported: Tq <= 16; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; q, out, k_new and v_new 16-byte aligned;
  * scale * log2(e) finite.
@@ -387,7 +386,7 @@ typedef struct {
  * see nothing give out = 0 and lse = -inf. Tq may be a whole prompt; window >= L_b is plain causal attention.
  * What a row does not see never reaches its result, NaN and infinities included, and pages of which no row sees
  * a token are not looked up at addresses of their own (their entries may be anything); a row that sees a key
- * with NaN is NaN.
+ * with NaN is NaN, its lse -inf.
  *
  * Supported: d in {64,128}; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; Tq >= 1, with k_new Tq <= 16 and window >= Tq;
  * Tq * Hq/Hkv < 2^31 - 65536, fewer than 2^24 blocks of 128 rows of a KV head in a call with Tq > 16;

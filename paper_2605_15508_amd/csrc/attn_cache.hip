@@ -729,7 +729,7 @@ __global__ void __launch_bounds__(64 * STS_WG_WAVES, 2) cache_attn_kernel(const 
         }
       }
       if (A.lse_out && seg == 0)
-        A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + tq] = L == 0.f ? -INFINITY : (m_all + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f;
+        A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + tq] = L > 0.f ? (m_all + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f : -INFINITY;
     }
     __syncthreads();
   }

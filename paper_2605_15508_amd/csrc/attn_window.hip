@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 && PAGES < 2 ? 3 : 2) wind
       }
     }
   if (A.lse_out && h == 0)
-    A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + qi] = l_run == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_run)) * 0.69314718055994530942f;
+    A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + qi] = l_run > 0.f ? (m_run + __builtin_amdgcn_logf(l_run)) * 0.69314718055994530942f : -INFINITY;
 }
 
 // The parts of a block's rows put together, in order: D / 4 threads a row, four channels each.
@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(256) window_combine_kernel(const WindowArgs A)
     *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at) = w;
   }
   if (A.lse_out && chan == 0)
-    A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    A.lse_out[((size_t)bt * A.Hq + head) * A.Tq + qi] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
 }
 
 }  // namespace

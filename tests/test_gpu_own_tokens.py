@@ -45,3 +45,29 @@ def test_own_keys_that_are_no_numbers(d, Tq, bad, N):
         assert not torch.isfinite(got[1][:, 2:, first:]).any(), name
         assert torch.equal(got[0][:, :, :2], want[0][:, :, :2]) and torch.equal(got[1][:, :2], want[1][:, :2]), name
         assert torch.equal(got[0][:, :first], want[0][:, :first]) and torch.equal(got[1][..., :first], want[1][..., :first]), name
+
+
+@pytest.mark.parametrize("Tq,N", [(1, 40), (1, 3000), (4, 500), (4, 20000), (40, 300), (40, 2000)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_that_are_no_numbers_have_no_logarithm(d, Tq, N):
+    """A cached key that is NaN: the rows that see it are NaN, and their lse is -inf, from one workgroup or several."""
+    Hq, Hkv = 4, 2
+    g = torch.Generator().manual_seed(N + Tq)
+    q = torch.randn(1, Tq, Hq, d, generator=g).to(torch.bfloat16).to(DEV)
+    k, v = (torch.randn(1, Hkv, N, d, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    codes, scales = (t.to(DEV) for t in packed_cache(1, Hkv, N, d, g)[:2])
+    bad = N - 2
+    k[:, 1, bad, 0] = math.nan
+    scales[:, 1, bad, 0, 0] = 255
+    idx = torch.arange(N, dtype=torch.int32, device=DEV).expand(1, Hq, N).contiguous()
+    p = torch.arange(N - Tq, N)
+    calls = {"window": (sts.sts_window_attn(q, k, v, 0.1, N), p >= bad), "short window": (sts.sts_window_attn(q, k, v, 0.1, 17), p >= bad)}
+    if Tq <= 16:
+        every = torch.ones(Tq, dtype=torch.bool)
+        calls.update({"packed": (sts.sts_packed_attn(q, codes, scales, 0.1), every), "lists": (sts.sts_packed_attn(q, codes, scales, 0.1, indices=idx), every),
+                      "sparse": (sts.sts_sparse_attn(q, k, v, idx, 0.1), every), "dense": (sts.sts_dense_attn(q, k, v, 0.1)[:2], every)})
+    for name, ((o, l), hit) in calls.items():
+        o, l = o.cpu(), l.cpu()
+        assert torch.isnan(o[:, hit, 2:]).all() and torch.isneginf(l[:, 2:, hit]).all(), name
+        assert torch.isfinite(o[:, :, :2]).all() and torch.isfinite(l[:, :2]).all(), name
+        assert torch.isfinite(o[:, ~hit]).all() and torch.isfinite(l[..., ~hit]).all(), name
