@@ -420,6 +420,80 @@ sts_status sts_packed_attn(const sts_packed_attn_params *p, void *stream);
 size_t sts_window_attn_workspace_bytes(const sts_window_params *p);
 sts_status sts_window_attn(const sts_window_params *p, void *stream);
 
+/* ----------------------------------------------------------------------------------------
+ * Layers over packed batches. Rows of B sequences lie one after the other in tensors of T rows: those of sequence b are starts[b] ..
+ * starts[b+1] - 1 (a sequence may be empty; starts must ascend and lie in [0,T], else rows are taken for wrong sequences, but none
+ * outside the tensors is touched). Rows that belong to no sequence are not read, and left as they were in the outputs.
+ * Rows of q, k and v have strides of their own (slices of one projection's output, for instance), unit stride on d.
+ *
+ * Supported: d in {64,128}; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; T * Hq/Hkv < 2^31 - 65536; strides multiples of 8 elements, of rows
+ * at least d and at most 2^25, of heads not negative; q, k, v and out 16-byte aligned; scale * log2(e) finite; fewer than 2^24 workgroups.
+ *
+ * sts_prompt_attn -- causal attention over whole prompts: query row i of a sequence sees the keys 0 .. i of its sequence,
+ *     s_j = scale * <Q[i,t,:], K[j,g,:]>,   out[i,t,:] = sum_j exp(s_j - lse) V[j,g,:],   lse[t,i] = ln sum_j exp(s_j)
+ * with g = t / (Hq/Hkv). What a row does not see never reaches its result, NaN and infinities included; a row that sees a key with NaN is NaN, its
+ * lse -inf. Weights enter the second product as bf16, sums and statistics are fp32. No workspace.
+ */
+typedef struct {
+  int32_t B, T, Hq, Hkv, d;
+  const void *q;            /* [dev] bf16 [T,Hq,d] */
+  const void *k, *v;        /* [dev] bf16 [T,Hkv,d] */
+  int64_t q_stride_n, q_stride_h;     /* in elements, between rows and between heads */
+  int64_t kv_stride_n, kv_stride_h;   /* shared by k and v */
+  const int32_t *starts;    /* [dev] [B+1] */
+  float scale;
+  void *out;                /* [dev] [T,Hq,d] of out_dtype, contiguous */
+  int32_t out_dtype;        /* sts_dtype */
+  float *lse_out;           /* [dev] optional [Hq,T] */
+} sts_prompt_params;
+
+/* sts_linear_attn -- linear attention with a decay for each head, in prompts, single tokens and verification blocks. Per sequence and KV head
+ * a state S of d x d fp32 numbers, and for its rows i in order (g = t / (Hq/Hkv))
+ *     S = exp(decay[i,g]) S + K[i,g,:] V[i,g,:]^T,   out[i,t,:] = scale * Q[i,t,:]^T S.
+ * decay holds natural logarithms, of each row and KV head or of the KV heads alone; they are meant to be <= 0 (-inf forgets all that was).
+ *
+ * States lie in pools of slots [num_slots][Hkv][d (K's channel)][d (V's)], state_stride elements from slot to slot: sequence b starts from slot
+ * slots[b] of `state` (slots NULL: b) and its state behind its last row goes to slot slots_out[b] of `state_out`. Without `state`, or with a
+ * slot outside the pool (-1, for instance), a sequence starts from zeros; without state_out, or with such a slot, its state is not kept. Both
+ * pools may be one, and a sequence's two slots the same; else no slot may be read or written by one sequence and written by another of the
+ * same call: what it then holds is not defined. A sequence without rows has its state copied.
+ * lens (optional): only the first lens[b] rows of sequence b count. So a verification block is one call with out and without state_out, and
+ * once it is known how many rows were accepted, a second with lens, state_out, and q and out NULL.
+ *
+ * starts NULL: T / B rows for each sequence. max_len (0: T) is the length of the longest sequence: rows of a sequence behind it are left out.
+ * With max_len <= 16 the recurrence is worked out row by row in fp32. Else by chunks of rows: k^T v enters the state as in fp32, while
+ * the weights of a chunk's rows and the state (as the operand of q^T S alone) are rounded to bf16.
+ * Values of v that are infinite or NaN do not reach rows before their own; from there on results and state that depend on them are NaN or
+ * infinite. The workspace's size depends on the integer fields and on whether starts is NULL.
+ */
+typedef struct {
+  int32_t B, T, max_len, Hq, Hkv, d;
+  const void *q;            /* [dev] bf16 [T,Hq,d], or NULL together with out */
+  const void *k, *v;        /* [dev] bf16 [T,Hkv,d] */
+  int64_t q_stride_n, q_stride_h, kv_stride_n, kv_stride_h;   /* as above */
+  const float *decay;       /* [dev] [Hkv], or [T,Hkv] */
+  int32_t decay_rows;       /* non-zero: [T,Hkv] */
+  const int32_t *starts;    /* [dev] [B+1], or NULL */
+  const int32_t *lens;      /* [dev] [B], or NULL: all rows */
+  float scale;
+  const float *state;       /* [dev] 16-byte aligned, or NULL; state_stride a multiple of 4, at least Hkv*d*d */
+  int64_t state_stride;
+  const int32_t *slots;     /* [dev] [B], or NULL */
+  int32_t num_slots;        /* at least B where slots is NULL */
+  float *state_out;         /* the same for the states behind the rows */
+  int64_t state_out_stride;
+  const int32_t *slots_out;
+  int32_t num_slots_out;
+  void *out;                /* [dev] [T,Hq,d] of out_dtype, contiguous, or NULL */
+  int32_t out_dtype;
+  void *workspace;          /* [dev] 256-byte aligned scratch */
+  size_t workspace_bytes;
+} sts_linear_params;
+
+sts_status sts_prompt_attn(const sts_prompt_params *p, void *stream);
+size_t sts_linear_attn_workspace_bytes(const sts_linear_params *p);
+sts_status sts_linear_attn(const sts_linear_params *p, void *stream);
+
 const char *sts_strerror(int status);   /* any int: values that are no sts_status give "unknown status" */
 int sts_version(void);
 
@@ -456,7 +530,12 @@ typedef enum {
   STS_K_PACKED_LOAD = 18,     /* rows of the 4-bit cache -> bf16 */
   STS_K_PACKED_ATTN = 19,     /* split attention over a 4-bit cache */
   STS_K_WINDOW = 20,       /* attention with a sliding window and sinks (short blocks and prompts) */
-  STS_K_COUNT_ = 21
+  STS_K_PROMPT = 21,       /* causal attention over packed prompts */
+  STS_K_LINEAR_STEP = 22,  /* linear attention, row by row */
+  STS_K_LINEAR_SUMS = 23,  /* linear attention by chunks: what each segment of a sequence adds to the state */
+  STS_K_LINEAR_CARRY = 24, /* the states before the segments */
+  STS_K_LINEAR_CHUNKS = 25, /* the results */
+  STS_K_COUNT_ = 26
 } sts_kernel_kind;
 #define STS_PROF_MAX 4096
 

@@ -22,7 +22,8 @@ KERNEL_KINDS = {"select_clear": 0, "select_agg": 1, "select_hist": 2, "select_ro
                 "select_write": 4, "attn_sparse": 5, "attn_dense": 6, "attn_combine": 7, "select_block": 8,
                 "headmap": 9, "select_small": 10, "select_local": 11, "select_pool": 12,
                 "attn_probsum": 13, "select_fused": 14, "union_rows": 15, "select_band": 16, "packed_store": 17,
-                "packed_load": 18, "packed_attn": 19, "window": 20}
+                "packed_load": 18, "packed_attn": 19, "window": 20, "prompt": 21, "linear_step": 22, "linear_sums": 23,
+                "linear_carry": 24, "linear_chunks": 25}
 KNOBS = {"attn_wgs_per_cu": 0, "select_spin_limit": 1, "probsum_wgs_per_cu": 2, "select_path": 3, "select_row_threads": 4}
 
 # every symbol include/sts.h declares
@@ -31,7 +32,7 @@ EXPORTS = ["sts_select_workspace_bytes", "sts_attn_workspace_bytes", "sts_select
            "sts_prof_read", "sts_attn_plan", "sts_head_map", "sts_headmap_workspace_bytes",
            "sts_sparse_attn_static", "sts_set_knob", "sts_get_knob", "sts_union_rows", "sts_packed_store",
            "sts_packed_load", "sts_packed_attn", "sts_packed_attn_workspace_bytes", "sts_window_attn",
-           "sts_window_attn_workspace_bytes"]
+           "sts_window_attn_workspace_bytes", "sts_prompt_attn", "sts_linear_attn", "sts_linear_attn_workspace_bytes"]
 STS_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -120,6 +121,27 @@ class WindowParams(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class PromptParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride_n", ctypes.c_int64), ("q_stride_h", ctypes.c_int64), ("kv_stride_n", ctypes.c_int64),
+                ("kv_stride_h", ctypes.c_int64), ("starts", ctypes.c_void_p), ("scale", ctypes.c_float),
+                ("out", ctypes.c_void_p), ("out_dtype", ctypes.c_int32), ("lse_out", ctypes.c_void_p)]
+
+
+class LinearParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("max_len", ctypes.c_int32), ("Hq", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("q_stride_n", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+                ("kv_stride_n", ctypes.c_int64), ("kv_stride_h", ctypes.c_int64), ("decay", ctypes.c_void_p),
+                ("decay_rows", ctypes.c_int32), ("starts", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("state", ctypes.c_void_p), ("state_stride", ctypes.c_int64),
+                ("slots", ctypes.c_void_p), ("num_slots", ctypes.c_int32), ("state_out", ctypes.c_void_p),
+                ("state_out_stride", ctypes.c_int64), ("slots_out", ctypes.c_void_p), ("num_slots_out", ctypes.c_int32),
+                ("out", ctypes.c_void_p), ("out_dtype", ctypes.c_int32), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -169,6 +191,11 @@ def load_library():
         f.argtypes = [ctypes.POINTER(params), ctypes.c_void_p]
         s.restype = ctypes.c_size_t
         s.argtypes = [ctypes.POINTER(params)]
+    lib.sts_prompt_attn.restype = lib.sts_linear_attn.restype = ctypes.c_int
+    lib.sts_prompt_attn.argtypes = [ctypes.POINTER(PromptParams), ctypes.c_void_p]
+    lib.sts_linear_attn.argtypes = [ctypes.POINTER(LinearParams), ctypes.c_void_p]
+    lib.sts_linear_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.sts_linear_attn_workspace_bytes.argtypes = [ctypes.POINTER(LinearParams)]
     lib.sts_set_knob.restype = None
     lib.sts_set_knob.argtypes = [ctypes.c_int, ctypes.c_double]
     lib.sts_get_knob.restype = ctypes.c_double
@@ -208,7 +235,7 @@ class PreparedCall:
     """A library call with its parameter block built once: calling the object enqueues the call
     again on torch's current stream with the same pointers (the tensors it was built from are kept
     alive here). For serving loops that repeat a call on fixed buffers: the per-call cost on the host
-    is one ctypes call. Calls of sts_packed_attn and sts_window_attn have a workspace of their own and
+    is one ctypes call. Calls of sts_packed_attn, sts_window_attn, sts_prompt_attn and sts_linear_attn have a workspace of their own (or need none) and
     run on any stream, one at a time each; those of the other functions share the workspace of the stream they were
     prepared on, unless one was given, and belong on that stream."""
 
@@ -718,6 +745,120 @@ def sts_window_attn(q, k, v, scale, window: int, sinks: int = 0, seq_lens=None, 
                      block_table=_ptr(block_table), table_stride=ts, num_pages=pages, kv_stride_page=sp, k_new=_ptr(k_new), v_new=_ptr(v_new))
     return _run_with_workspace(lib.sts_window_attn, lib.sts_window_attn_workspace_bytes, p, "sts_window_attn", "attn", workspace, q.device, (out, lse),
                                (q, k, v, seq_lens, block_table, k_new, v_new), prepare)
+
+
+def _packed_rows(t, T, heads, d, dev, what):
+    """Strides of rows and heads of a packed tensor [T,heads,d]."""
+    import torch
+
+    assert t.device == dev and t.dtype == torch.bfloat16 and tuple(t.shape) == (T, heads, d), what
+    # (a stride that steps over nothing says nothing: the packed one stands for it)
+    n, h, one = t.stride()
+    assert one == 1, f"{what}: unit stride on the head's channels"
+    return (n if T > 1 else heads * d), (h if heads > 1 else d)
+
+
+def _kv_rows(k, v, dev):
+    """T, Hkv, d and the strides that k and v [T,Hkv,d] share."""
+    assert k.dim() == 3
+    T, Hkv, d = k.shape
+    strides = _packed_rows(k, T, Hkv, d, dev, "k")
+    assert _packed_rows(v, T, Hkv, d, dev, "v") == strides, "k and v have the same strides"
+    return T, Hkv, d, strides
+
+
+def _starts(starts, dev):
+    import torch
+
+    assert starts.device == dev and starts.dtype == torch.int32 and starts.dim() == 1 and starts.is_contiguous() and starts.shape[0] >= 1
+    return starts.shape[0] - 1
+
+
+def sts_prompt_attn(q, k, v, starts, scale, out=None, out_dtype=None, want_lse=True, lse_out=None, prepare=False):
+    """Causal attention over whole prompts that are packed one after the other: q [T,Hq,d], k/v [T,Hkv,d] bf16 (rows and heads strided
+    ok), starts [B+1] int32 (device): sequence b has the rows starts[b] .. starts[b+1]-1 -> (out [T,Hq,d], lse [Hq,T] or None). Rows of no
+    sequence stay as they are in `out` and `lse_out`. prepare=True returns a PreparedCall. See sts_prompt_attn in include/sts.h."""
+    import torch
+
+    lib = load_library()
+    dev = q.device
+    _current(dev)
+    T, Hkv, d, (kn, kh) = _kv_rows(k, v, dev)
+    Hq = q.shape[1]
+    qn, qh = _packed_rows(q, T, Hq, d, dev, "q")
+    B = _starts(starts, dev)
+    if out is None:
+        out = torch.empty(T, Hq, d, dtype=out_dtype or torch.bfloat16, device=dev)
+    assert out.device == dev and out.dtype in (torch.bfloat16, torch.float32) and out.is_contiguous() and tuple(out.shape) == (T, Hq, d)
+    if lse_out is None and want_lse:
+        lse_out = torch.empty(Hq, T, dtype=torch.float32, device=dev)
+    assert lse_out is None or (lse_out.device == dev and lse_out.dtype == torch.float32 and lse_out.is_contiguous() and tuple(lse_out.shape) == (Hq, T))
+    p = PromptParams(B, T, Hq, Hkv, d, _ptr(q), _ptr(k), _ptr(v), qn, qh, kn, kh, _ptr(starts), float(scale), _ptr(out),
+                     STS_BF16 if out.dtype == torch.bfloat16 else STS_F32, _ptr(lse_out))
+    if prepare:       # build once, launch many times (see PreparedCall)
+        return PreparedCall(lib.sts_prompt_attn, p, "sts_prompt_attn", (out, lse_out), (q, k, v, starts))
+    _check(lib.sts_prompt_attn(ctypes.byref(p), _stream()), "sts_prompt_attn")
+    return out, lse_out
+
+
+def _state_pool(pool, slots, B, Hkv, d, dev):
+    """Pointer, stride, slots' pointer and number of slots of a pool of states [slots,Hkv,d,d] fp32 (the first dimension strided ok)."""
+    import torch
+
+    if pool is None:
+        assert slots is None, "slots without a pool of states"
+        return None, 0, None, 0
+    assert pool.device == dev and pool.dtype == torch.float32 and tuple(pool.shape[1:]) == (Hkv, d, d) and (pool.shape[0] == 0 or pool[0].is_contiguous())
+    return _list_ptr(pool), pool.stride(0) if pool.shape[0] > 1 else Hkv * d * d, _per_batch(slots, B, dev), pool.shape[0]
+
+
+def sts_linear_attn(q, k, v, decay, scale=1.0, starts=None, lens=None, max_len=None, state=None, slots=None, state_out=None, slots_out=None,
+                    out=None, out_dtype=None, workspace=None, prepare=False):
+    """Linear attention with a decay for each head -> (out, state_out). Packed: q [T,Hq,d], k/v [T,Hkv,d] bf16 (rows and heads strided ok), starts
+    [B+1] int32 (device), max_len the longest sequence's rows if known (host; None: T). Or B sequences of the same length without starts: q
+    [B,n,Hq,d], k/v [B,n,Hkv,d], whose rows can be viewed as packed ones. decay: fp32 logarithms, [Hkv] or one per row and KV head. state and
+    state_out [slots,Hkv,d,d] fp32 pools, slots and slots_out [B] int32 (None: sequence b has slot b; slots_out None also where state_out is state
+    and slots is given: the same slots). lens [B]: rows that count. q None: states only, out is None. Rows of no sequence, and those behind
+    lens, stay as they are in `out`. prepare=True returns a PreparedCall. See sts_linear_attn in include/sts.h."""
+    import torch
+
+    lib = load_library()
+    dev = k.device
+    _current(dev)
+    shape = None
+    if starts is None:
+        assert k.dim() == 4 and v.dim() == 4 and k.shape == v.shape and (q is None or (q.dim() == 4 and q.shape[:2] == k.shape[:2]))
+        B, n = k.shape[:2]
+        shape = None if q is None else tuple(q.shape)
+        k, v, q = (None if t is None else t.view(B * n, *t.shape[2:]) for t in (k, v, q))
+        assert decay.dim() == 1 or tuple(decay.shape[:2]) == (B, n)
+        decay = decay if decay.dim() == 1 else decay.view(B * n, -1)
+        assert max_len is None, "max_len goes with starts"
+    else:
+        B = _starts(starts, dev)
+    T, Hkv, d, (kn, kh) = _kv_rows(k, v, dev)
+    Hq, qn, qh = Hkv, 0, 0
+    if q is not None:
+        Hq = q.shape[1]
+        qn, qh = _packed_rows(q, T, Hq, d, dev, "q")
+        shape = shape or (T, Hq, d)
+        if out is None:
+            out = torch.empty(shape, dtype=out_dtype or torch.bfloat16, device=dev)
+        assert out.device == dev and out.dtype in (torch.bfloat16, torch.float32) and out.is_contiguous() and tuple(out.shape) == shape
+    else:
+        assert out is None
+    assert decay.device == dev and decay.dtype == torch.float32 and decay.is_contiguous() and tuple(decay.shape) in ((Hkv,), (T, Hkv))
+    if state_out is not None and state_out is state and slots_out is None:
+        slots_out = slots
+    sp, ss, sl, sn = _state_pool(state, slots, B, Hkv, d, dev)
+    op, os_, ol, on = _state_pool(state_out, slots_out, B, Hkv, d, dev)
+    p = LinearParams(B=B, T=T, max_len=0 if max_len is None else _i32(max_len), Hq=Hq, Hkv=Hkv, d=d, q=None if q is None else _list_ptr(q), k=_ptr(k), v=_ptr(v),
+                     q_stride_n=qn, q_stride_h=qh, kv_stride_n=kn, kv_stride_h=kh, decay=_ptr(decay), decay_rows=1 if decay.dim() == 2 else 0,
+                     starts=_ptr(starts), lens=_per_batch(lens, B, dev), scale=float(scale), state=sp, state_stride=ss, slots=sl, num_slots=sn,
+                     state_out=op, state_out_stride=os_, slots_out=ol, num_slots_out=on, out=None if q is None else _list_ptr(out),
+                     out_dtype=STS_BF16 if out is None or out.dtype == torch.bfloat16 else STS_F32)
+    return _run_with_workspace(lib.sts_linear_attn, lib.sts_linear_attn_workspace_bytes, p, "sts_linear_attn", "linear", workspace, dev, (out, state_out),
+                               (q, k, v, decay, starts, lens, state, slots, slots_out), prepare)
 
 
 def sts_head_map(a_d, a_t, k: int, workspace=None):

@@ -1,0 +1,346 @@
+// Causal attention over whole prompts whose rows are packed one after the other (gfx950).
+//
+// A workgroup of four waves has 128 query rows of one sequence and KV head: row r of the sequence's L * G rows is position r / G of
+// the group's head r % G, so that the heads of a group share every K and V tile and a block spans 128 / G positions. It looks at the keys 0
+// .. of the sequence up to its last position, 64 at a time; K and V go to LDS, two tiles of each, the next on its way there while one is
+// worked on.
+//
+// Transposed, on v_mfma_f32_32x32x16_bf16: S^T = K Q^T gives lane (h, c) = (lane / 32, lane % 32) the scores of query c with keys 8 j + 4 h + i
+// (j = 0..3, i = 0..3) of each 32, two j of which are what it supplies as the B operand of O^T += V^T P^T for 16 keys: P stays in its lane,
+// and V's operand takes the keys in that order, out of V's rows in LDS by the transposing read.
+#include <float.h>
+
+#include "attn_util.h"
+#include "layers.h"
+
+namespace {
+
+constexpr int WAVES = 4, ROWS = STS_PROMPT_ROWS, TK = 64;
+static_assert(ROWS == 32 * WAVES, "");
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
+typedef __attribute__((address_space(3))) unsigned char *lds_ptr;
+typedef const __attribute__((address_space(3))) u32x4 *lds_u32x4;
+
+// Where 16-byte chunk c of row r lies in its row: K's reads (16 rows, one chunk each) and V's (4 rows, 64 bytes each) meet in no bank.
+template <int D> __device__ __forceinline__ int k_chunk(int r, int c) { return D == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7); }
+template <int D> __device__ __forceinline__ int v_chunk(int r, int c) { return D == 128 ? c ^ ((r & 3) << 2) : c ^ ((r & 2) << 1); }
+
+// bits 0 .. n - 1, none for n <= 0
+__device__ __forceinline__ uint64_t first_keys(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+template <int D>
+__global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kernel(const PromptArgs A) {
+  constexpr int KS = D / 16;             // contraction steps of S
+  constexpr int DT = D / 32;             // 32-channel tiles of O
+  constexpr int CH = D / 8;              // 16-byte chunks of a row
+  constexpr int NL = TK * CH / (64 * WAVES);       // chunks of K (and of V) per thread and tile
+  constexpr int RL = 64 / CH;                      // rows that a wave's load covers
+  __shared__ __attribute__((aligned(16))) u32x4 lds_k0[TK * CH], lds_k1[TK * CH], lds_v0[TK * CH], lds_v1[TK * CH];
+  __shared__ __attribute__((aligned(16))) uint32_t lds_odd[2][WAVES];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
+  // Blocks of one KV head next to each other on one die (workgroup i runs on die i % 8); late ones, which have more keys, first.
+  const int total = gridDim.x, x = blockIdx.x % STS_XCDS;
+  const int j = x * (total / STS_XCDS) + min(x, total % STS_XCDS) + blockIdx.x / STS_XCDS;
+  const int g = A.by_numbers.of(j), number = A.numbers - 1 - (j - g * A.numbers);
+  const PackedPiece piece = find_piece(A.seqs, number, [&](int begin) { return (int)((int64_t)begin * A.G / ROWS); });
+  const int L = piece.len, rows = L * A.G, row_0 = piece.index * ROWS;
+  if (piece.b < 0 || row_0 >= rows) return;
+
+  const int row_w = row_0 + wave * 32;
+  const bool ok = row_w + col < rows;
+  const int r = min(row_w + col, rows - 1);
+  const int p = A.by_group.of(r), head = g * A.G + r - p * A.G;          // this lane's query
+  const int b_lo = A.by_group.of(row_0), b_hi = A.by_group.of(min(row_0 + ROWS - 1, rows - 1));      // the workgroup's positions
+  const int w_lo = A.by_group.of(min(row_w, rows - 1));                                              // the wave's first
+  const int places = b_hi + 1, tiles = (places + TK - 1) / TK;           // keys that some query of the block sees
+
+  // ---- Q, as the B operand: channels 16 s + 8 h .. of query col. The scale's sign goes to Q.
+  const uint32_t q_keep = A.scale == 0.f ? 0u : 0xffffffffu, q_flip = A.scale < 0.f ? 0x80008000u : 0u;
+  const float sl2 = A.scale == 0.f ? 1.f : fabsf(A.scale_log2);
+  bf16x8 Q[KS];
+  {
+    const uint16_t *qp = A.q + (piece.begin + (int64_t)p) * A.q_stride_n + head * A.q_stride_h + 8 * h;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) Q[s] = __builtin_bit_cast(bf16x8, (*reinterpret_cast<const u32x4 *>(qp + 16 * s) & q_keep) ^ q_flip);
+  }
+
+  // ---- loads, straight to LDS: load m of a wave fills the 1 KB of rows (wave NL + m) RL .., lane by lane, so the permutation of a
+  // row's chunks is in what a lane asks for. Rows that no query of the block sees are read from the last one that some query does: their
+  // weight is 0, but 0 times what lies there may be NaN.
+  const int row0 = wave * NL * RL + lane / CH, slot0 = lane % CH;
+  const int64_t row_bytes = A.kv_stride_n * 2, from = (piece.begin * A.kv_stride_n + g * A.kv_stride_h) * 2;
+  const unsigned char *kbase = reinterpret_cast<const unsigned char *>(A.k) + from, *vbase = reinterpret_cast<const unsigned char *>(A.v) + from;
+  uint32_t k_off[NL], v_off[NL];
+#pragma unroll
+  for (int m = 0; m < NL; ++m) {
+    const int row = row0 + RL * m;
+    k_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * k_chunk<D>(row, slot0);
+    v_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * v_chunk<D>(row, slot0);
+  }
+  // K's or V's tile t (past the last: the last again, which nobody reads)
+  auto load = [&](int t, const unsigned char *base, u32x4 *to, bool is_v) {
+    const int n0 = min(t, tiles - 1) * TK;
+    u32x4 *const mine = to + wave * NL * 64;
+    const __amdgpu_buffer_rsrc_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(base + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
+    if (n0 + TK <= places) {
+#pragma unroll
+      for (int m = 0; m < NL; ++m) __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(mine + 64 * m), 16, (int)(is_v ? v_off[m] : k_off[m]), 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int m = 0; m < NL; ++m) {
+        const int row = row0 + RL * m, chunk = is_v ? v_chunk<D>(row, slot0) : k_chunk<D>(row, slot0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(mine + 64 * m), 16, (int)((uint32_t)min(row, places - 1 - n0) * (uint32_t)row_bytes + 16 * chunk), 0, 0, 0);
+      }
+    }
+  };
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 acc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
+
+  // Where the lane reads: K's chunk 2 s + h of row 32 kt + col, and V's operand for channels 32 dt .. and keys 16 s .., two transposed
+  // reads of keys 16 s + 4 h + 0..3 and 8 further on. Both are one address with a few bits flipped by s or dt, plus a constant.
+  const int k_lane = col * CH * 16 + 16 * k_chunk<D>(col, h);
+  const int t_row = 4 * h + ((lane & 15) >> 2), t_col = (lane & 16) + 4 * (lane & 3);       // within 16 keys, 32 channels
+  const int v_lane = (t_row * CH + v_chunk<D>(t_row, t_col >> 3)) * 16 + (t_col & 7) * 2;
+  auto v_operand = [&](const u32x4 *v, int at, int dt, int s) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const u32x2 v2 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_ptr)v + (at ^ (64 * dt)) + (16 * s + 8 * e) * CH * 16)));
+      w[2 * e] = v2[0];
+      w[2 * e + 1] = v2[1];
+    }
+    return w;
+  };
+
+  // S of one tile
+  auto product = [&](const u32x4 *k, f32x16 (&S)[2]) {
+    int k_at = k_lane;
+    asm("" : "+v"(k_at));                        // (what comes of it is made anew in every tile, not kept in registers)
+    const f32x16 zero = {};
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const bf16x8 Ka = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)k + (k_at ^ (32 * s)) + 32 * kt * CH * 16));
+        S[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Ka, Q[s], s ? S[kt] : zero, 0, 0, 0);
+      }
+  };
+  // keys behind the query score -inf
+  auto hide = [&](int t, f32x16 (&S)[2]) {
+    const uint64_t seen = first_keys(p + 1 - t * TK) >> (4 * h);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      const int word = (int)(uint32_t)(seen >> (32 * kt));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(word, (i & 3) + 8 * (i >> 2), 1);
+        const float s = S[kt][i];
+        S[kt][i] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, s) & keep) | (0xff800000u & ~keep));
+      }
+    }
+  };
+  auto highest = [&](const f32x16 (&S)[2]) {
+    float m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = top(S[0][i], S[1][i]);
+#pragma unroll
+    for (int i = 4; i < 16; ++i) m[i & 3] = top(m[i & 3], top(S[0][i], S[1][i]));
+    return sl2 * top(top(m[0], m[1]), top(m[2], m[3]));
+  };
+  // the running maximum takes in a tile's; both halves of the wave hold half of a query's scores
+  auto raise = [&](float mine) {
+    if (__builtin_amdgcn_ballot_w64(mine > m_run) != 0) {
+      const uint32_t w = __builtin_bit_cast(uint32_t, mine);
+      const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+      const uint32_t q0 = q[0], q1 = q[1];
+      const float m_new = fmaxf(m_run, top(__builtin_bit_cast(float, q0), __builtin_bit_cast(float, q1)));
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
+    }
+  };
+  // exp(S - m), as the B operands of the second product (bf16, half a step, 2^-8 of each), and their sum in fp32
+  auto weights = [&](const f32x16 (&S)[2], u32x4 (&P)[4]) {
+    const float m_ref = m_run == -INFINITY ? 0.f : m_run;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * e], sl2, -m_ref));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * e + 1], sl2, -m_ref));
+        sum[e] += p0 + p1;
+        P[s][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+      }
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+  // A tile that not every query of the block sees whole: has it a value that is no number, or infinite? Each wave looks through the rows
+  // that it asked for, in slot `at`; the answer is there after the next barrier.
+  auto partly_seen = [&](int t) { return t * TK + TK - 1 > b_lo; };
+  auto look_through = [&](const u32x4 *v, int at) {
+    float z[4] = {0.f, 0.f, 0.f, 0.f};            // sums of 0 times the values: 0, or no number
+    const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
+#pragma unroll
+    for (int m = 0; m < NL; ++m) {
+      const u32x4 w = *(lds_u32x4)((lds_ptr)v + 16 * (lane + 64 * (wave * NL + m)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t two = w[e];
+        z[e] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), none, z[e], false);
+      }
+    }
+    const float all = (z[0] + z[1]) + (z[2] + z[3]);
+    const bool mine = __builtin_amdgcn_ballot_w64(all != 0.f) != 0;       // (true for what is no number)
+    if (lane == 0) lds_odd[at][wave] = mine;
+  };
+  auto odd_values = [&](int at) {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    uint32_t any = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) any |= lds_odd[at][w];
+    return __builtin_amdgcn_readfirstlane((int)any) != 0;
+  };
+  // does a query of the wave not see all keys of tile t?
+  auto masked = [&](int t) { return t * TK + TK - 1 > w_lo; };
+
+  // ---- The next tile's scores are worked out while this one's weights are: matrix and vector instructions of one wave, which do
+  // not wait for each other. K is a tile ahead of V.
+  // What was asked for has come, and what was read is in registers: the tiles change hands.
+  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  bool later = false;              // tiles left for the end: see below
+  {
+    f32x16 S[2];
+    load(0, kbase, lds_k0, false);
+    load(0, vbase, lds_v0, true);
+    load(1, kbase, lds_k1, false);
+    arrived();
+    product(lds_k0, S);
+    if (masked(0)) hide(0, S);
+    raise(highest(S));
+    auto step = [&](int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
+      arrived();
+      load(t + 2, kbase, k_free, false);
+      load(t + 1, vbase, v_free, true);
+      bool odd = false;
+      if (partly_seen(t)) {
+        look_through(v, t & 1);
+        odd = odd_values(t & 1);
+      }
+      f32x16 N[2];
+      u32x4 P[4];
+      product(k_next, N);
+      const float sum = weights(S, P);
+      if (!odd) {
+        l_run += sum;
+        int v_at = v_lane;
+        asm("" : "+v"(v_at));
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v, v_at, dt, s)), __builtin_bit_cast(bf16x8, P[s]), acc[dt], 0, 0, 0);
+      }
+      later |= odd;
+      if (t + 1 < tiles) {
+        if (masked(t + 1)) hide(t + 1, N);
+        raise(highest(N));
+      }
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) S[kt] = N[kt];
+    };
+    for (int t = 0;; t += 2) {
+      step(t, lds_k1, lds_k0, lds_v0, lds_v1);
+      if (t + 1 >= tiles) break;
+      step(t + 1, lds_k0, lds_k1, lds_v1, lds_v0);
+      if (t + 2 >= tiles) break;
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);              // all that was asked for has come
+    // What is infinite or no number must not reach queries that do not see it, and 0 times it is not 0: such tiles come last, key
+    // by key, and a key's row is taken in only where it is seen.
+    if (__syncthreads_or(later)) {
+      for (int t = 0; t < tiles; ++t) {
+        if (!partly_seen(t)) continue;
+        arrived();
+        load(t, kbase, lds_k0, false);
+        load(t, vbase, lds_v0, true);
+        arrived();
+        look_through(lds_v0, 0);
+        if (!odd_values(0)) continue;
+        u32x4 P[4];
+        product(lds_k0, S);
+        hide(t, S);
+        l_run += weights(S, P);
+        const uint64_t seen = first_keys(p + 1 - t * TK);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          for (int key = 0; key < 16; ++key) {
+            u32x4 own;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
+              own[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
+            }
+            const bool see = (seen >> (16 * s + key)) & 1u;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+              const f32x16 zero = {};
+              const f32x16 z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(lds_v0, v_lane, dt, s) & own),
+                                                                       __builtin_bit_cast(bf16x8, P[s] & own), zero, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) acc[dt][i] += see ? z[i] : 0.f;
+              __builtin_amdgcn_sched_barrier(0);         // (one product's registers at a time)
+            }
+          }
+      }
+    }
+  }
+
+  // ---- out
+  {
+    const uint32_t w = __builtin_bit_cast(uint32_t, l_run);
+    const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    const uint32_t q0 = q[0], q1 = q[1];
+    l_run = __builtin_bit_cast(float, q0) + __builtin_bit_cast(float, q1);
+  }
+  if (!ok) return;
+  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+  const size_t row = (size_t)piece.begin + p, at = (row * A.Hq + head) * D + 4 * h;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x4 o = {acc[dt][4 * e] * inv, acc[dt][4 * e + 1] * inv, acc[dt][4 * e + 2] * inv, acc[dt][4 * e + 3] * inv};
+      if (A.out_dtype == STS_F32) {
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 32 * dt + 8 * e) = o;
+      } else {
+        const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[0], o[1]}), bf16x2)),
+                         __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[2], o[3]}), bf16x2))};
+        *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at + 32 * dt + 8 * e) = w;
+      }
+    }
+  // (a row whose sum is no number has the logarithm -inf, as everywhere in the library)
+  if (A.lse_out && h == 0) A.lse_out[(size_t)head * A.seqs.T + row] = l_run > 0.f ? (m_run + __builtin_amdgcn_logf(l_run)) * 0.69314718055994530942f : -INFINITY;
+}
+
+}  // namespace
+
+hipError_t launch_prompt_attn(const PromptArgs &a, int d, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.numbers * a.Hkv)), block(64 * WAVES);
+  if (d == 128) STS_LAUNCH(prompt_attn_kernel<128>, grid, block, 0, s, a);
+  else STS_LAUNCH(prompt_attn_kernel<64>, grid, block, 0, s, a);
+  return sts_take_launch_status();
+}

@@ -1,0 +1,462 @@
+// Linear attention with a decay for each head (gfx950): per KV head a state S of d x d numbers in fp32, and
+//     S_i = exp(g_i) S_(i-1) + k_i v_i^T,    out_i = scale q_i^T S_i.
+//
+// The recurrent form (few rows of a sequence) does just that. A workgroup has 32 columns of a state, a thread 4 of them in d / 32 rows; the state
+// is read once, stays in registers for all rows and is written once. What bounds it: memory, 8 bytes for every number of the state.
+//
+// The chunked form (prompts) takes 32 rows at a time. With c_i the sum of g over the chunk's rows up to i,
+//     out_i = scale (exp(c_i) q_i^T S + sum_(j <= i) exp(c_i - c_j) (q_i . k_j) v_j),    S' = exp(c_32) S + sum_j exp(c_32 - c_j) k_j v_j^T.
+// A wave has 32 columns of the state (and of out) in the accumulators of v_mfma_f32_32x32x16_bf16 and works out the chunk's 32 x 32
+// products q . k by itself, so that these pass from accumulator to operand in their lane, as the state does: nothing goes through LDS but
+// rows of Q, K and V. Long sequences are cut into segments: one kernel sums up what each segment adds to the state, one
+// adds these up along the sequence, and a third starts every segment from the state before it.
+#include "attn_util.h"
+#include "layers.h"
+
+namespace {
+
+constexpr int C = STS_LINEAR_CHUNK;
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr double LOG2E_64 = 1.44269504088896340736;
+static_assert(C == 32, "");
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
+typedef __attribute__((address_space(3))) unsigned char *lds_ptr;
+typedef const __attribute__((address_space(3))) u32x4 *lds_u32x4;
+
+// 2^x in 64 bits (to some 1e-14), for x <= 1000: the series of exp on [-ln(2) / 2, ln(2) / 2]
+__device__ __forceinline__ double exp2_64(double x) {
+  const double n = __builtin_rint(x), r = (x - n) * 0.69314718055994530942;
+  double p = 1.0 / 39916800.0;
+  p = __builtin_fma(p, r, 1.0 / 3628800.0);
+  p = __builtin_fma(p, r, 1.0 / 362880.0);
+  p = __builtin_fma(p, r, 1.0 / 40320.0);
+  p = __builtin_fma(p, r, 1.0 / 5040.0);
+  p = __builtin_fma(p, r, 1.0 / 720.0);
+  p = __builtin_fma(p, r, 1.0 / 120.0);
+  p = __builtin_fma(p, r, 1.0 / 24.0);
+  p = __builtin_fma(p, r, 1.0 / 6.0);
+  p = __builtin_fma(p, r, 0.5);
+  p = __builtin_fma(p, r, 1.0);
+  p = __builtin_fma(p, r, 1.0);
+  return x < -1000.0 ? 0.0 : __builtin_ldexp(p, (int)n);
+}
+
+// where the state of sequence b begins, or NULL: there is none (a slot outside the pool stands for none)
+__device__ __forceinline__ const float *state_in(const LinearArgs &A, int b) {
+  if (!A.state) return nullptr;
+  const int slot = A.slots ? A.slots[b] : b;
+  return slot < 0 || slot >= A.num_slots ? nullptr : A.state + slot * A.state_stride;
+}
+__device__ __forceinline__ float *state_out(const LinearArgs &A, int b) {
+  if (!A.state_out) return nullptr;
+  const int slot = A.slots_out ? A.slots_out[b] : b;
+  return slot < 0 || slot >= A.num_slots_out ? nullptr : A.state_out + slot * A.state_out_stride;
+}
+// the rows of a sequence that count
+__device__ __forceinline__ int rows_of(const LinearArgs &A, int b, int len) { return min(A.lens ? min(max(A.lens[b], 0), len) : len, A.max_len); }
+
+__device__ __forceinline__ float of_bf16(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
+
+// ---------------------------------------------------------------------------------------------- recurrent form
+template <int N> struct Words { uint32_t w[N]; };
+
+template <int D>
+__global__ void __launch_bounds__(256) linear_step_kernel(const LinearArgs A) {
+  constexpr int RK = D / 32;              // rows of the state per thread
+  constexpr int SLICES = D / 32, MAX = STS_LINEAR_STEP, HEADS = 4;      // heads that are worked on at once
+  __shared__ uint16_t lds_k[MAX][D], lds_v[MAX][32];
+  __shared__ float lds_f[MAX];
+  __shared__ __attribute__((aligned(16))) float lds_o[2][HEADS][4][32];
+
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const int unit = blockIdx.x / SLICES, slice = blockIdx.x % SLICES;
+  const int b = A.by_heads.of(unit), g = unit - b * A.Hkv;
+  int begin, len;
+  seq_rows(A.seqs, b, begin, len);
+  const int n = min(rows_of(A, b, len), MAX);
+  const int col = 32 * slice + 4 * (tid & 7), row = RK * (tid >> 3);
+  f32x4 S[RK];
+  const float *from = state_in(A, b);
+  const size_t head_at = (size_t)g * D * D;
+#pragma unroll
+  for (int r = 0; r < RK; ++r) S[r] = from ? *reinterpret_cast<const f32x4 *>(from + head_at + (row + r) * D + col) : f32x4{0.f, 0.f, 0.f, 0.f};
+  // the rows of K and V that are needed, and the decays
+  for (int i = tid; i < n * (D / 8); i += 256) {
+    const int t = i / (D / 8), c = i % (D / 8);
+    *reinterpret_cast<u32x4 *>(&lds_k[t][8 * c]) = *reinterpret_cast<const u32x4 *>(A.k + (begin + (int64_t)t) * A.kv_stride_n + g * A.kv_stride_h + 8 * c);
+  }
+  for (int i = tid; i < n * 4; i += 256)
+    *reinterpret_cast<u32x4 *>(&lds_v[i / 4][8 * (i % 4)]) =
+        *reinterpret_cast<const u32x4 *>(A.v + (begin + (int64_t)(i / 4)) * A.kv_stride_n + g * A.kv_stride_h + 32 * slice + 8 * (i % 4));
+  if (tid < n) lds_f[tid] = (float)exp2_64((double)A.decay[A.decay_rows ? (begin + (size_t)tid) * A.Hkv + g : g] * LOG2E_64);
+  __syncthreads();
+
+  int parity = 0;
+  for (int t = 0; t < n; ++t) {
+    const float f = lds_f[t];
+    float kk[RK];
+#pragma unroll
+    for (int r = 0; r < RK; ++r) kk[r] = of_bf16(lds_k[t][row + r]);
+    const f32x4 v = {of_bf16(lds_v[t][4 * (tid & 7)]), of_bf16(lds_v[t][4 * (tid & 7) + 1]), of_bf16(lds_v[t][4 * (tid & 7) + 2]), of_bf16(lds_v[t][4 * (tid & 7) + 3])};
+#pragma unroll
+    for (int r = 0; r < RK; ++r) S[r] = S[r] * f + v * kk[r];
+    if (!A.out) continue;
+    for (int h0 = 0; h0 < A.G; h0 += HEADS) {
+      const uint16_t *q = A.q + (begin + (int64_t)t) * A.q_stride_n + row;
+      Words<RK / 2> w[HEADS];
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h) w[h] = *reinterpret_cast<const Words<RK / 2> *>(q + (g * A.G + min(h0 + h, A.G - 1)) * A.q_stride_h);
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h) {
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < RK; ++r) o += S[r] * of_bf16(r % 2 ? w[h].w[r / 2] >> 16 : w[h].w[r / 2] & 0xffffu);
+        // the wave's eight groups of rows: lanes 8, 16 and 32 apart
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          o[e] += __shfl_xor(o[e], 8, 64);
+          o[e] += __shfl_xor(o[e], 16, 64);
+          o[e] += __shfl_xor(o[e], 32, 64);
+        }
+        if ((tid & 63) < 8) *reinterpret_cast<f32x4 *>(&lds_o[parity][h][wave][4 * (tid & 7)]) = o;
+      }
+      __syncthreads();
+      if (tid < 32 * HEADS && h0 + tid / 32 < A.G) {
+        const int h = tid / 32, c = tid % 32;
+        const float o = A.scale * ((lds_o[parity][h][0][c] + lds_o[parity][h][1][c]) + (lds_o[parity][h][2][c] + lds_o[parity][h][3][c]));
+        const size_t at = ((begin + (size_t)t) * A.Hq + g * A.G + h0 + h) * D + 32 * slice + c;
+        if (A.out_dtype == STS_F32) static_cast<float *>(A.out)[at] = o;
+        else static_cast<__bf16 *>(A.out)[at] = (__bf16)o;
+      }
+      parity ^= 1;       // (the next results go elsewhere; those after them come behind the next barrier)
+    }
+  }
+  float *to = state_out(A, b);
+  if (!to) return;
+#pragma unroll
+  for (int r = 0; r < RK; ++r) *reinterpret_cast<f32x4 *>(to + head_at + (row + r) * D + col) = S[r];
+}
+
+// ------------------------------------------------------------------------------------------------ chunked form
+// Where 16-byte chunk c of row r lies in its row: neither reads of one chunk of 16 rows nor transposing reads of 64 bytes of 4 rows meet in a
+// bank.
+template <int D> __device__ __forceinline__ int place(int r, int c) {
+  return D == 128 ? c ^ ((r & 3) << 2 | (r >> 2 & 3)) : c ^ ((r >> 1 & 1) << 2 | (r >> 2 & 3));
+}
+
+// sums over the lanes of each half up to the lane's own (DPP: within rows of 16, then the first row's total to the second)
+__device__ __forceinline__ float scan32(float x) {
+  auto add = [&](auto ctrl, auto rows) {
+    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, true));
+  };
+  add(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());      // row_shr:1
+  add(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+  add(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+  add(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+  const float first = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(((threadIdx.x & 32) | 15) << 2, __builtin_bit_cast(int, x)));
+  return threadIdx.x & 16 ? x + first : x;
+}
+
+// OUT: results, from the state before the segment; else what the segment adds to the state (or, of a sequence with one segment, its
+// state)
+template <int D, bool OUT>
+__global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs A) {
+  constexpr int NW = D / 32;             // waves, each with 32 columns of the state
+  constexpr int KS = D / 16, MT = D / 32, CH = D / 8;
+  constexpr int NL = C * CH / (64 * NW), RL = 64 / CH;      // loads of a wave for 32 rows, rows that each covers
+  __shared__ __attribute__((aligned(16))) u32x4 lds_k[C * CH], lds_v[C * CH], lds_q[OUT ? C * CH : 1];
+  __shared__ __attribute__((aligned(16))) float lds_c[NW][2][C];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
+  const int number = A.by_heads.of(blockIdx.x), g = blockIdx.x - number * A.Hkv;
+  const PackedPiece piece = find_piece(A.seqs, number, [&](int begin) { return A.by_segment.of(begin); });
+  if (piece.b < 0) return;
+  const int len = rows_of(A, piece.b, piece.len), first = piece.index * A.segment;
+  const int segments = max((len + A.segment - 1) / A.segment, 1);
+  if (piece.index >= segments) return;
+  const bool last = piece.index == segments - 1;
+  if (!OUT && A.out && last) return;                 // (the results' kernel brings the last segment's state)
+  const int rows = min(A.segment, len - first), begin = piece.begin + first;
+
+  // ---- the state: lane (h, col) has column 32 wave + col, in element 4 j + i of tile m the row 32 m + 16 (j / 2) + 8 h + 4 (j % 2) + i
+  f32x16 S[MT];
+  const size_t part_at = ((size_t)number * A.Hkv + g) * D * D;
+  const float *from = segments > 1 ? (OUT ? A.part + part_at : nullptr) : state_in(A, piece.b);
+  if (segments == 1 && from) from += (size_t)g * D * D;
+  const int s_at = 8 * h * D + 32 * wave + col;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) S[m][e] = from ? from[s_at + (32 * m + 16 * (e >> 3) + (e & 7)) * D] : 0.f;
+
+  // ---- loads, straight to LDS, rows behind the last from the last
+  const int row0 = wave * NL * RL + lane / CH, slot0 = lane % CH;
+  auto load = [&](int chunk, const uint16_t *base, int64_t stride, u32x4 *to) {
+    const __amdgpu_buffer_rsrc_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(base + (begin + (int64_t)chunk * C) * stride), 0, 0xffffffff, 0x00027000);
+    const int most = rows - 1 - chunk * C;
+#pragma unroll
+    for (int m = 0; m < NL; ++m) {
+      const int row = row0 + RL * m;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(to + (wave * NL + m) * 64), 16, (int)((uint32_t)min(row, most) * (uint32_t)(stride * 2) + 16 * place<D>(row, slot0)), 0, 0, 0);
+    }
+  };
+  const uint16_t *k = A.k + g * A.kv_stride_h, *v = A.v + g * A.kv_stride_h;
+  // what was asked for has come, and what was read is in registers
+  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+  // ---- reads: chunk 2 s + h of row col; by the transposing read rows 16 s + 4 h + 0..3 and 8 further on of 32 channels. For K the middle two
+  // of each 16 channels' fours change places: then the state's rows lie in a lane's accumulators in the order of an operand.
+  const int r_lane = col * CH * 16 + 16 * place<D>(col, h);
+  const int t_row = 4 * h + ((lane & 15) >> 2), t_four = lane & 3;
+  const int v_chan = (lane & 16) + 4 * t_four, k_chan = (lane & 16) + 4 * ((t_four & 1) << 1 | t_four >> 1);
+  auto transposed = [&](const u32x4 *tile, int chan, int s) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = 16 * s + 8 * e + t_row;
+      const u32x2 two = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_ptr)tile + (row * CH + place<D>(row, chan >> 3)) * 16 + (chan & 7) * 2)));
+      w[2 * e] = two[0];
+      w[2 * e + 1] = two[1];
+    }
+    return __builtin_bit_cast(bf16x8, w);
+  };
+
+  const float fixed = A.decay_rows ? 0.f : A.decay[g] * LOG2E;
+  double all = 0.0, drift = 1.0;
+  const int chunks = (rows + C - 1) / C;
+  for (int chunk = 0; chunk < chunks; ++chunk) {
+    const int n = min(rows - chunk * C, C);
+    arrived();
+    load(chunk, k, A.kv_stride_n, lds_k);
+    load(chunk, v, A.kv_stride_n, lds_v);
+    if (OUT) load(chunk, A.q + (g * A.G) * A.q_stride_h, A.q_stride_n, lds_q);
+    // ---- decays, in powers of two: c = sum up to the row `col`, and sums over the rows behind the lane's sixteen rows 8 j + 4 h + i
+    float gate = 0.f;
+    if (col < n) gate = A.decay_rows ? A.decay[(begin + (size_t)chunk * C + col) * A.Hkv + g] * LOG2E : fixed;
+    if (gate < -150.f) gate = -150.f;        // (2^-150 is 0 in fp32; an infinite sum would have no differences)
+    const float c = scan32(gate);
+    const float after = scan32(col ? __shfl(gate, (threadIdx.x & 32) | (32 - col), 64) : 0.f);      // of rows 32 - col .. 31
+    lds_c[wave][0][col] = c;
+    lds_c[wave][1][31 - col] = after;
+    float near[16], left[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int s = 8 * (e >> 2) + 4 * h + (e & 3);
+      near[e] = __builtin_amdgcn_exp2f(c - lds_c[wave][0][s]);
+      left[e] = s < n ? __builtin_amdgcn_exp2f(lds_c[wave][1][s]) : 0.f;
+    }
+    const float c_end = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c), 31));
+    const float e_t = __builtin_amdgcn_exp2f(c);
+    arrived();
+    bf16x8 V[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) V[s] = transposed(lds_v, 32 * wave + v_chan, s);
+
+    if constexpr (OUT) {
+      // Has the chunk a value that is infinite or no number? Rows before it do not see it, but 0 times it is not 0.
+      float z = 0.f;
+      const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t two = __builtin_bit_cast(u32x4, V[s])[e];
+          z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), none, z, false);
+        }
+      const bool odd = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
+      for (int hd = 0; hd < A.G; ++hd) {
+        const int head = g * A.G + hd;
+        if (hd) {
+          arrived();
+          load(chunk, A.q + head * A.q_stride_h, A.q_stride_n, lds_q);
+          arrived();
+        }
+        bf16x8 Q[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds_q + (r_lane ^ (32 * s))));
+        // X^T = K Q^T: row q . k of keys 8 j + 4 h + i and query col; O^T = S^T Q^T. The state enters the product as bf16 (half a step, 2^-8 of
+        // each number; the state itself stays as it is)
+        f32x16 X = {}, O = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) X = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds_k + (r_lane ^ (32 * s)))), Q[s], X, 0, 0, 0);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            u32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{S[m][8 * s + 2 * e], S[m][8 * s + 2 * e + 1]}), bf16x2));
+            O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), Q[2 * m + s], O, 0, 0, 0);
+          }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) O[e] *= e_t;
+        // the weights, as bf16 (half a step, 2^-8 of each), none for keys behind the query, whatever their product is
+        bf16x8 P[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          u32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            f32x2 x;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
+              x[i] = key <= col ? near[at] * X[at] : 0.f;
+            }
+            w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+          }
+          P[s] = __builtin_bit_cast(bf16x8, w);
+        }
+        if (!odd) {
+#pragma unroll
+          for (int s = 0; s < 2; ++s) O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], O, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            for (int key = 0; key < 16; ++key) {      // key by key, and a row is taken in only where it is seen
+              u32x4 own;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
+                own[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
+              }
+              const f32x16 zero = {};
+              const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, V[s]) & own),
+                                                                       __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, P[s]) & own), zero, 0, 0, 0);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) O[e] += 16 * s + key <= col ? x[e] : 0.f;
+            }
+        }
+        if (col < n) {
+          const size_t at = ((begin + (size_t)chunk * C + col) * A.Hq + head) * D + 32 * wave + 4 * h;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x4 o = {O[4 * j] * A.scale, O[4 * j + 1] * A.scale, O[4 * j + 2] * A.scale, O[4 * j + 3] * A.scale};
+            if (A.out_dtype == STS_F32) {
+              *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 8 * j) = o;
+            } else {
+              const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[0], o[1]}), bf16x2)),
+                               __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[2], o[3]}), bf16x2))};
+              *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at + 8 * j) = w;
+            }
+          }
+        }
+      }
+    }
+
+    // ---- The state behind the chunk. Its decay's rounding would add up over a long sequence (always the same one, where the decay is fixed): what
+    // a rounded factor is off by goes into the next.
+    all += c_end;
+    const double exact = exp2_64((double)c_end) * drift;
+    const float f = (float)exact;
+    drift = f > 1e-30f ? 1.0 + (exact - (double)f) * (double)(1.f / f) : 1.0;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) S[m][e] *= f;
+    // V with its weights as the sum of three bf16 numbers, which hold an fp32's bits: the products enter the state as exactly as in fp32
+    bf16x8 W[3][2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const u32x4 two = __builtin_bit_cast(u32x4, V[s]);
+      u32x4 w[3];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f32x2 x = {left[8 * s + 2 * e] * __builtin_bit_cast(float, two[e] << 16), left[8 * s + 2 * e + 1] * __builtin_bit_cast(float, two[e] & 0xffff0000u)};
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          const uint32_t top2 = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+          w[i][e] = top2;
+          x[0] -= __builtin_bit_cast(float, top2 << 16);
+          x[1] -= __builtin_bit_cast(float, top2 & 0xffff0000u);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 3; ++i) W[i][s] = __builtin_bit_cast(bf16x8, w[i]);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const bf16x8 K = transposed(lds_k, 32 * m + k_chan, s);
+#pragma unroll
+        for (int i = 2; i >= 0; --i) S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K, W[i][s], S[m], 0, 0, 0);
+      }
+  }
+
+  float *to;
+  if (segments > 1 && !OUT) {
+    to = A.part + part_at;
+    if (threadIdx.x == 0) A.part_log[(size_t)number * A.Hkv + g] = all;
+  } else {
+    if (!last) return;
+    to = state_out(A, piece.b);
+    if (!to) return;
+    to += (size_t)g * D * D;
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) to[s_at + (32 * m + 16 * (e >> 3) + (e & 7)) * D] = S[m][e];
+}
+
+// Along each sequence of several segments: the state before every segment takes the place of what the segment adds. A thread has four numbers.
+template <int D>
+__global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
+  constexpr int PER = D * D / 1024;      // workgroups for a state
+  const int unit = blockIdx.x / PER, at = 4 * ((blockIdx.x % PER) * 256 + threadIdx.x);
+  const int b = A.by_heads.of(unit), g = unit - b * A.Hkv;
+  int begin, len;
+  seq_rows(A.seqs, b, begin, len);
+  len = rows_of(A, b, len);
+  const int segments = (len + A.segment - 1) / A.segment;
+  if (segments < 2) return;
+  const float *from = state_in(A, b);
+  f32x4 S = from ? *reinterpret_cast<const f32x4 *>(from + (size_t)g * D * D + at) : f32x4{0.f, 0.f, 0.f, 0.f};
+  const size_t number = (size_t)A.by_segment.of(begin) + b;
+  for (int i = 0; i < segments; ++i) {
+    const bool last = i == segments - 1;
+    float *part = A.part + ((number + i) * A.Hkv + g) * D * D + at;
+    const float f = last && A.out ? 0.f : (float)exp2_64(A.part_log[(number + i) * A.Hkv + g]);
+    const f32x4 own = last && A.out ? f32x4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f32x4 *>(part);
+    *reinterpret_cast<f32x4 *>(part) = S;
+    S = S * f + own;
+  }
+  if (A.out) return;
+  float *to = state_out(A, b);
+  if (to) *reinterpret_cast<f32x4 *>(to + (size_t)g * D * D + at) = S;
+}
+
+}  // namespace
+
+hipError_t launch_linear_step(const LinearArgs &a, int d, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.seqs.B * a.Hkv * (d / 32))), block(256);
+  if (d == 128) STS_LAUNCH(linear_step_kernel<128>, grid, block, 0, s, a);
+  else STS_LAUNCH(linear_step_kernel<64>, grid, block, 0, s, a);
+  return sts_take_launch_status();
+}
+
+hipError_t launch_linear_sums(const LinearArgs &a, int d, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.numbers * a.Hkv)), block(2 * d);
+  if (d == 128) STS_LAUNCH((linear_chunk_kernel<128, false>), grid, block, 0, s, a);
+  else STS_LAUNCH((linear_chunk_kernel<64, false>), grid, block, 0, s, a);
+  return sts_take_launch_status();
+}
+
+hipError_t launch_linear_chunks(const LinearArgs &a, int d, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.numbers * a.Hkv)), block(2 * d);
+  if (d == 128) STS_LAUNCH((linear_chunk_kernel<128, true>), grid, block, 0, s, a);
+  else STS_LAUNCH((linear_chunk_kernel<64, true>), grid, block, 0, s, a);
+  return sts_take_launch_status();
+}
+
+hipError_t launch_linear_carry(const LinearArgs &a, int d, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.seqs.B * a.Hkv * (d * d / 1024))), block(256);
+  if (d == 128) STS_LAUNCH(linear_carry_kernel<128>, grid, block, 0, s, a);
+  else STS_LAUNCH(linear_carry_kernel<64>, grid, block, 0, s, a);
+  return sts_take_launch_status();
+}
