@@ -25,6 +25,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
 typedef __attribute__((address_space(3))) unsigned char *lds_ptr;
 typedef const __attribute__((address_space(3))) u32x4 *lds_u32x4;
+typedef __attribute__((address_space(3))) float *lds_f32;
 
 // 2^x in 64 bits (to some 1e-14), for x <= 1000: the series of exp on [-ln(2) / 2, ln(2) / 2]
 __device__ __forceinline__ double exp2_64(double x) {
@@ -161,14 +162,17 @@ __device__ __forceinline__ float scan32(float x) {
 }
 
 // OUT: results, from the state before the segment; else what the segment adds to the state (or, of a sequence with one segment, its
-// state)
-template <int D, bool OUT>
+// state). GATES: a decay for every row; GROUP: several heads to a KV head
+template <int D, bool OUT, bool GATES, bool GROUP>
 __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs A) {
   constexpr int NW = D / 32;             // waves, each with 32 columns of the state
   constexpr int KS = D / 16, MT = D / 32, CH = D / 8;
   constexpr int NL = C * CH / (64 * NW), RL = 64 / CH;      // loads of a wave for 32 rows, rows that each covers
-  __shared__ __attribute__((aligned(16))) u32x4 lds_k[C * CH], lds_v[C * CH], lds_q[OUT ? C * CH : 1];
-  __shared__ __attribute__((aligned(16))) float lds_c[NW][2][C];
+  // Two chunks of K, V, the first head's Q, the decays and (two numbers for each row and wave) their sums; the other heads' Q take turns in two
+  // more places. Arrays of their own, so that the compiler can tell the loads that fill one from the reads of another, and the sums are in the chunk's
+  // since a read of an array that no load fills waits for all loads.
+  constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, AT_G = (OUT ? 3 : 2) * TILE, AT_C = AT_G + NW * 16, ALL = GATES ? AT_C + NW * 16 : AT_G;
+  __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_q0[GROUP ? TILE : 1], lds_q1[GROUP ? TILE : 1];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
@@ -180,18 +184,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   if (piece.index >= segments) return;
   const bool last = piece.index == segments - 1;
   if (!OUT && A.out && last) return;                 // (the results' kernel brings the last segment's state)
-  const int rows = min(A.segment, len - first), begin = piece.begin + first;
-
-  // ---- the state: lane (h, col) has column 32 wave + col, in element 4 j + i of tile m the row 32 m + 16 (j / 2) + 8 h + 4 (j % 2) + i
-  f32x16 S[MT];
-  const size_t part_at = ((size_t)number * A.Hkv + g) * D * D;
-  const float *from = segments > 1 ? (OUT ? A.part + part_at : nullptr) : state_in(A, piece.b);
-  if (segments == 1 && from) from += (size_t)g * D * D;
-  const int s_at = 8 * h * D + 32 * wave + col;
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) S[m][e] = from ? from[s_at + (32 * m + 16 * (e >> 3) + (e & 7)) * D] : 0.f;
+  const int rows = min(A.segment, len - first), begin = piece.begin + first, chunks = (rows + C - 1) / C;
 
   // ---- loads, straight to LDS, rows behind the last from the last
   const int row0 = wave * NL * RL + lane / CH, slot0 = lane % CH;
@@ -204,59 +197,99 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
       __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(to + (wave * NL + m) * 64), 16, (int)((uint32_t)min(row, most) * (uint32_t)(stride * 2) + 16 * place<D>(row, slot0)), 0, 0, 0);
     }
   };
-  const uint16_t *k = A.k + g * A.kv_stride_h, *v = A.v + g * A.kv_stride_h;
-  // what was asked for has come, and what was read is in registers
-  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  const uint16_t *k = A.k + g * A.kv_stride_h, *v = A.v + g * A.kv_stride_h, *q = A.q + (g * A.G) * A.q_stride_h;
+  // decays in powers of two (2^-150 is 0 in fp32; an infinite sum would have no differences)
+  auto power = [](float decay) { return decay * LOG2E < -150.f ? -150.f : decay * LOG2E; };
+  const float fixed = GATES ? 0.f : power(A.decay[g]);
+  auto load_gates = [&](int chunk, u32x4 *to) {       // (each wave has them to itself, both halves the same)
+    const __amdgpu_buffer_rsrc_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(A.decay + (begin + (size_t)chunk * C) * A.Hkv + g), 0, 0xffffffff, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(to + wave * 16), 4, (int)((uint32_t)min(col, rows - 1 - chunk * C) * (uint32_t)A.Hkv * 4), 0, 0, 0);
+  };
+  if (chunks > 0) {
+    load(0, k, A.kv_stride_n, lds_0);
+    load(0, v, A.kv_stride_n, lds_0 + AT_V);
+    if (OUT) load(0, q, A.q_stride_n, lds_0 + AT_Q);
+    if (GATES) load_gates(0, lds_0 + AT_G);
+  }
+
+  // ---- the state: lane (h, col) has column 32 wave + col, in element 4 j + i of tile m the row 32 m + 16 (j / 2) + 8 h + 4 (j % 2) + i
+  f32x16 S[MT];
+  const size_t part_at = ((size_t)number * A.Hkv + g) * D * D;
+  const float *from = segments > 1 ? (OUT ? A.part + part_at : nullptr) : state_in(A, piece.b);
+  if (segments == 1 && from) from += (size_t)g * D * D;
+  const int s_at = 8 * h * D + 32 * wave + col;
+  if (from) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) S[m][e] = from[s_at + (32 * m + 16 * (e >> 3) + (e & 7)) * D];
+  } else {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) S[m][e] = 0.f;
+  }
 
   // ---- reads: chunk 2 s + h of row col; by the transposing read rows 16 s + 4 h + 0..3 and 8 further on of 32 channels. For K the middle two
   // of each 16 channels' fours change places: then the state's rows lie in a lane's accumulators in the order of an operand.
   const int r_lane = col * CH * 16 + 16 * place<D>(col, h);
   const int t_row = 4 * h + ((lane & 15) >> 2), t_four = lane & 3;
-  const int v_chan = (lane & 16) + 4 * t_four, k_chan = (lane & 16) + 4 * ((t_four & 1) << 1 | t_four >> 1);
-  auto transposed = [&](const u32x4 *tile, int chan, int s) {
+  auto first_of = [&](int chan) { return (t_row * CH + place<D>(t_row, chan >> 3)) * 16 + (chan & 7) * 2; };
+  const int v_lane = first_of(32 * wave + (lane & 16) + 4 * t_four), k_lane = first_of((lane & 16) + 4 * ((t_four & 1) << 1 | t_four >> 1));
+  // (8 rows further on bit 1 of a chunk's place changes, 32 channels further on bit 2)
+  auto transposed = [&](const u32x4 *tile, int at, int m, int s) {
     u32x4 w;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int row = 16 * s + 8 * e + t_row;
-      const u32x2 two = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_ptr)tile + (row * CH + place<D>(row, chan >> 3)) * 16 + (chan & 7) * 2)));
+      const u32x2 two = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_ptr)tile + (at ^ (64 * m) ^ (32 * e)) + (16 * s + 8 * e) * CH * 16)));
       w[2 * e] = two[0];
       w[2 * e + 1] = two[1];
     }
     return __builtin_bit_cast(bf16x8, w);
   };
+  // What was asked for before the last step's stores has come (memory operations end in their order), and what was read is in registers.
+  auto turn = [] {
+    if (OUT) asm volatile("s_waitcnt vmcnt(2) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
 
-  const float fixed = A.decay_rows ? 0.f : A.decay[g] * LOG2E;
   double all = 0.0, drift = 1.0;
-  const int chunks = (rows + C - 1) / C;
-  for (int chunk = 0; chunk < chunks; ++chunk) {
-    const int n = min(rows - chunk * C, C);
-    arrived();
-    load(chunk, k, A.kv_stride_n, lds_k);
-    load(chunk, v, A.kv_stride_n, lds_v);
-    if (OUT) load(chunk, A.q + (g * A.G) * A.q_stride_h, A.q_stride_n, lds_q);
-    // ---- decays, in powers of two: c = sum up to the row `col`, and sums over the rows behind the lane's sixteen rows 8 j + 4 h + i
-    float gate = 0.f;
-    if (col < n) gate = A.decay_rows ? A.decay[(begin + (size_t)chunk * C + col) * A.Hkv + g] * LOG2E : fixed;
-    if (gate < -150.f) gate = -150.f;        // (2^-150 is 0 in fp32; an infinite sum would have no differences)
-    const float c = scan32(gate);
-    const float after = scan32(col ? __shfl(gate, (threadIdx.x & 32) | (32 - col), 64) : 0.f);      // of rows 32 - col .. 31
-    lds_c[wave][0][col] = c;
-    lds_c[wave][1][31 - col] = after;
-    float near[16], left[16];
+  float near[16];                  // weights of keys 8 j + 4 h + i for the query col, if it is not before them
+  if (!GATES) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int s = 8 * (e >> 2) + 4 * h + (e & 3);
-      near[e] = __builtin_amdgcn_exp2f(c - lds_c[wave][0][s]);
-      left[e] = s < n ? __builtin_amdgcn_exp2f(lds_c[wave][1][s]) : 0.f;
+    for (int e = 0; e < 16; ++e) near[e] = __builtin_amdgcn_exp2f((float)(col - (8 * (e >> 2) + 4 * h + (e & 3))) * fixed);
+  }
+  auto body = [&](int chunk, u32x4 *lds, u32x4 *next) {
+    const int n = min(rows - chunk * C, C);
+    turn();
+    if (chunk + 1 < chunks) {
+      load(chunk + 1, k, A.kv_stride_n, next);
+      load(chunk + 1, v, A.kv_stride_n, next + AT_V);
+      if (GATES) load_gates(chunk + 1, next + AT_G);
     }
-    const float c_end = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c), 31));
-    const float e_t = __builtin_amdgcn_exp2f(c);
-    arrived();
+    // ---- decays: c = sum up to the row `col`, and sums over the rows behind each row
+    const lds_ptr sums = (lds_ptr)(lds + AT_C + wave * 16);
+    float c, c_end;
+    if constexpr (GATES) {
+      const float gate = power(*(lds_f32)((lds_ptr)(lds + AT_G + wave * 16) + 4 * col)), own = col < n ? gate : 0.f;
+      c = scan32(own);
+      const float turned = __shfl(own, (threadIdx.x & 32) | ((32 - col) & 31), 64), after = scan32(col ? turned : 0.f);      // of rows 32 - col .. 31
+      *(lds_f32)(sums + 4 * col) = c;
+      *(lds_f32)(sums + 4 * (C + 31 - col)) = after;
+      c_end = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c), 31));
+    } else {
+      c = (float)(col + 1) * fixed;
+      c_end = (float)n * fixed;
+    }
+    // (what comes of these is made anew in every chunk, not kept in registers)
+    int r_at = r_lane, v_at = v_lane, k_at = k_lane;
+    asm("" : "+v"(r_at), "+v"(v_at), "+v"(k_at));
     bf16x8 V[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) V[s] = transposed(lds_v, 32 * wave + v_chan, s);
+    for (int s = 0; s < 2; ++s) V[s] = transposed(lds + AT_V, v_at, 0, s);
 
     if constexpr (OUT) {
+      const float e_t = __builtin_amdgcn_exp2f(c);
       // Has the chunk a value that is infinite or no number? Rows before it do not see it, but 0 times it is not 0.
       float z = 0.f;
       const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
@@ -268,21 +301,18 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
           z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), none, z, false);
         }
       const bool odd = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
-      for (int hd = 0; hd < A.G; ++hd) {
-        const int head = g * A.G + hd;
-        if (hd) {
-          arrived();
-          load(chunk, A.q + head * A.q_stride_h, A.q_stride_n, lds_q);
-          arrived();
-        }
+      auto head = [&](int hd, const u32x4 *own_q, u32x4 *to_q) {
+        if (hd) turn();
+        if (GROUP && hd + 1 < A.G) load(chunk, q + (hd + 1) * A.q_stride_h, A.q_stride_n, to_q);
+        else if (chunk + 1 < chunks) load(chunk + 1, q, A.q_stride_n, next + AT_Q);
         bf16x8 Q[KS];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds_q + (r_lane ^ (32 * s))));
+        for (int s = 0; s < KS; ++s) Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)own_q + (r_at ^ (32 * s))));
         // X^T = K Q^T: row q . k of keys 8 j + 4 h + i and query col; O^T = S^T Q^T. The state enters the product as bf16 (half a step, 2^-8 of
         // each number; the state itself stays as it is)
         f32x16 X = {}, O = {};
 #pragma unroll
-        for (int s = 0; s < KS; ++s) X = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds_k + (r_lane ^ (32 * s)))), Q[s], X, 0, 0, 0);
+        for (int s = 0; s < KS; ++s) X = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds + (r_at ^ (32 * s)))), Q[s], X, 0, 0, 0);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -294,6 +324,10 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
           }
 #pragma unroll
         for (int e = 0; e < 16; ++e) O[e] *= e_t;
+        if (GATES) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) near[e] = __builtin_amdgcn_exp2f(c - *(lds_f32)(sums + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));
+        }
         // the weights, as bf16 (half a step, 2^-8 of each), none for keys behind the query, whatever their product is
         bf16x8 P[2];
 #pragma unroll
@@ -331,20 +365,38 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
               for (int e = 0; e < 16; ++e) O[e] += 16 * s + key <= col ? x[e] : 0.f;
             }
         }
-        if (col < n) {
-          const size_t at = ((begin + (size_t)chunk * C + col) * A.Hq + head) * D + 32 * wave + 4 * h;
+        // Two stores or more, which `turn` counts. The lane has channels 8 j + 4 h + i; as bf16 the halves of the wave exchange some, so that each
+        // has eight channels side by side.
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f32x4 o = {O[4 * j] * A.scale, O[4 * j + 1] * A.scale, O[4 * j + 2] * A.scale, O[4 * j + 3] * A.scale};
-            if (A.out_dtype == STS_F32) {
-              *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 8 * j) = o;
-            } else {
-              const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[0], o[1]}), bf16x2)),
-                               __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[2], o[3]}), bf16x2))};
-              *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at + 8 * j) = w;
+        for (int e = 0; e < 16; ++e) O[e] *= A.scale;
+        const size_t at = ((begin + (size_t)chunk * C + col) * A.Hq + g * A.G + hd) * D + 32 * wave;
+        if (A.out_dtype == STS_F32) {
+          if (col < n) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 8 * j + 4 * h) = f32x4{O[4 * j], O[4 * j + 1], O[4 * j + 2], O[4 * j + 3]};
+          }
+        } else {
+          u32x4 w[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{O[8 * j + 2 * i], O[8 * j + 2 * i + 1]}), bf16x2));
+              const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{O[8 * j + 4 + 2 * i], O[8 * j + 5 + 2 * i]}), bf16x2));
+              const auto swapped = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+              w[j][i] = swapped[0];
+              w[j][2 + i] = swapped[1];
             }
+          if (col < n) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(A.out) + at + 16 * j + 8 * h) = w[j];
           }
         }
+      };
+      head(0, lds + AT_Q, lds_q0);
+      for (int hd = 1; GROUP && hd < A.G; hd += 2) {
+        head(hd, lds_q0, lds_q1);
+        if (hd + 1 < A.G) head(hd + 1, lds_q1, lds_q0);
       }
     }
 
@@ -366,7 +418,13 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
       u32x4 w[3];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        f32x2 x = {left[8 * s + 2 * e] * __builtin_bit_cast(float, two[e] << 16), left[8 * s + 2 * e + 1] * __builtin_bit_cast(float, two[e] & 0xffff0000u)};
+        f32x2 x = {__builtin_bit_cast(float, two[e] << 16), __builtin_bit_cast(float, two[e] & 0xffff0000u)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
+          const float left = __builtin_amdgcn_exp2f(GATES ? *(lds_f32)(sums + 4 * (C + key)) : (float)(n - 1 - key) * fixed);
+          x[i] *= key < n ? left : 0.f;
+        }
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
           const uint32_t top2 = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
@@ -382,10 +440,15 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const bf16x8 K = transposed(lds_k, 32 * m + k_chan, s);
+        const bf16x8 K = transposed(lds, k_at, m, s);
 #pragma unroll
         for (int i = 2; i >= 0; --i) S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K, W[i][s], S[m], 0, 0, 0);
       }
+  };
+  __builtin_amdgcn_s_waitcnt(0x0f70);              // (no stores come behind the first loads)
+  for (int chunk = 0; chunk < chunks; chunk += 2) {
+    body(chunk, lds_0, lds_1);
+    if (chunk + 1 < chunks) body(chunk + 1, lds_1, lds_0);
   }
 
   float *to;
@@ -440,19 +503,21 @@ hipError_t launch_linear_step(const LinearArgs &a, int d, hipStream_t s) {
   return sts_take_launch_status();
 }
 
-hipError_t launch_linear_sums(const LinearArgs &a, int d, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.numbers * a.Hkv)), block(2 * d);
-  if (d == 128) STS_LAUNCH((linear_chunk_kernel<128, false>), grid, block, 0, s, a);
-  else STS_LAUNCH((linear_chunk_kernel<64, false>), grid, block, 0, s, a);
+template <int D, bool OUT>
+static hipError_t launch_chunks(const LinearArgs &a, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.numbers * a.Hkv)), block(2 * D);
+  const bool group = OUT && a.G > 1;
+  if (a.decay_rows) {
+    if (group) STS_LAUNCH((linear_chunk_kernel<D, OUT, true, OUT>), grid, block, 0, s, a);
+    else STS_LAUNCH((linear_chunk_kernel<D, OUT, true, false>), grid, block, 0, s, a);
+  } else {
+    if (group) STS_LAUNCH((linear_chunk_kernel<D, OUT, false, OUT>), grid, block, 0, s, a);
+    else STS_LAUNCH((linear_chunk_kernel<D, OUT, false, false>), grid, block, 0, s, a);
+  }
   return sts_take_launch_status();
 }
-
-hipError_t launch_linear_chunks(const LinearArgs &a, int d, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.numbers * a.Hkv)), block(2 * d);
-  if (d == 128) STS_LAUNCH((linear_chunk_kernel<128, true>), grid, block, 0, s, a);
-  else STS_LAUNCH((linear_chunk_kernel<64, true>), grid, block, 0, s, a);
-  return sts_take_launch_status();
-}
+hipError_t launch_linear_sums(const LinearArgs &a, int d, hipStream_t s) { return d == 128 ? launch_chunks<128, false>(a, s) : launch_chunks<64, false>(a, s); }
+hipError_t launch_linear_chunks(const LinearArgs &a, int d, hipStream_t s) { return d == 128 ? launch_chunks<128, true>(a, s) : launch_chunks<64, true>(a, s); }
 
 hipError_t launch_linear_carry(const LinearArgs &a, int d, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.seqs.B * a.Hkv * (d * d / 1024))), block(256);
