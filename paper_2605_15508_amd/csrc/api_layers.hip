@@ -46,8 +46,8 @@ sts_status plan_linear(const sts_linear_params *p, LinearPlan &pl) {
   pl.step = pl.max_len <= STS_LINEAR_STEP;
   if ((int64_t)p->B * p->Hkv * (p->d * p->d / 1024) >= MOST_GROUPS) return STS_EUNSUPPORTED;
   if (pl.step) return STS_OK;
-  // Segments: as many as the chip runs workgroups at once, two on a compute unit, but of 128 rows at least.
-  int64_t segment = ((int64_t)p->T * p->Hkv / (2 * sts_cu_count()) + STS_LINEAR_CHUNK - 1) / STS_LINEAR_CHUNK * STS_LINEAR_CHUNK;
+  // Segments: as many as the chip runs workgroups at once, two on a compute unit (four of half the waves), but of 128 rows at least.
+  int64_t segment = ((int64_t)p->T * p->Hkv / ((p->d == 128 ? 2 : 4) * sts_cu_count()) + STS_LINEAR_CHUNK - 1) / STS_LINEAR_CHUNK * STS_LINEAR_CHUNK;
   if (segment < 128) segment = 128;
   pl.segment = (int32_t)segment;
   const int64_t numbers = piece_numbers(p->T, segment, p->B);

@@ -45,6 +45,12 @@ __device__ __forceinline__ double exp2_64(double x) {
   return x < -1000.0 ? 0.0 : __builtin_ldexp(p, (int)n);
 }
 
+// the same in 32 bits, of a sum that is kept in 64
+__device__ __forceinline__ float exp2_32(double x) {
+  const float y = (float)x, rest = (float)(x - (double)y);
+  return __builtin_amdgcn_exp2f(y) * (1.f + 0.6931471806f * rest);
+}
+
 // where the state of sequence b begins, or NULL: there is none (a slot outside the pool stands for none)
 __device__ __forceinline__ const float *state_in(const LinearArgs &A, int b) {
   if (!A.state) return nullptr;
@@ -171,7 +177,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   // Two chunks of K, V, the first head's Q, the decays and (two numbers for each row and wave) their sums; the other heads' Q take turns in two
   // more places. Arrays of their own, so that the compiler can tell the loads that fill one from the reads of another, and the sums are in the chunk's
   // since a read of an array that no load fills waits for all loads.
-  constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, AT_G = (OUT ? 3 : 2) * TILE, AT_C = AT_G + NW * 16, ALL = GATES ? AT_C + NW * 16 : AT_G;
+  constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, AT_G = (OUT ? 3 : 2) * TILE, AT_C = AT_G + (GATES ? NW * 16 : 0), ALL = AT_C + NW * 16;
   __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_q0[GROUP ? TILE : 1], lds_q1[GROUP ? TILE : 1];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -253,12 +259,17 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
 
-  double all = 0.0, drift = 1.0;
-  float near[16];                  // weights of keys 8 j + 4 h + i for the query col, if it is not before them
-  if (!GATES) {
+  // The state is held as S / F, F the product of the decays since it was last multiplied out (its logarithm `low` is a sum in 64 bits, so that no
+  // factor's rounding adds up over a long sequence); what a chunk adds is divided by F instead.
+  double all = 0.0, low = 0.0;
+  auto multiply_out = [&] {
+    const float f = exp2_32(low);
+    low = 0.0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) near[e] = __builtin_amdgcn_exp2f((float)(col - (8 * (e >> 2) + 4 * h + (e & 3))) * fixed);
-  }
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) S[m][e] *= f;
+  };
   auto body = [&](int chunk, u32x4 *lds, u32x4 *next) {
     const int n = min(rows - chunk * C, C);
     turn();
@@ -267,29 +278,44 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
       load(chunk + 1, v, A.kv_stride_n, next + AT_V);
       if (GATES) load_gates(chunk + 1, next + AT_G);
     }
-    // ---- decays: c = sum up to the row `col`, and sums over the rows behind each row
+    // ---- decays: c = sum up to the row `col`, `after` the sum behind row `key`
     const lds_ptr sums = (lds_ptr)(lds + AT_C + wave * 16);
-    float c, c_end;
+    float c, c_end, after;
+    int key = col;
     if constexpr (GATES) {
       const float gate = power(*(lds_f32)((lds_ptr)(lds + AT_G + wave * 16) + 4 * col)), own = col < n ? gate : 0.f;
       c = scan32(own);
-      const float turned = __shfl(own, (threadIdx.x & 32) | ((32 - col) & 31), 64), after = scan32(col ? turned : 0.f);      // of rows 32 - col .. 31
-      *(lds_f32)(sums + 4 * col) = c;
-      *(lds_f32)(sums + 4 * (C + 31 - col)) = after;
       c_end = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c), 31));
+      const float turned = __shfl(own, (threadIdx.x & 32) | ((32 - col) & 31), 64);
+      key = 31 - col;
+      after = scan32(col ? turned : 0.f);
     } else {
       c = (float)(col + 1) * fixed;
       c_end = (float)n * fixed;
+      after = (float)(n - 1 - col) * fixed;
     }
+    // With u_i = exp(c_i - c_32), out_i = scale u_i (q_i . (exp(c_32) S) + sum exp(c_32 - c_j) (q_i . k_j) v_j): one weight for each key, which the state
+    // takes too. Not where u would leave fp32's range (or a decay is no number): there each pair has a weight of its own.
+    const bool apart = !(c_end >= -60.f);
+    const double low_before = low;
+    all += c_end;
+    low += c_end;
+    if (!apart && low < -16.0) multiply_out();
+    const float F = apart ? 1.f : exp2_32(low), F_inv = apart ? 1.f : exp2_32(-low);
+    *(lds_f32)(sums + 4 * col) = c;
+    *(lds_f32)(sums + 4 * (C + key)) = key < n ? __builtin_amdgcn_exp2f(after) * F_inv : 0.f;
     // (what comes of these is made anew in every chunk, not kept in registers)
     int r_at = r_lane, v_at = v_lane, k_at = k_lane;
     asm("" : "+v"(r_at), "+v"(v_at), "+v"(k_at));
+    float left[16];                // weights of keys 8 j + 4 h + i
+#pragma unroll
+    for (int e = 0; e < 16; ++e) left[e] = *(lds_f32)(sums + 4 * (C + 8 * (e >> 2) + 4 * h + (e & 3)));
     bf16x8 V[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) V[s] = transposed(lds + AT_V, v_at, 0, s);
 
     if constexpr (OUT) {
-      const float e_t = __builtin_amdgcn_exp2f(c);
+      const float own_factor = A.scale * (apart ? 1.f : F * __builtin_amdgcn_exp2f(c - c_end));
       // Has the chunk a value that is infinite or no number? Rows before it do not see it, but 0 times it is not 0.
       float z = 0.f;
       const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
@@ -305,6 +331,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
         if (hd) turn();
         if (GROUP && hd + 1 < A.G) load(chunk, q + (hd + 1) * A.q_stride_h, A.q_stride_n, to_q);
         else if (chunk + 1 < chunks) load(chunk + 1, q, A.q_stride_n, next + AT_Q);
+        asm volatile("" ::: "memory");             // (the stores come behind these loads: see `turn`)
         bf16x8 Q[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)own_q + (r_at ^ (32 * s))));
@@ -322,11 +349,16 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
             for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{S[m][8 * s + 2 * e], S[m][8 * s + 2 * e + 1]}), bf16x2));
             O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), Q[2 * m + s], O, 0, 0, 0);
           }
+        if (apart) {
+          const float f = exp2_32(low_before + c);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) O[e] *= e_t;
-        if (GATES) {
+          for (int e = 0; e < 16; ++e) {
+            O[e] *= f;
+            X[e] *= __builtin_amdgcn_exp2f(c - *(lds_f32)(sums + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));
+          }
+        } else {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) near[e] = __builtin_amdgcn_exp2f(c - *(lds_f32)(sums + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));
+          for (int e = 0; e < 16; ++e) X[e] *= left[e];
         }
         // the weights, as bf16 (half a step, 2^-8 of each), none for keys behind the query, whatever their product is
         bf16x8 P[2];
@@ -339,7 +371,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
-              x[i] = key <= col ? near[at] * X[at] : 0.f;
+              x[i] = key <= col ? X[at] : 0.f;
             }
             w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
           }
@@ -368,7 +400,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
         // Two stores or more, which `turn` counts. The lane has channels 8 j + 4 h + i; as bf16 the halves of the wave exchange some, so that each
         // has eight channels side by side.
 #pragma unroll
-        for (int e = 0; e < 16; ++e) O[e] *= A.scale;
+        for (int e = 0; e < 16; ++e) O[e] *= own_factor;
         const size_t at = ((begin + (size_t)chunk * C + col) * A.Hq + g * A.G + hd) * D + 32 * wave;
         if (A.out_dtype == STS_F32) {
           if (col < n) {
@@ -400,17 +432,9 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
       }
     }
 
-    // ---- The state behind the chunk. Its decay's rounding would add up over a long sequence (always the same one, where the decay is fixed): what
-    // a rounded factor is off by goes into the next.
-    all += c_end;
-    const double exact = exp2_64((double)c_end) * drift;
-    const float f = (float)exact;
-    drift = f > 1e-30f ? 1.0 + (exact - (double)f) * (double)(1.f / f) : 1.0;
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) S[m][e] *= f;
-    // V with its weights as the sum of three bf16 numbers, which hold an fp32's bits: the products enter the state as exactly as in fp32
+    // ---- The state behind the chunk. V with its weights is the sum of three bf16 numbers, which hold an fp32's bits: the products enter the state
+    // as exactly as in fp32.
+    if (apart) multiply_out();
     bf16x8 W[3][2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -418,13 +442,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
       u32x4 w[3];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        f32x2 x = {__builtin_bit_cast(float, two[e] << 16), __builtin_bit_cast(float, two[e] & 0xffff0000u)};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
-          const float left = __builtin_amdgcn_exp2f(GATES ? *(lds_f32)(sums + 4 * (C + key)) : (float)(n - 1 - key) * fixed);
-          x[i] *= key < n ? left : 0.f;
-        }
+        f32x2 x = {left[8 * s + 2 * e] * __builtin_bit_cast(float, two[e] << 16), left[8 * s + 2 * e + 1] * __builtin_bit_cast(float, two[e] & 0xffff0000u)};
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
           const uint32_t top2 = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
@@ -451,6 +469,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     if (chunk + 1 < chunks) body(chunk + 1, lds_1, lds_0);
   }
 
+  multiply_out();
   float *to;
   if (segments > 1 && !OUT) {
     to = A.part + part_at;
