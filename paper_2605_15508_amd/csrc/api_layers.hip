@@ -31,6 +31,7 @@ struct LinearPlan {
   int32_t each, max_len;     // rows of a sequence without starts; rows of the longest
   int32_t segment, numbers;
   bool several;              // a sequence may have more than one segment
+  bool carry;                // states are handed on: between segments, and to the heads of a group
   size_t part_bytes, log_bytes;
   size_t total() const { return part_bytes + log_bytes ? part_bytes + log_bytes : 256; }
 };
@@ -47,14 +48,15 @@ sts_status plan_linear(const sts_linear_params *p, LinearPlan &pl) {
   if ((int64_t)p->B * p->Hkv * (p->d * p->d / 1024) >= MOST_GROUPS) return STS_EUNSUPPORTED;
   if (pl.step) return STS_OK;
   // Segments: as many as the chip runs workgroups at once, two on a compute unit (four of half the waves), but of 128 rows at least.
-  int64_t segment = ((int64_t)p->T * p->Hkv / ((p->d == 128 ? 2 : 4) * sts_cu_count()) + STS_LINEAR_CHUNK - 1) / STS_LINEAR_CHUNK * STS_LINEAR_CHUNK;
+  int64_t segment = ((int64_t)p->T * p->Hq / ((p->d == 128 ? 2 : 4) * sts_cu_count()) + STS_LINEAR_CHUNK - 1) / STS_LINEAR_CHUNK * STS_LINEAR_CHUNK;
   if (segment < 128) segment = 128;
   pl.segment = (int32_t)segment;
   const int64_t numbers = piece_numbers(p->T, segment, p->B);
-  if (numbers * p->Hkv >= MOST_GROUPS) return STS_EUNSUPPORTED;
+  if (numbers * p->Hq + STS_XCDS * STS_MAX_GROUP >= MOST_GROUPS) return STS_EUNSUPPORTED;
   pl.numbers = (int32_t)numbers;
   pl.several = pl.max_len > segment;
-  if (pl.several) {
+  pl.carry = pl.several || (p->out && p->Hq > p->Hkv);
+  if (pl.carry) {
     pl.part_bytes = align256((size_t)numbers * p->Hkv * p->d * p->d * sizeof(float));
     pl.log_bytes = align256((size_t)numbers * p->Hkv * sizeof(double));
   }
@@ -141,20 +143,21 @@ sts_status sts_linear_attn(const sts_linear_params *p, void *stream) {
   a.out = p->out;
   a.out_dtype = p->out_dtype;
   a.by_heads = divide_by(a.Hkv);
+  a.by_group = divide_by(a.G);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int d = p->d;
   if (pl.step) return sts_run_kernel(STS_K_LINEAR_STEP, s, [&] { return launch_linear_step(a, d, s); }) == hipSuccess ? STS_OK : STS_EHIP;
   a.segment = pl.segment;
   a.numbers = pl.numbers;
   a.by_segment = divide_by(pl.segment);
-  if (pl.several) {
+  if (pl.carry) {
     if (!p->workspace || p->workspace_bytes < pl.part_bytes + pl.log_bytes || !aligned(p->workspace, 256)) return STS_EWORKSPACE;
     a.part = static_cast<float *>(p->workspace);
     a.part_log = reinterpret_cast<double *>(static_cast<unsigned char *>(p->workspace) + pl.part_bytes);
   }
   hipError_t rc = hipSuccess;
   if (pl.several || !p->out) rc = sts_run_kernel(STS_K_LINEAR_SUMS, s, [&] { return launch_linear_sums(a, d, s); });
-  if (rc == hipSuccess && pl.several) rc = sts_run_kernel(STS_K_LINEAR_CARRY, s, [&] { return launch_linear_carry(a, d, s); });
+  if (rc == hipSuccess && pl.carry) rc = sts_run_kernel(STS_K_LINEAR_CARRY, s, [&] { return launch_linear_carry(a, d, s); });
   if (rc == hipSuccess && p->out) rc = sts_run_kernel(STS_K_LINEAR_CHUNKS, s, [&] { return launch_linear_chunks(a, d, s); });
   return rc == hipSuccess ? STS_OK : STS_EHIP;
 }

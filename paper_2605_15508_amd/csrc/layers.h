@@ -86,8 +86,8 @@ struct LinearArgs {
   // chunked form: rows of a segment (a multiple of STS_LINEAR_CHUNK), numbers of segments (piece_numbers), and for sequences of several segments
   // what each adds to the state, later the state before it, and the logarithm of its decay
   int32_t segment, numbers;
-  Divisor by_segment, by_heads;
-  float *part;                       // [numbers][Hkv][d][d], or NULL: no sequence has two segments
+  Divisor by_segment, by_heads, by_group;
+  float *part;                       // [numbers][Hkv][d][d], or NULL: nothing is handed on
   double *part_log;                  // [numbers][Hkv]
 };
 constexpr int STS_LINEAR_CHUNK = 32, STS_LINEAR_STEP = 16;      // rows of a chunk; rows of a sequence that the recurrent form takes at most

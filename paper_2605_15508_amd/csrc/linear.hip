@@ -168,21 +168,26 @@ __device__ __forceinline__ float scan32(float x) {
 }
 
 // OUT: results, from the state before the segment; else what the segment adds to the state (or, of a sequence with one segment, its
-// state). GATES: a decay for every row; GROUP: several heads to a KV head
-template <int D, bool OUT, bool GATES, bool GROUP>
+// state). GATES: a decay for every row
+template <int D, bool OUT, bool GATES>
 __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs A) {
   constexpr int NW = D / 32;             // waves, each with 32 columns of the state
   constexpr int KS = D / 16, MT = D / 32, CH = D / 8;
   constexpr int NL = C * CH / (64 * NW), RL = 64 / CH;      // loads of a wave for 32 rows, rows that each covers
-  // Two chunks of K, V, the first head's Q, the decays and (two numbers for each row and wave) their sums; the other heads' Q take turns in two
-  // more places. Arrays of their own, so that the compiler can tell the loads that fill one from the reads of another, and the sums are in the chunk's
-  // since a read of an array that no load fills waits for all loads.
+  // Three chunks of K, V, Q, the decays and (two numbers for each row and wave) their sums. Arrays of their own, so that the compiler can tell the
+  // loads that fill one from the reads of another, and the sums are in the chunk's since a read of an array that no load fills waits for all loads.
   constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, AT_G = (OUT ? 3 : 2) * TILE, AT_C = AT_G + (GATES ? NW * 16 : 0), ALL = AT_C + NW * 16;
-  __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_q0[GROUP ? TILE : 1], lds_q1[GROUP ? TILE : 1];
+  constexpr int LOADS = (OUT ? 3 : 2) * NL + (GATES ? 1 : 0), STORES = OUT ? 2 : 0;      // of a wave and chunk
+  __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_2[ALL];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
-  const int number = A.by_heads.of(blockIdx.x), g = blockIdx.x - number * A.Hkv;
+  // Neighbouring units on different dies (workgroup i runs on die i % 8), which evens out the numbers that no segment has; the heads of a group (each
+  // with a state of its own, which is the same) on one die, one after the other: they read the same K and V.
+  const int turns = blockIdx.x / STS_XCDS, eight = OUT ? A.by_group.of(turns) : turns, hd = OUT ? turns - eight * A.G : 0;
+  const int unit = eight * STS_XCDS + blockIdx.x % STS_XCDS;
+  if (unit >= A.numbers * A.Hkv) return;
+  const int number = A.by_heads.of(unit), g = unit - number * A.Hkv, head = g * A.G + hd;
   const PackedPiece piece = find_piece(A.seqs, number, [&](int begin) { return A.by_segment.of(begin); });
   if (piece.b < 0) return;
   const int len = rows_of(A, piece.b, piece.len), first = piece.index * A.segment;
@@ -192,37 +197,41 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   if (!OUT && A.out && last) return;                 // (the results' kernel brings the last segment's state)
   const int rows = min(A.segment, len - first), begin = piece.begin + first, chunks = (rows + C - 1) / C;
 
-  // ---- loads, straight to LDS, rows behind the last from the last
+  // ---- loads, straight to LDS, rows behind the last from the last; behind the last chunk nothing is loaded (by loads of no bytes: the number of loads
+  // is always the same)
   const int row0 = wave * NL * RL + lane / CH, slot0 = lane % CH;
-  auto load = [&](int chunk, const uint16_t *base, int64_t stride, u32x4 *to) {
-    const __amdgpu_buffer_rsrc_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(base + (begin + (int64_t)chunk * C) * stride), 0, 0xffffffff, 0x00027000);
-    const int most = rows - 1 - chunk * C;
+  auto rsrc = [&](const void *at, bool any) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, __builtin_amdgcn_readfirstlane(any ? -1 : 0), 0x00027000); };
+  auto load_rows = [&](int chunk, const uint16_t *base, int64_t stride, u32x4 *to) {
+    const __amdgpu_buffer_rsrc_t at = rsrc(base + (begin + (int64_t)chunk * C) * stride, chunk < chunks);
+    const int most = max(rows - 1 - chunk * C, 0);
 #pragma unroll
     for (int m = 0; m < NL; ++m) {
       const int row = row0 + RL * m;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(to + (wave * NL + m) * 64), 16, (int)((uint32_t)min(row, most) * (uint32_t)(stride * 2) + 16 * place<D>(row, slot0)), 0, 0, 0);
     }
   };
-  const uint16_t *k = A.k + g * A.kv_stride_h, *v = A.v + g * A.kv_stride_h, *q = A.q + (g * A.G) * A.q_stride_h;
+  const uint16_t *k = A.k + g * A.kv_stride_h, *v = A.v + g * A.kv_stride_h, *q = A.q + head * A.q_stride_h;
+  auto load = [&](int chunk, u32x4 *to) {
+    load_rows(chunk, k, A.kv_stride_n, to);
+    load_rows(chunk, v, A.kv_stride_n, to + AT_V);
+    if (GATES)           // (each wave has them to itself, both halves the same)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(A.decay + (begin + (size_t)chunk * C) * A.Hkv + g, chunk < chunks), (lds_ptr)(to + AT_G + wave * 16), 4,
+                                               (int)((uint32_t)min(col, max(rows - 1 - chunk * C, 0)) * (uint32_t)A.Hkv * 4), 0, 0, 0);
+    if (OUT) load_rows(chunk, q, A.q_stride_n, to + AT_Q);
+    asm volatile("" ::: "memory");       // (a chunk's stores come behind these loads: see `turn`)
+  };
   // decays in powers of two (2^-150 is 0 in fp32; an infinite sum would have no differences)
   auto power = [](float decay) { return decay * LOG2E < -150.f ? -150.f : decay * LOG2E; };
   const float fixed = GATES ? 0.f : power(A.decay[g]);
-  auto load_gates = [&](int chunk, u32x4 *to) {       // (each wave has them to itself, both halves the same)
-    const __amdgpu_buffer_rsrc_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(A.decay + (begin + (size_t)chunk * C) * A.Hkv + g), 0, 0xffffffff, 0x00027000);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(to + wave * 16), 4, (int)((uint32_t)min(col, rows - 1 - chunk * C) * (uint32_t)A.Hkv * 4), 0, 0, 0);
-  };
-  if (chunks > 0) {
-    load(0, k, A.kv_stride_n, lds_0);
-    load(0, v, A.kv_stride_n, lds_0 + AT_V);
-    if (OUT) load(0, q, A.q_stride_n, lds_0 + AT_Q);
-    if (GATES) load_gates(0, lds_0 + AT_G);
-  }
+  load(0, lds_0);
 
   // ---- the state: lane (h, col) has column 32 wave + col, in element 4 j + i of tile m the row 32 m + 16 (j / 2) + 8 h + 4 (j % 2) + i
   f32x16 S[MT];
   const size_t part_at = ((size_t)number * A.Hkv + g) * D * D;
-  const float *from = segments > 1 ? (OUT ? A.part + part_at : nullptr) : state_in(A, piece.b);
-  if (segments == 1 && from) from += (size_t)g * D * D;
+  // (Heads of a group start from a copy of a sequence's state: the one that writes the state behind its rows may be done before another begins.)
+  const bool carried = segments > 1 || (OUT && A.G > 1);
+  const float *from = carried ? (OUT ? A.part + part_at : nullptr) : state_in(A, piece.b);
+  if (!carried && from) from += (size_t)g * D * D;
   const int s_at = 8 * h * D + 32 * wave + col;
   if (from) {
 #pragma unroll
@@ -253,11 +262,9 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     }
     return __builtin_bit_cast(bf16x8, w);
   };
-  // What was asked for before the last step's stores has come (memory operations end in their order), and what was read is in registers.
-  auto turn = [] {
-    if (OUT) asm volatile("s_waitcnt vmcnt(2) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  };
+  // The chunk has come: behind its loads lie the next chunk's and the last chunk's stores at least (memory operations end in their order). And
+  // what was read is in registers.
+  auto turn = [] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS + STORES) : "memory"); };
 
   // The state is held as S / F, F the product of the decays since it was last multiplied out (its logarithm `low` is a sum in 64 bits, so that no
   // factor's rounding adds up over a long sequence); what a chunk adds is divided by F instead.
@@ -270,14 +277,10 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 #pragma unroll
       for (int e = 0; e < 16; ++e) S[m][e] *= f;
   };
-  auto body = [&](int chunk, u32x4 *lds, u32x4 *next) {
+  auto body = [&](int chunk, u32x4 *lds, u32x4 *free) {
     const int n = min(rows - chunk * C, C);
     turn();
-    if (chunk + 1 < chunks) {
-      load(chunk + 1, k, A.kv_stride_n, next);
-      load(chunk + 1, v, A.kv_stride_n, next + AT_V);
-      if (GATES) load_gates(chunk + 1, next + AT_G);
-    }
+    load(chunk + 2, free);
     // ---- decays: c = sum up to the row `col`, `after` the sum behind row `key`
     const lds_ptr sums = (lds_ptr)(lds + AT_C + wave * 16);
     float c, c_end, after;
@@ -327,108 +330,97 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
           z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), none, z, false);
         }
       const bool odd = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
-      auto head = [&](int hd, const u32x4 *own_q, u32x4 *to_q) {
-        if (hd) turn();
-        if (GROUP && hd + 1 < A.G) load(chunk, q + (hd + 1) * A.q_stride_h, A.q_stride_n, to_q);
-        else if (chunk + 1 < chunks) load(chunk + 1, q, A.q_stride_n, next + AT_Q);
-        asm volatile("" ::: "memory");             // (the stores come behind these loads: see `turn`)
-        bf16x8 Q[KS];
+      bf16x8 Q[KS];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)own_q + (r_at ^ (32 * s))));
-        // X^T = K Q^T: row q . k of keys 8 j + 4 h + i and query col; O^T = S^T Q^T. The state enters the product as bf16 (half a step, 2^-8 of
-        // each number; the state itself stays as it is)
-        f32x16 X = {}, O = {};
+      for (int s = 0; s < KS; ++s) Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)(lds + AT_Q) + (r_at ^ (32 * s))));
+      // X^T = K Q^T: row q . k of keys 8 j + 4 h + i and query col; O^T = S^T Q^T. The state enters the product as bf16 (half a step, 2^-8 of
+      // each number; the state itself stays as it is)
+      f32x16 X = {}, O = {};
 #pragma unroll
-        for (int s = 0; s < KS; ++s) X = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds + (r_at ^ (32 * s)))), Q[s], X, 0, 0, 0);
+      for (int s = 0; s < KS; ++s) X = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds + (r_at ^ (32 * s)))), Q[s], X, 0, 0, 0);
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            u32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{S[m][8 * s + 2 * e], S[m][8 * s + 2 * e + 1]}), bf16x2));
-            O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), Q[2 * m + s], O, 0, 0, 0);
-          }
-        if (apart) {
-          const float f = exp2_32(low_before + c);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            O[e] *= f;
-            X[e] *= __builtin_amdgcn_exp2f(c - *(lds_f32)(sums + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) X[e] *= left[e];
-        }
-        // the weights, as bf16 (half a step, 2^-8 of each), none for keys behind the query, whatever their product is
-        bf16x8 P[2];
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           u32x4 w;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            f32x2 x;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
-              x[i] = key <= col ? X[at] : 0.f;
-            }
-            w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-          }
-          P[s] = __builtin_bit_cast(bf16x8, w);
+          for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{S[m][8 * s + 2 * e], S[m][8 * s + 2 * e + 1]}), bf16x2));
+          O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), Q[2 * m + s], O, 0, 0, 0);
         }
-        if (!odd) {
+      if (apart) {
+        const float f = exp2_32(low_before + c);
 #pragma unroll
-          for (int s = 0; s < 2; ++s) O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], O, 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-            for (int key = 0; key < 16; ++key) {      // key by key, and a row is taken in only where it is seen
-              u32x4 own;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
-                own[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
-              }
-              const f32x16 zero = {};
-              const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, V[s]) & own),
-                                                                       __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, P[s]) & own), zero, 0, 0, 0);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) O[e] += 16 * s + key <= col ? x[e] : 0.f;
-            }
+        for (int e = 0; e < 16; ++e) {
+          O[e] *= f;
+          X[e] *= __builtin_amdgcn_exp2f(c - *(lds_f32)(sums + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));
         }
-        // Two stores or more, which `turn` counts. The lane has channels 8 j + 4 h + i; as bf16 the halves of the wave exchange some, so that each
-        // has eight channels side by side.
+      } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) O[e] *= own_factor;
-        const size_t at = ((begin + (size_t)chunk * C + col) * A.Hq + g * A.G + hd) * D + 32 * wave;
-        if (A.out_dtype == STS_F32) {
-          if (col < n) {
+        for (int e = 0; e < 16; ++e) X[e] *= left[e];
+      }
+      // the weights, as bf16 (half a step, 2^-8 of each), none for keys behind the query, whatever their product is
+      bf16x8 P[2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 8 * j + 4 * h) = f32x4{O[4 * j], O[4 * j + 1], O[4 * j + 2], O[4 * j + 3]};
+      for (int s = 0; s < 2; ++s) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f32x2 x;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
+            x[i] = key <= col ? X[at] : 0.f;
           }
-        } else {
-          u32x4 w[2];
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{O[8 * j + 2 * i], O[8 * j + 2 * i + 1]}), bf16x2));
-              const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{O[8 * j + 4 + 2 * i], O[8 * j + 5 + 2 * i]}), bf16x2));
-              const auto swapped = __builtin_amdgcn_permlane32_swap(x, y, false, false);
-              w[j][i] = swapped[0];
-              w[j][2 + i] = swapped[1];
-            }
-          if (col < n) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(A.out) + at + 16 * j + 8 * h) = w[j];
-          }
+          w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
         }
-      };
-      head(0, lds + AT_Q, lds_q0);
-      for (int hd = 1; GROUP && hd < A.G; hd += 2) {
-        head(hd, lds_q0, lds_q1);
-        if (hd + 1 < A.G) head(hd + 1, lds_q1, lds_q0);
+        P[s] = __builtin_bit_cast(bf16x8, w);
+      }
+      if (!odd) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], O, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          for (int key = 0; key < 16; ++key) {      // key by key, and a row is taken in only where it is seen
+            u32x4 own;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
+              own[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
+            }
+            const f32x16 zero = {};
+            const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, V[s]) & own),
+                                                                     __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, P[s]) & own), zero, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) O[e] += 16 * s + key <= col ? x[e] : 0.f;
+          }
+      }
+      // Two stores or more, which `turn` counts. The lane has channels 8 j + 4 h + i; as bf16 the halves of the wave exchange some, so that each
+      // has eight channels side by side.
+#pragma unroll
+      for (int e = 0; e < 16; ++e) O[e] *= own_factor;
+      const size_t at = ((begin + (size_t)chunk * C + col) * A.Hq + head) * D + 32 * wave;
+      if (A.out_dtype == STS_F32) {
+        if (col < n) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 8 * j + 4 * h) = f32x4{O[4 * j], O[4 * j + 1], O[4 * j + 2], O[4 * j + 3]};
+        }
+      } else {
+        u32x4 w[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{O[8 * j + 2 * i], O[8 * j + 2 * i + 1]}), bf16x2));
+            const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{O[8 * j + 4 + 2 * i], O[8 * j + 5 + 2 * i]}), bf16x2));
+            const auto swapped = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+            w[j][i] = swapped[0];
+            w[j][2 + i] = swapped[1];
+          }
+        if (col < n) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(A.out) + at + 16 * j + 8 * h) = w[j];
+        }
       }
     }
 
@@ -463,10 +455,14 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
         for (int i = 2; i >= 0; --i) S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K, W[i][s], S[m], 0, 0, 0);
       }
   };
-  __builtin_amdgcn_s_waitcnt(0x0f70);              // (no stores come behind the first loads)
-  for (int chunk = 0; chunk < chunks; chunk += 2) {
-    body(chunk, lds_0, lds_1);
-    if (chunk + 1 < chunks) body(chunk + 1, lds_1, lds_0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // (no stores come behind the first loads)
+  load(1, lds_1);
+  for (int chunk = 0; chunk < chunks; chunk += 3) {
+    body(chunk, lds_0, lds_2);
+    if (chunk + 1 >= chunks) break;
+    body(chunk + 1, lds_1, lds_0);
+    if (chunk + 2 >= chunks) break;
+    body(chunk + 2, lds_2, lds_1);
   }
 
   multiply_out();
@@ -475,7 +471,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     to = A.part + part_at;
     if (threadIdx.x == 0) A.part_log[(size_t)number * A.Hkv + g] = all;
   } else {
-    if (!last) return;
+    if (!last || hd != 0) return;
     to = state_out(A, piece.b);
     if (!to) return;
     to += (size_t)g * D * D;
@@ -495,22 +491,33 @@ __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
   int begin, len;
   seq_rows(A.seqs, b, begin, len);
   len = rows_of(A, b, len);
-  const int segments = (len + A.segment - 1) / A.segment;
-  if (segments < 2) return;
+  const int segments = max((len + A.segment - 1) / A.segment, 1);
+  if (segments < 2 && !(A.out && A.G > 1)) return;
   const float *from = state_in(A, b);
   f32x4 S = from ? *reinterpret_cast<const f32x4 *>(from + (size_t)g * D * D + at) : f32x4{0.f, 0.f, 0.f, 0.f};
-  const size_t number = (size_t)A.by_segment.of(begin) + b;
-  for (int i = 0; i < segments; ++i) {
-    const bool last = i == segments - 1;
-    float *part = A.part + ((number + i) * A.Hkv + g) * D * D + at;
-    const float f = last && A.out ? 0.f : (float)exp2_64(A.part_log[(number + i) * A.Hkv + g]);
-    const f32x4 own = last && A.out ? f32x4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f32x4 *>(part);
-    *reinterpret_cast<f32x4 *>(part) = S;
-    S = S * f + own;
+  const size_t first = ((size_t)A.by_segment.of(begin) + b) * A.Hkv + g;
+  // (the last segment's sum is there only where nobody else brings the state behind it)
+  const int sums = A.out ? segments - 1 : segments;
+  constexpr int AT_ONCE = 8;
+  for (int i0 = 0; i0 < segments; i0 += AT_ONCE) {
+    f32x4 own[AT_ONCE];
+    float f[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const size_t part = first + (size_t)min(i0 + i, max(sums - 1, 0)) * A.Hkv;
+      own[i] = i0 + i < sums ? *reinterpret_cast<const f32x4 *>(A.part + part * D * D + at) : f32x4{0.f, 0.f, 0.f, 0.f};
+      f[i] = i0 + i < sums ? (float)exp2_64(A.part_log[part]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      if (i0 + i < segments) *reinterpret_cast<f32x4 *>(A.part + (first + (size_t)(i0 + i) * A.Hkv) * D * D + at) = S;
+      S = S * f[i] + own[i];
+      if (i0 + i + 1 == sums && !A.out) {
+        float *to = state_out(A, b);
+        if (to) *reinterpret_cast<f32x4 *>(to + (size_t)g * D * D + at) = S;
+      }
+    }
   }
-  if (A.out) return;
-  float *to = state_out(A, b);
-  if (to) *reinterpret_cast<f32x4 *>(to + (size_t)g * D * D + at) = S;
 }
 
 }  // namespace
@@ -524,15 +531,9 @@ hipError_t launch_linear_step(const LinearArgs &a, int d, hipStream_t s) {
 
 template <int D, bool OUT>
 static hipError_t launch_chunks(const LinearArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.numbers * a.Hkv)), block(2 * D);
-  const bool group = OUT && a.G > 1;
-  if (a.decay_rows) {
-    if (group) STS_LAUNCH((linear_chunk_kernel<D, OUT, true, OUT>), grid, block, 0, s, a);
-    else STS_LAUNCH((linear_chunk_kernel<D, OUT, true, false>), grid, block, 0, s, a);
-  } else {
-    if (group) STS_LAUNCH((linear_chunk_kernel<D, OUT, false, OUT>), grid, block, 0, s, a);
-    else STS_LAUNCH((linear_chunk_kernel<D, OUT, false, false>), grid, block, 0, s, a);
-  }
+  const dim3 grid((unsigned)(((int64_t)a.numbers * a.Hkv + STS_XCDS - 1) / STS_XCDS * STS_XCDS * (OUT ? a.G : 1))), block(2 * D);
+  if (a.decay_rows) STS_LAUNCH((linear_chunk_kernel<D, OUT, true>), grid, block, 0, s, a);
+  else STS_LAUNCH((linear_chunk_kernel<D, OUT, false>), grid, block, 0, s, a);
   return sts_take_launch_status();
 }
 hipError_t launch_linear_sums(const LinearArgs &a, int d, hipStream_t s) { return d == 128 ? launch_chunks<128, false>(a, s) : launch_chunks<64, false>(a, s); }
