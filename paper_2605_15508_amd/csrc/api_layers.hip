@@ -24,12 +24,15 @@ sts_status validate(int B, int T, int Hq, int Hkv, int d, int out_dtype, float s
   return STS_OK;
 }
 
+#ifndef STS_PARTS
+#define STS_PARTS 2
+#endif
 constexpr int64_t MOST_GROUPS = 1 << 24;      // workgroups of 256 threads that a grid's dimension holds
 
 struct LinearPlan {
   bool step;                 // the recurrent form
   int32_t each, max_len;     // rows of a sequence without starts; rows of the longest
-  int32_t segment, numbers;
+  int32_t segment, parts, numbers, part_numbers;
   bool several;              // a sequence may have more than one segment
   bool carry;                // states are handed on: between segments, and to the heads of a group
   size_t part_bytes, log_bytes;
@@ -47,18 +50,26 @@ sts_status plan_linear(const sts_linear_params *p, LinearPlan &pl) {
   pl.step = pl.max_len <= STS_LINEAR_STEP;
   if ((int64_t)p->B * p->Hkv * (p->d * p->d / 1024) >= MOST_GROUPS) return STS_EUNSUPPORTED;
   if (pl.step) return STS_OK;
-  // Segments: as many as the chip runs workgroups at once, two on a compute unit (four of half the waves), but of 128 rows at least.
-  int64_t segment = ((int64_t)p->T * p->Hq / ((p->d == 128 ? 2 : 4) * sts_cu_count()) + STS_LINEAR_CHUNK - 1) / STS_LINEAR_CHUNK * STS_LINEAR_CHUNK;
+  // Segments: as many as the chip runs workgroups at once, two on a compute unit (four of half the waves), counting half a one more for each sequence
+  // (its last), but of 128 rows at least. With many sequences, as many as cut those of twice the average length.
+  const int64_t at_once = (int64_t)(p->d == 128 ? 2 : 4) * sts_cu_count() / p->Hq, left = at_once - p->B / 2 > at_once / 2 ? at_once - p->B / 2 : at_once / 2;
+  int64_t segment = (p->T / (left > 0 ? left : 1) + STS_LINEAR_CHUNK) / STS_LINEAR_CHUNK * STS_LINEAR_CHUNK;
   if (segment < 128) segment = 128;
+  // The sums are worked out once for all heads of a group: in parts of the segments, so that they, too, fill the chip.
+  const int G = p->Hq / p->Hkv;
+  int64_t parts = G >= STS_PARTS ? STS_PARTS : 1;
+  segment = (segment + parts * STS_LINEAR_CHUNK - 1) / (parts * STS_LINEAR_CHUNK) * (parts * STS_LINEAR_CHUNK);
+  const int64_t numbers = piece_numbers(p->T, segment, p->B), part_numbers = piece_numbers(p->T, segment / parts, p->B);
+  if (numbers * p->Hq + STS_XCDS * STS_MAX_GROUP >= MOST_GROUPS || part_numbers * p->Hkv + STS_XCDS >= MOST_GROUPS) return STS_EUNSUPPORTED;
   pl.segment = (int32_t)segment;
-  const int64_t numbers = piece_numbers(p->T, segment, p->B);
-  if (numbers * p->Hq + STS_XCDS * STS_MAX_GROUP >= MOST_GROUPS) return STS_EUNSUPPORTED;
+  pl.parts = (int32_t)parts;
   pl.numbers = (int32_t)numbers;
-  pl.several = pl.max_len > segment;
+  pl.part_numbers = (int32_t)part_numbers;
+  pl.several = pl.max_len > (p->out ? segment : segment / parts);
   pl.carry = pl.several || (p->out && p->Hq > p->Hkv);
   if (pl.carry) {
-    pl.part_bytes = align256((size_t)numbers * p->Hkv * p->d * p->d * sizeof(float));
-    pl.log_bytes = align256((size_t)numbers * p->Hkv * sizeof(double));
+    pl.part_bytes = align256((size_t)part_numbers * p->Hkv * p->d * p->d * sizeof(float));
+    pl.log_bytes = align256((size_t)part_numbers * p->Hkv * sizeof(double));
   }
   return STS_OK;
 }
@@ -148,8 +159,12 @@ sts_status sts_linear_attn(const sts_linear_params *p, void *stream) {
   const int d = p->d;
   if (pl.step) return sts_run_kernel(STS_K_LINEAR_STEP, s, [&] { return launch_linear_step(a, d, s); }) == hipSuccess ? STS_OK : STS_EHIP;
   a.segment = pl.segment;
+  a.parts = pl.parts;
+  a.part_rows = pl.segment / pl.parts;
   a.numbers = pl.numbers;
-  a.by_segment = divide_by(pl.segment);
+  a.part_numbers = pl.part_numbers;
+  a.by_segment = divide_by(a.segment);
+  a.by_part = divide_by(a.part_rows);
   if (pl.carry) {
     if (!p->workspace || p->workspace_bytes < pl.part_bytes + pl.log_bytes || !aligned(p->workspace, 256)) return STS_EWORKSPACE;
     a.part = static_cast<float *>(p->workspace);

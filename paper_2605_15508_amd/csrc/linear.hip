@@ -168,17 +168,20 @@ __device__ __forceinline__ float scan32(float x) {
 }
 
 // OUT: results, from the state before the segment; else what the segment adds to the state (or, of a sequence with one segment, its
-// state). GATES: a decay for every row
-template <int D, bool OUT, bool GATES>
+// state)
+template <int D, bool OUT>
 __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs A) {
   constexpr int NW = D / 32;             // waves, each with 32 columns of the state
   constexpr int KS = D / 16, MT = D / 32, CH = D / 8;
   constexpr int NL = C * CH / (64 * NW), RL = 64 / CH;      // loads of a wave for 32 rows, rows that each covers
-  // Three chunks of K, V, Q, the decays and (two numbers for each row and wave) their sums. Arrays of their own, so that the compiler can tell the
-  // loads that fill one from the reads of another, and the sums are in the chunk's since a read of an array that no load fills waits for all loads.
-  constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, AT_G = (OUT ? 3 : 2) * TILE, AT_C = AT_G + (GATES ? NW * 16 : 0), ALL = AT_C + NW * 16;
-  constexpr int LOADS = (OUT ? 3 : 2) * NL + (GATES ? 1 : 0), STORES = OUT ? 2 : 0;      // of a wave and chunk
-  __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_2[ALL];
+  constexpr int BLOCK = D == 128 ? 15 : 9, MINE = (BLOCK + NW - 1) / NW;   // chunks whose decays are worked out at once, those of a wave
+  // Three chunks of K, V and Q, and a block's decays: for each row its sum c, its weight as a key, its factor as a query, and for each chunk four
+  // numbers. Arrays of their own, so that the compiler can tell the loads that fill one from the reads of another; it would have reads of an array
+  // that no load fills wait for all loads, so that one load of no bytes goes to the decays', too.
+  constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, ALL = (OUT ? 3 : 2) * TILE;
+  constexpr int LOADS = (OUT ? 3 : 2) * NL, STORES = OUT ? 2 : 0;      // of a wave and chunk
+  constexpr int AT_KEY = MINE * NW * C * 4, AT_QUERY = 2 * AT_KEY, AT_CHUNK = 3 * AT_KEY;
+  __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_2[ALL], lds_d[AT_CHUNK / 16 + 16];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
@@ -186,50 +189,58 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   // with a state of its own, which is the same) on one die, one after the other: they read the same K and V.
   const int turns = blockIdx.x / STS_XCDS, eight = OUT ? A.by_group.of(turns) : turns, hd = OUT ? turns - eight * A.G : 0;
   const int unit = eight * STS_XCDS + blockIdx.x % STS_XCDS;
-  if (unit >= A.numbers * A.Hkv) return;
+  if (unit >= (OUT ? A.numbers : A.part_numbers) * A.Hkv) return;
   const int number = A.by_heads.of(unit), g = unit - number * A.Hkv, head = g * A.G + hd;
-  const PackedPiece piece = find_piece(A.seqs, number, [&](int begin) { return A.by_segment.of(begin); });
+  const PackedPiece piece = find_piece(A.seqs, number, [&](int begin) { return OUT ? A.by_segment.of(begin) : A.by_part.of(begin); });
   if (piece.b < 0) return;
-  const int len = rows_of(A, piece.b, piece.len), first = piece.index * A.segment;
+  const int len = rows_of(A, piece.b, piece.len), most = OUT ? A.segment : A.part_rows, first = piece.index * most;
   const int segments = max((len + A.segment - 1) / A.segment, 1);
-  if (piece.index >= segments) return;
-  const bool last = piece.index == segments - 1;
-  if (!OUT && A.out && last) return;                 // (the results' kernel brings the last segment's state)
-  const int rows = min(A.segment, len - first), begin = piece.begin + first, chunks = (rows + C - 1) / C;
+  if (first >= max(len, 1)) return;
+  // (the last segment's state is brought by the results' kernel)
+  if (!OUT && A.out && piece.index >= (segments - 1) * A.parts) return;
+  // (the same for all lanes, which the compiler does not see)
+  const int rows = __builtin_amdgcn_readfirstlane(min(most, len - first)), begin = __builtin_amdgcn_readfirstlane(piece.begin + first), chunks = (rows + C - 1) / C;
+  const bool last = first + rows >= len;
 
-  // ---- loads, straight to LDS, rows behind the last from the last; behind the last chunk nothing is loaded (by loads of no bytes: the number of loads
-  // is always the same)
+  // ---- loads, straight to LDS. Rows behind the last lie behind the end that the loads are told and come as zeros; so do whole chunks (the number of
+  // loads is always the same).
   const int row0 = wave * NL * RL + lane / CH, slot0 = lane % CH;
-  auto rsrc = [&](const void *at, bool any) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, __builtin_amdgcn_readfirstlane(any ? -1 : 0), 0x00027000); };
-  auto load_rows = [&](int chunk, const uint16_t *base, int64_t stride, u32x4 *to) {
-    const __amdgpu_buffer_rsrc_t at = rsrc(base + (begin + (int64_t)chunk * C) * stride, chunk < chunks);
-    const int most = max(rows - 1 - chunk * C, 0);
+  uint32_t kv_off[NL], q_off[NL];
 #pragma unroll
-    for (int m = 0; m < NL; ++m) {
-      const int row = row0 + RL * m;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(to + (wave * NL + m) * 64), 16, (int)((uint32_t)min(row, most) * (uint32_t)(stride * 2) + 16 * place<D>(row, slot0)), 0, 0, 0);
-    }
+  for (int m = 0; m < NL; ++m) {
+    const int row = row0 + RL * m;
+    kv_off[m] = (uint32_t)row * (uint32_t)(A.kv_stride_n * 2) + 16 * place<D>(row, slot0);
+    q_off[m] = (uint32_t)row * (uint32_t)(A.q_stride_n * 2) + 16 * place<D>(row, slot0);
+  }
+  auto load_rows = [&](int chunk, const uint16_t *base, int64_t stride, const uint32_t (&off)[NL], u32x4 *to) {
+    const int n = __builtin_amdgcn_readfirstlane(min(rows - chunk * C, C)), end = n > 0 ? (n - 1) * (int)(stride * 2) + 2 * D : 0;
+    const __amdgpu_buffer_rsrc_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(base + (int64_t)chunk * C * stride), 0, end, 0x00027000);
+#pragma unroll
+    for (int m = 0; m < NL; ++m) __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(to + (wave * NL + m) * 64), 16, (int)off[m], 0, 0, 0);
   };
-  const uint16_t *k = A.k + g * A.kv_stride_h, *v = A.v + g * A.kv_stride_h, *q = A.q + head * A.q_stride_h;
+  const uint16_t *k = A.k + begin * A.kv_stride_n + g * A.kv_stride_h, *v = A.v + begin * A.kv_stride_n + g * A.kv_stride_h;
+  const uint16_t *q = A.q + begin * A.q_stride_n + head * A.q_stride_h;
   auto load = [&](int chunk, u32x4 *to) {
-    load_rows(chunk, k, A.kv_stride_n, to);
-    load_rows(chunk, v, A.kv_stride_n, to + AT_V);
-    if (GATES)           // (each wave has them to itself, both halves the same)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(A.decay + (begin + (size_t)chunk * C) * A.Hkv + g, chunk < chunks), (lds_ptr)(to + AT_G + wave * 16), 4,
-                                               (int)((uint32_t)min(col, max(rows - 1 - chunk * C, 0)) * (uint32_t)A.Hkv * 4), 0, 0, 0);
-    if (OUT) load_rows(chunk, q, A.q_stride_n, to + AT_Q);
+    load_rows(chunk, k, A.kv_stride_n, kv_off, to);
+    load_rows(chunk, v, A.kv_stride_n, kv_off, to + AT_V);
+    if (OUT) load_rows(chunk, q, A.q_stride_n, q_off, to + AT_Q);
     asm volatile("" ::: "memory");       // (a chunk's stores come behind these loads: see `turn`)
   };
-  // decays in powers of two (2^-150 is 0 in fp32; an infinite sum would have no differences)
-  auto power = [](float decay) { return decay * LOG2E < -150.f ? -150.f : decay * LOG2E; };
-  const float fixed = GATES ? 0.f : power(A.decay[g]);
+  // (a wave's part of a block's decays: row `col` of every NW-th chunk)
+  float gates[MINE];
+  auto load_gates = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) gates[i] = A.decay[A.decay_rows ? (begin + (size_t)min((base + wave + i * NW) * C + col, max(rows - 1, 0))) * A.Hkv + g : g];
+  };
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(A.k), 0, 0, 0x00027000), (lds_ptr)lds_d, 4, 0, 0, 0, 0);
+  if (rows > 0) load_gates(0);
   load(0, lds_0);
 
   // ---- the state: lane (h, col) has column 32 wave + col, in element 4 j + i of tile m the row 32 m + 16 (j / 2) + 8 h + 4 (j % 2) + i
   f32x16 S[MT];
-  const size_t part_at = ((size_t)number * A.Hkv + g) * D * D;
+  const size_t part = (OUT ? (size_t)A.by_part.of(piece.begin) + piece.b + (size_t)piece.index * A.parts : (size_t)number) * A.Hkv + g, part_at = part * D * D;
   // (Heads of a group start from a copy of a sequence's state: the one that writes the state behind its rows may be done before another begins.)
-  const bool carried = segments > 1 || (OUT && A.G > 1);
+  const bool carried = A.part && (OUT ? segments > 1 || A.G > 1 : A.out || len > A.part_rows);
   const float *from = carried ? (OUT ? A.part + part_at : nullptr) : state_in(A, piece.b);
   if (!carried && from) from += (size_t)g * D * D;
   const int s_at = 8 * h * D + 32 * wave + col;
@@ -265,168 +276,112 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   // The chunk has come: behind its loads lie the next chunk's and the last chunk's stores at least (memory operations end in their order). And
   // what was read is in registers.
   auto turn = [] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS + STORES) : "memory"); };
+  auto all_waves = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-  // The state is held as S / F, F the product of the decays since it was last multiplied out (its logarithm `low` is a sum in 64 bits, so that no
-  // factor's rounding adds up over a long sequence); what a chunk adds is divided by F instead.
+  // ---- Decays, in powers of two: c_i the sum over the chunk's rows up to i. With u_i = exp(c_i - c_32)
+  //     out_i = scale u_i (q_i . (exp(c_32) S) + sum exp(c_32 - c_j) (q_i . k_j) v_j),
+  // so that each key has one weight, which the state takes too. Not where u would leave fp32's range, or a decay is no number: in such a chunk (`apart`)
+  // each pair's weight is worked out.
+  // The state is held as S / F with 2^-16 < F <= 1: F is the decays' product so far but for a power of 2^16, by which the state is multiplied
+  // where F would leave that range (exactly), and a key's weight is divided by F. F's logarithm `low` is a sum in 64 bits: no factor's rounding adds up
+  // over a long sequence.
+  // A chunk's four numbers: the power of two; apart (1) or not (0); the logarithm of F before the chunk; nothing.
   double all = 0.0, low = 0.0;
-  auto multiply_out = [&] {
-    const float f = exp2_32(low);
-    low = 0.0;
+  const lds_ptr decays = (lds_ptr)lds_d;
+  auto number_of = [&](int at) { return *(lds_f32)(decays + at); };
+  auto work_out = [&](int base) {
+    auto power = [](float decay) { return decay * LOG2E < -150.f ? -150.f : decay * LOG2E; };      // (2^-150 is 0 in fp32; an infinite sum would have no differences)
+    float c[MINE], after[MINE];
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      const int chunk = wave + i * NW;
+      const float own = (base + chunk) * C + col < rows ? power(gates[i]) : 0.f;
+      const float turned = __shfl(own, (threadIdx.x & 32) | ((32 - col) & 31), 64);
+      c[i] = scan32(own);
+      after[i] = scan32(col ? turned : 0.f);        // behind row 31 - col
+      *(lds_f32)(decays + chunk * C * 4 + 4 * col) = c[i];
+    }
+    load_gates(base + BLOCK);
+    all_waves();
+    // (no branches but those that all lanes take alike: the loop around would get ways through it that there are not, and the compiler's waits with them)
+    const int mine = lane & 15;            // the lane's chunk
+    const float end = number_of((min(mine, BLOCK - 1) * C + 31) * 4);
+    double before = 0.0, behind = 0.0;
+    const double first = low;
+#pragma unroll
+    for (int i = 0; i < BLOCK; ++i) {      // (0 behind the last chunk)
+      before = mine == i ? low : before;
+      low += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, end), i));
+      behind = mine == i ? low : behind;
+    }
+    all += low - first;
+    auto whole = [](double x) { return __builtin_ceil(x * 0.0625) * 16.0; };
+    const double low_before = before - whole(before), low_behind = behind - whole(behind);
+    const float F = exp2_32(low_behind), F_inv = exp2_32(-low_behind), step = __builtin_amdgcn_exp2f((float)(whole(behind) - whole(before)));
+    low -= whole(low);
+    *(__attribute__((address_space(3))) f32x4 *)(decays + AT_CHUNK + 16 * mine) = f32x4{step, end >= -60.f ? 0.f : 1.f, (float)low_before, 0.f};
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      const int chunk = wave + i * NW, row = (base + chunk) * C, at = chunk * C * 4;
+      auto of_chunk = [&](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), min(chunk, BLOCK - 1))); };
+      const float factor = of_chunk(F), inverse = of_chunk(F_inv), c_end = of_chunk(end);
+      *(lds_f32)(decays + AT_KEY + at + 4 * (31 - col)) = row + 31 - col < rows ? __builtin_amdgcn_exp2f(after[i]) * inverse : 0.f;
+      *(lds_f32)(decays + AT_QUERY + at + 4 * col) = A.scale * (c_end >= -60.f ? factor * __builtin_amdgcn_exp2f(c[i] - c_end) : 1.f);
+    }
+    all_waves();
+  };
+  auto multiply = [&](float f) {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int e = 0; e < 16; ++e) S[m][e] *= f;
   };
-  auto body = [&](int chunk, u32x4 *lds, u32x4 *free) {
-    const int n = min(rows - chunk * C, C);
+
+  auto body = [&](int chunk, int in_block, u32x4 *lds, u32x4 *free) {
     turn();
-    load(chunk + 2, free);
-    // ---- decays: c = sum up to the row `col`, `after` the sum behind row `key`
-    const lds_ptr sums = (lds_ptr)(lds + AT_C + wave * 16);
-    float c, c_end, after;
-    int key = col;
-    if constexpr (GATES) {
-      const float gate = power(*(lds_f32)((lds_ptr)(lds + AT_G + wave * 16) + 4 * col)), own = col < n ? gate : 0.f;
-      c = scan32(own);
-      c_end = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c), 31));
-      const float turned = __shfl(own, (threadIdx.x & 32) | ((32 - col) & 31), 64);
-      key = 31 - col;
-      after = scan32(col ? turned : 0.f);
-    } else {
-      c = (float)(col + 1) * fixed;
-      c_end = (float)n * fixed;
-      after = (float)(n - 1 - col) * fixed;
-    }
-    // With u_i = exp(c_i - c_32), out_i = scale u_i (q_i . (exp(c_32) S) + sum exp(c_32 - c_j) (q_i . k_j) v_j): one weight for each key, which the state
-    // takes too. Not where u would leave fp32's range (or a decay is no number): there each pair has a weight of its own.
-    const bool apart = !(c_end >= -60.f);
-    const double low_before = low;
-    all += c_end;
-    low += c_end;
-    if (!apart && low < -16.0) multiply_out();
-    const float F = apart ? 1.f : exp2_32(low), F_inv = apart ? 1.f : exp2_32(-low);
-    *(lds_f32)(sums + 4 * col) = c;
-    *(lds_f32)(sums + 4 * (C + key)) = key < n ? __builtin_amdgcn_exp2f(after) * F_inv : 0.f;
+    load(chunk + 2, free);                 // (before the reads: behind them the compiler would wait for the next chunk's)
     // (what comes of these is made anew in every chunk, not kept in registers)
     int r_at = r_lane, v_at = v_lane, k_at = k_lane;
     asm("" : "+v"(r_at), "+v"(v_at), "+v"(k_at));
-    float left[16];                // weights of keys 8 j + 4 h + i
-#pragma unroll
-    for (int e = 0; e < 16; ++e) left[e] = *(lds_f32)(sums + 4 * (C + 8 * (e >> 2) + 4 * h + (e & 3)));
-    bf16x8 V[2];
+    // what is read is asked for first
+    const lds_ptr mine = decays + in_block * C * 4;
+    const f32x4 four = *(const __attribute__((address_space(3))) f32x4 *)(decays + AT_CHUNK + 16 * in_block);
+    bf16x8 K[KS], Q[KS], T[2 * MT], V[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) V[s] = transposed(lds + AT_V, v_at, 0, s);
-
+    float left[16];                // weights of keys 8 j + 4 h + i
+#pragma unroll
+    for (int e = 0; e < 16; ++e) left[e] = *(lds_f32)(mine + AT_KEY + 4 * (8 * (e >> 2) + 4 * h + (e & 3)));
+    const float own_factor = OUT ? *(lds_f32)(mine + AT_QUERY + 4 * col) : 0.f;
     if constexpr (OUT) {
-      const float own_factor = A.scale * (apart ? 1.f : F * __builtin_amdgcn_exp2f(c - c_end));
-      // Has the chunk a value that is infinite or no number? Rows before it do not see it, but 0 times it is not 0.
-      float z = 0.f;
-      const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t two = __builtin_bit_cast(u32x4, V[s])[e];
-          z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), none, z, false);
-        }
-      const bool odd = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
-      bf16x8 Q[KS];
-#pragma unroll
-      for (int s = 0; s < KS; ++s) Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)(lds + AT_Q) + (r_at ^ (32 * s))));
-      // X^T = K Q^T: row q . k of keys 8 j + 4 h + i and query col; O^T = S^T Q^T. The state enters the product as bf16 (half a step, 2^-8 of
-      // each number; the state itself stays as it is)
-      f32x16 X = {}, O = {};
-#pragma unroll
-      for (int s = 0; s < KS; ++s) X = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds + (r_at ^ (32 * s)))), Q[s], X, 0, 0, 0);
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          u32x4 w;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{S[m][8 * s + 2 * e], S[m][8 * s + 2 * e + 1]}), bf16x2));
-          O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), Q[2 * m + s], O, 0, 0, 0);
-        }
-      if (apart) {
-        const float f = exp2_32(low_before + c);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          O[e] *= f;
-          X[e] *= __builtin_amdgcn_exp2f(c - *(lds_f32)(sums + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) X[e] *= left[e];
-      }
-      // the weights, as bf16 (half a step, 2^-8 of each), none for keys behind the query, whatever their product is
-      bf16x8 P[2];
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          f32x2 x;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
-            x[i] = key <= col ? X[at] : 0.f;
-          }
-          w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-        }
-        P[s] = __builtin_bit_cast(bf16x8, w);
-      }
-      if (!odd) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], O, 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-          for (int key = 0; key < 16; ++key) {      // key by key, and a row is taken in only where it is seen
-            u32x4 own;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
-              own[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
-            }
-            const f32x16 zero = {};
-            const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, V[s]) & own),
-                                                                     __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, P[s]) & own), zero, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) O[e] += 16 * s + key <= col ? x[e] : 0.f;
-          }
-      }
-      // Two stores or more, which `turn` counts. The lane has channels 8 j + 4 h + i; as bf16 the halves of the wave exchange some, so that each
-      // has eight channels side by side.
-#pragma unroll
-      for (int e = 0; e < 16; ++e) O[e] *= own_factor;
-      const size_t at = ((begin + (size_t)chunk * C + col) * A.Hq + head) * D + 32 * wave;
-      if (A.out_dtype == STS_F32) {
-        if (col < n) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 8 * j + 4 * h) = f32x4{O[4 * j], O[4 * j + 1], O[4 * j + 2], O[4 * j + 3]};
-        }
-      } else {
-        u32x4 w[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{O[8 * j + 2 * i], O[8 * j + 2 * i + 1]}), bf16x2));
-            const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{O[8 * j + 4 + 2 * i], O[8 * j + 5 + 2 * i]}), bf16x2));
-            const auto swapped = __builtin_amdgcn_permlane32_swap(x, y, false, false);
-            w[j][i] = swapped[0];
-            w[j][2 + i] = swapped[1];
-          }
-        if (col < n) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(A.out) + at + 16 * j + 8 * h) = w[j];
-        }
+      for (int s = 0; s < KS; ++s) {
+        K[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds + (r_at ^ (32 * s))));
+        Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)(lds + AT_Q) + (r_at ^ (32 * s))));
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (chunk >= chunks) return;
+    const float f0 = four[0], f1 = four[1];        // (a cast of a vector's element would be one of its first)
+    const float f = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f0)));
+    if (f != 1.f && f1 == 0.f) multiply(f);
+    const bool apart = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f1)) != 0;
 
-    // ---- The state behind the chunk. V with its weights is the sum of three bf16 numbers, which hold an fp32's bits: the products enter the state
-    // as exactly as in fp32.
-    if (apart) multiply_out();
+    // ---- X^T = K Q^T: row q . k of keys 8 j + 4 h + i and query col; O^T = S^T Q^T. The state enters the product as bf16 (half a step, 2^-8 of
+    // each number; the state itself stays as it is). The order of instructions is given (the compiler's own waits for every operand by itself): matrix
+    // instructions alternate with what makes operands of the state and of V.
+    f32x16 X = {}, O = {};
+    if constexpr (OUT) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        X = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K[s], Q[s], X, 0, 0, 0);
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{S[s / 2][8 * (s % 2) + 2 * e], S[s / 2][8 * (s % 2) + 2 * e + 1]}), bf16x2));
+        O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), Q[s], O, 0, 0, 0);
+      }
+    }
+    // V with its weights as the sum of three bf16 numbers, which hold an fp32's bits: the products enter the state as exactly as in fp32
     bf16x8 W[3][2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -449,27 +404,156 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const bf16x8 K = transposed(lds, k_at, m, s);
+      for (int s = 0; s < 2; ++s) T[2 * m + s] = transposed(lds, k_at, m, s);
+    bool odd = false;
+    if constexpr (OUT) {
+      // Has the chunk a value that is infinite or no number? Rows before it do not see it, but 0 times it is not 0.
+      float z = 0.f;
+      const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
 #pragma unroll
-        for (int i = 2; i >= 0; --i) S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K, W[i][s], S[m], 0, 0, 0);
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t two = __builtin_bit_cast(u32x4, V[s])[e];
+          z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), none, z, false);
+        }
+      odd = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
+#pragma unroll
+      for (int i = 0; i < 2 * KS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 160 / (2 * KS), 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (apart) multiply(f);
+
+    // ---- The state, and the weights of the chunk's rows, as bf16 (half a step, 2^-8 of each): none for keys behind the query, whatever their
+    // product is. (Worked out without a look at `apart` and `odd`, and once more where one of them holds.)
+    f32x16 R = O;
+    auto weights = [&](const f32x16 &x, bf16x8 (&P)[2]) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f32x2 y;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
+            y[i] = key <= col ? x[at] : 0.f;
+          }
+          w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+        }
+        P[s] = __builtin_bit_cast(bf16x8, w);
+      }
+    };
+    if constexpr (OUT) {
+      f32x16 x;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = X[e] * left[e];
+      bf16x8 P[2];
+      weights(x, P);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) R = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], R, 0, 0, 0);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 2; i >= 0; --i)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(T[2 * m + s], W[i][s], S[m], 0, 0, 0);
+    if constexpr (OUT) {
+#pragma unroll
+      for (int i = 0; i < 6 * MT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x2, 48 / (4 * MT), 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (apart || odd) {
+        const float c = *(lds_f32)(mine + 4 * col), own = apart ? exp2_32((double)four[2] + c) : 1.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float pair = __builtin_amdgcn_exp2f(c - *(lds_f32)(mine + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));
+          R[e] = O[e] * own;
+          X[e] *= apart ? pair : left[e];
+        }
+        bf16x8 P[2];
+        weights(X, P);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          for (int key = 0; key < 16; ++key) {      // key by key, and a row is taken in only where it is seen
+            u32x4 own_key;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
+              own_key[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
+            }
+            const f32x16 zero = {};
+            const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, V[s]) & own_key),
+                                                                     __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, P[s]) & own_key), zero, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) R[e] += 16 * s + key <= col ? x[e] : 0.f;
+          }
+      }
+    }
+    if constexpr (OUT) {
+      // Two stores or more, which `turn` counts. The lane has channels 8 j + 4 h + i; as bf16 the halves of the wave exchange some, so that each
+      // has eight channels side by side.
+#pragma unroll
+      for (int e = 0; e < 16; ++e) R[e] *= own_factor;
+      // (rows behind the last are behind the end that the stores are told)
+      const int n = __builtin_amdgcn_readfirstlane(min(rows - chunk * C, C)), bytes = A.out_dtype == STS_F32 ? 4 : 2, pitch = A.Hq * D * bytes;
+      const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(static_cast<unsigned char *>(A.out) + (((int64_t)begin + chunk * C) * A.Hq + head) * D * bytes, 0,
+                                                                          (n - 1) * pitch + D * bytes, 0x00027000);
+      const int at = col * pitch + 32 * wave * bytes;
+      if (A.out_dtype == STS_F32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 o = {R[4 * j], R[4 * j + 1], R[4 * j + 2], R[4 * j + 3]};
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), to, at + 32 * j + 16 * h, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          u32x4 w;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{R[8 * j + 2 * i], R[8 * j + 2 * i + 1]}), bf16x2));
+            const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{R[8 * j + 4 + 2 * i], R[8 * j + 5 + 2 * i]}), bf16x2));
+            const auto swapped = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+            w[i] = swapped[0];
+            w[2 + i] = swapped[1];
+          }
+          __builtin_amdgcn_raw_buffer_store_b128(w, to, at + 32 * j + 16 * h, 0, 0);
+        }
+      }
+    }
   };
+  work_out(0);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // (no stores come behind the first loads)
   load(1, lds_1);
-  for (int chunk = 0; chunk < chunks; chunk += 3) {
-    body(chunk, lds_0, lds_2);
-    if (chunk + 1 >= chunks) break;
-    body(chunk + 1, lds_1, lds_0);
-    if (chunk + 2 >= chunks) break;
-    body(chunk + 2, lds_2, lds_1);
+  // (three chunks at a time, present or not: with more ways out of the loop than one the compiler would see ways back into it that there are not, and
+  // wait for the loads of a chunk to come)
+  for (int base = 0;;) {
+    int i = 0;
+    do {
+      body(base + i, i, lds_0, lds_2);
+      body(base + i + 1, i + 1, lds_1, lds_0);
+      body(base + i + 2, i + 2, lds_2, lds_1);
+      i += 3;
+    } while (i < BLOCK && base + i < chunks);
+    base += BLOCK;
+    if (base >= chunks) break;
+    all_waves();                           // (nobody reads the last block's decays any more)
+    work_out(base);
   }
+  multiply(exp2_32(low));
 
-  multiply_out();
   float *to;
-  if (segments > 1 && !OUT) {
+  if (!OUT && carried) {
     to = A.part + part_at;
-    if (threadIdx.x == 0) A.part_log[(size_t)number * A.Hkv + g] = all;
+    if (threadIdx.x == 0) A.part_log[part] = all;
   } else {
     if (!last || hd != 0) return;
     to = state_out(A, piece.b);
@@ -491,33 +575,35 @@ __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
   int begin, len;
   seq_rows(A.seqs, b, begin, len);
   len = rows_of(A, b, len);
-  const int segments = max((len + A.segment - 1) / A.segment, 1);
-  if (segments < 2 && !(A.out && A.G > 1)) return;
+  // (what the sums' kernel leaves: the parts before the last segment, or all of a sequence with several of them)
+  const int segments = max((len + A.segment - 1) / A.segment, 1), all = max((len + A.part_rows - 1) / A.part_rows, 1);
+  if (A.out ? segments < 2 && A.G == 1 : all < 2) return;
+  const int sums = A.out ? (segments - 1) * A.parts : all, stop = A.out ? sums + 1 : all;
   const float *from = state_in(A, b);
   f32x4 S = from ? *reinterpret_cast<const f32x4 *>(from + (size_t)g * D * D + at) : f32x4{0.f, 0.f, 0.f, 0.f};
-  const size_t first = ((size_t)A.by_segment.of(begin) + b) * A.Hkv + g;
-  // (the last segment's sum is there only where nobody else brings the state behind it)
-  const int sums = A.out ? segments - 1 : segments;
+  const size_t first = ((size_t)A.by_part.of(begin) + b) * A.Hkv + g;
   constexpr int AT_ONCE = 8;
-  for (int i0 = 0; i0 < segments; i0 += AT_ONCE) {
+  for (int i0 = 0, next = 0; i0 < stop; i0 += AT_ONCE) {
     f32x4 own[AT_ONCE];
     float f[AT_ONCE];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
       const size_t part = first + (size_t)min(i0 + i, max(sums - 1, 0)) * A.Hkv;
       own[i] = i0 + i < sums ? *reinterpret_cast<const f32x4 *>(A.part + part * D * D + at) : f32x4{0.f, 0.f, 0.f, 0.f};
-      f[i] = i0 + i < sums ? (float)exp2_64(A.part_log[part]) : 0.f;
+      f[i] = i0 + i < sums ? (float)exp2_64(A.part_log[part]) : 1.f;
     }
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
-      if (i0 + i < segments) *reinterpret_cast<f32x4 *>(A.part + (first + (size_t)(i0 + i) * A.Hkv) * D * D + at) = S;
-      S = S * f[i] + own[i];
-      if (i0 + i + 1 == sums && !A.out) {
-        float *to = state_out(A, b);
-        if (to) *reinterpret_cast<f32x4 *>(to + (size_t)g * D * D + at) = S;
+      if (A.out && i0 + i == next && next < stop) {
+        *reinterpret_cast<f32x4 *>(A.part + (first + (size_t)next * A.Hkv) * D * D + at) = S;
+        next += A.parts;
       }
+      S = S * f[i] + own[i];
     }
   }
+  if (A.out) return;
+  float *to = state_out(A, b);
+  if (to) *reinterpret_cast<f32x4 *>(to + (size_t)g * D * D + at) = S;
 }
 
 }  // namespace
@@ -531,9 +617,8 @@ hipError_t launch_linear_step(const LinearArgs &a, int d, hipStream_t s) {
 
 template <int D, bool OUT>
 static hipError_t launch_chunks(const LinearArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)a.numbers * a.Hkv + STS_XCDS - 1) / STS_XCDS * STS_XCDS * (OUT ? a.G : 1))), block(2 * D);
-  if (a.decay_rows) STS_LAUNCH((linear_chunk_kernel<D, OUT, true>), grid, block, 0, s, a);
-  else STS_LAUNCH((linear_chunk_kernel<D, OUT, false>), grid, block, 0, s, a);
+  const dim3 grid((unsigned)(((int64_t)(OUT ? a.numbers : a.part_numbers) * a.Hkv + STS_XCDS - 1) / STS_XCDS * STS_XCDS * (OUT ? a.G : 1))), block(2 * D);
+  STS_LAUNCH((linear_chunk_kernel<D, OUT>), grid, block, 0, s, a);
   return sts_take_launch_status();
 }
 hipError_t launch_linear_sums(const LinearArgs &a, int d, hipStream_t s) { return d == 128 ? launch_chunks<128, false>(a, s) : launch_chunks<64, false>(a, s); }
