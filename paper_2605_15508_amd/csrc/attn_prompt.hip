@@ -31,6 +31,46 @@ template <int D> __device__ __forceinline__ int v_chunk(int r, int c) { return D
 // bits 0 .. n - 1, none for n <= 0
 __device__ __forceinline__ uint64_t first_keys(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
+// sum over the wave (DPP: within rows of 16, then along the rows)
+__device__ __forceinline__ int wave_sum(int x) {
+  auto add = [&](auto ctrl, auto rows) { x += __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(rows)::value, 0xf, true); };
+  add(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());      // row_shr:1
+  add(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+  add(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+  add(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+  add(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());      // row_bcast:15
+  add(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());      // row_bcast:31
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// The block of rank `rank` where those furthest along their sequences, which see the most keys, come first: of up to 64 sequences, one to a lane. A
+// block's place in its sequence is the least i with no more than `rank` blocks behind it.
+__device__ __forceinline__ PackedPiece block_of_rank(const PackedSeqs &s, int G, int rank) {
+  const int lane = threadIdx.x & 63, b = min(lane, s.B - 1);
+  const int begin = min(max(s.starts[b], 0), s.T), len = max(min(max(s.starts[b + 1], 0), s.T) - begin, 0);
+  const int blocks = lane < s.B ? (int)(((int64_t)len * G + ROWS - 1) / ROWS) : 0;
+  int lo = 0, hi = 0, behind = 0;
+  if (s.B == 1) {
+    lo = __builtin_amdgcn_readlane(blocks, 0) - 1 - rank;
+    behind = rank;
+  } else {
+    if (rank >= wave_sum(blocks)) return {-1, 0, 0, 0};
+    while (__builtin_amdgcn_ballot_w64(blocks > hi) != 0) hi = 2 * hi + 1;      // (the longest sequence's blocks, up to a power of two: 2^24 at most)
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1, n = wave_sum(max(blocks - mid - 1, 0));
+      if (n <= rank) hi = mid;
+      else lo = mid + 1;
+    }
+    behind = wave_sum(max(blocks - lo - 1, 0));
+  }
+  const uint64_t there = __builtin_amdgcn_ballot_w64(blocks > lo);
+  const int nth = __builtin_amdgcn_mbcnt_hi((uint32_t)(there >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there, 0));
+  const uint64_t mine = __builtin_amdgcn_ballot_w64(blocks > lo && nth == rank - behind);
+  if (lo < 0 || mine == 0) return {-1, 0, 0, 0};
+  const int k = __builtin_ctzll(mine);
+  return {k, __builtin_amdgcn_readlane(begin, k), __builtin_amdgcn_readlane(len, k), lo};
+}
+
 template <int D>
 __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kernel(const PromptArgs A) {
   constexpr int KS = D / 16;             // contraction steps of S
@@ -43,11 +83,12 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
-  // Blocks of one KV head next to each other on one die (workgroup i runs on die i % 8); late ones, which have more keys, first.
+  // Blocks of one KV head next to each other on one die (workgroup i runs on die i % 8), those with more keys first.
   const int total = gridDim.x, x = blockIdx.x % STS_XCDS;
   const int j = x * (total / STS_XCDS) + min(x, total % STS_XCDS) + blockIdx.x / STS_XCDS;
-  const int g = A.by_numbers.of(j), number = A.numbers - 1 - (j - g * A.numbers);
-  const PackedPiece piece = find_piece(A.seqs, number, [&](int begin) { return (int)((int64_t)begin * A.G / ROWS); });
+  const int g = A.by_numbers.of(j), rank = j - g * A.numbers;
+  const PackedPiece piece = A.seqs.B <= 64 ? block_of_rank(A.seqs, A.G, rank)
+                                           : find_piece(A.seqs, A.numbers - 1 - rank, [&](int begin) { return (int)((int64_t)begin * A.G / ROWS); });
   const int L = piece.len, rows = L * A.G, row_0 = piece.index * ROWS;
   if (piece.b < 0 || row_0 >= rows) return;
 
@@ -157,9 +198,10 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
     for (int i = 4; i < 16; ++i) m[i & 3] = top(m[i & 3], top(S[0][i], S[1][i]));
     return sl2 * top(top(m[0], m[1]), top(m[2], m[3]));
   };
-  // the running maximum takes in a tile's; both halves of the wave hold half of a query's scores
+  // The running maximum takes in a tile's; both halves of the wave hold half of a query's scores. It may lag behind by a factor of 2^8, which weights and
+  // sums have room for: so the sums are multiplied anew in the first tiles only, not wherever one of 32 queries finds a larger score.
   auto raise = [&](float mine) {
-    if (__builtin_amdgcn_ballot_w64(mine > m_run) != 0) {
+    if (__builtin_amdgcn_ballot_w64(mine > m_run + 8.f) != 0) {
       const uint32_t w = __builtin_bit_cast(uint32_t, mine);
       const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
       const uint32_t q0 = q[0], q1 = q[1];
