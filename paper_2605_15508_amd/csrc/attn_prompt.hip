@@ -111,8 +111,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
   }
 
   // ---- loads, straight to LDS: load m of a wave fills the 1 KB of rows (wave NL + m) RL .., lane by lane, so the permutation of a
-  // row's chunks is in what a lane asks for. Rows that no query of the block sees are read from the last one that some query does: their
-  // weight is 0, but 0 times what lies there may be NaN.
+  // row's chunks is in what a lane asks for. Rows that no query of the block sees lie behind the end that the loads are told and come as zeros.
   const int row0 = wave * NL * RL + lane / CH, slot0 = lane % CH;
   const int64_t row_bytes = A.kv_stride_n * 2, from = (piece.begin * A.kv_stride_n + g * A.kv_stride_h) * 2;
   const unsigned char *kbase = reinterpret_cast<const unsigned char *>(A.k) + from, *vbase = reinterpret_cast<const unsigned char *>(A.v) + from;
@@ -123,21 +122,13 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
     k_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * k_chunk<D>(row, slot0);
     v_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * v_chunk<D>(row, slot0);
   }
-  // K's or V's tile t (past the last: the last again, which nobody reads)
+  // K's or V's tile t (past the last: nothing but zeros)
   auto load = [&](int t, const unsigned char *base, u32x4 *to, bool is_v) {
-    const int n0 = min(t, tiles - 1) * TK;
+    const int n = __builtin_amdgcn_readfirstlane(min(places - t * TK, TK)), end = n > 0 ? (n - 1) * (int)row_bytes + 2 * D : 0;
     u32x4 *const mine = to + wave * NL * 64;
-    const __amdgpu_buffer_rsrc_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(base + n0 * row_bytes), 0, 0xffffffff, 0x00027000);
-    if (n0 + TK <= places) {
+    const __amdgpu_buffer_rsrc_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(base + (int64_t)t * TK * row_bytes), 0, end, 0x00027000);
 #pragma unroll
-      for (int m = 0; m < NL; ++m) __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(mine + 64 * m), 16, (int)(is_v ? v_off[m] : k_off[m]), 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int m = 0; m < NL; ++m) {
-        const int row = row0 + RL * m, chunk = is_v ? v_chunk<D>(row, slot0) : k_chunk<D>(row, slot0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(mine + 64 * m), 16, (int)((uint32_t)min(row, places - 1 - n0) * (uint32_t)row_bytes + 16 * chunk), 0, 0, 0);
-      }
-    }
+    for (int m = 0; m < NL; ++m) __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(mine + 64 * m), 16, (int)(is_v ? v_off[m] : k_off[m]), 0, 0, 0);
   };
 
   float m_run = -INFINITY, l_run = 0.f;
@@ -304,7 +295,75 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) S[kt] = N[kt];
     };
-    for (int t = 0;; t += 2) {
+    // Tiles that every query of the block sees whole, and so does the next: nothing is hidden, and no value that some do not see. The order of
+    // instructions is given, step by step (the compiler asks for each operand right before it needs it): matrix instructions beside a part of the
+    // weights, operands asked for two steps ahead.
+    auto whole = [&](int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
+      arrived();
+      load(t + 2, kbase, k_free, false);
+      load(t + 1, vbase, v_free, true);
+      int k_at = k_lane, v_at = v_lane;
+      asm("" : "+v"(k_at), "+v"(v_at));
+      constexpr int PART = 16 / KS;          // pairs of weights beside the two matrix instructions of a step
+      const f32x16 zero = {};
+      f32x16 N[2];
+      u32x4 P[4], V[2][DT];
+      bf16x8 K[3][2];
+      auto read_k = [&](int s) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) K[s % 3][kt] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)k_next + (k_at ^ (32 * s)) + 32 * kt * CH * 16));
+      };
+      auto read_v = [&](int s) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) V[s % 2][dt] = v_operand(v, v_at, dt, s);
+      };
+      const float m_ref = m_run == -INFINITY ? 0.f : m_run;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      read_k(0);
+      read_k(1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        if (s + 2 < KS) read_k(s + 2);
+        else if (s + 2 == KS) read_v(0);
+        else read_v(1);
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) N[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K[s % 3][kt], Q[s], s ? N[kt] : zero, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < PART; ++i) {
+          const int pair = s * PART + i, at = 2 * (pair & 7);
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[pair >> 3][at], sl2, -m_ref));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[pair >> 3][at + 1], sl2, -m_ref));
+          sum[pair & 3] += p0 + p1;
+          P[pair >> 2][pair & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      float most[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, V[s % 2][dt]), __builtin_bit_cast(bf16x8, P[s]), acc[dt], 0, 0, 0);
+        if (s + 2 < 4) read_v(s + 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float two = top(N[0][4 * s + i], N[1][4 * s + i]);
+          most[i] = s ? top(most[i], two) : two;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      raise(sl2 * top(top(most[0], most[1]), top(most[2], most[3])));
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) S[kt] = N[kt];
+    };
+    const int seen_whole = __builtin_amdgcn_readfirstlane((b_lo + 1) / TK);
+    int t = 0;
+    for (; t + 2 < seen_whole; t += 2) {
+      whole(t, lds_k1, lds_k0, lds_v0, lds_v1);
+      whole(t + 1, lds_k0, lds_k1, lds_v1, lds_v0);
+    }
+    for (;; t += 2) {
       step(t, lds_k1, lds_k0, lds_v0, lds_v1);
       if (t + 1 >= tiles) break;
       step(t + 1, lds_k0, lds_k1, lds_v1, lds_v0);
