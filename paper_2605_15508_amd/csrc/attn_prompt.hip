@@ -264,41 +264,10 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
     product(lds_k0, S);
     if (masked(0)) hide(0, S);
     raise(highest(S));
-    auto step = [&](int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
-      arrived();
-      load(t + 2, kbase, k_free, false);
-      load(t + 1, vbase, v_free, true);
-      bool odd = false;
-      if (partly_seen(t)) {
-        look_through(v, t & 1);
-        odd = odd_values(t & 1);
-      }
-      f32x16 N[2];
-      u32x4 P[4];
-      product(k_next, N);
-      const float sum = weights(S, P);
-      if (!odd) {
-        l_run += sum;
-        int v_at = v_lane;
-        asm("" : "+v"(v_at));
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v, v_at, dt, s)), __builtin_bit_cast(bf16x8, P[s]), acc[dt], 0, 0, 0);
-      }
-      later |= odd;
-      if (t + 1 < tiles) {
-        if (masked(t + 1)) hide(t + 1, N);
-        raise(highest(N));
-      }
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) S[kt] = N[kt];
-    };
-    // Tiles that every query of the block sees whole, and so does the next: nothing is hidden, and no value that some do not see. The order of
-    // instructions is given, step by step (the compiler asks for each operand right before it needs it): matrix instructions beside a part of the
-    // weights, operands asked for two steps ahead.
-    auto whole = [&](int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
+    // The order of instructions is given, step by step (the compiler asks for each operand right before it needs it): matrix instructions beside a part
+    // of the weights, operands asked for two steps ahead. `edge`: a tile that not every query of the block sees whole, or such a next one.
+    auto step = [&](auto edge, int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
+      constexpr bool EDGE = decltype(edge)::value;
       arrived();
       load(t + 2, kbase, k_free, false);
       load(t + 1, vbase, v_free, true);
@@ -317,6 +286,11 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) V[s % 2][dt] = v_operand(v, v_at, dt, s);
       };
+      bool odd = false;
+      if (EDGE && partly_seen(t)) {
+        look_through(v, t & 1);
+        odd = odd_values(t & 1);
+      }
       const float m_ref = m_run == -INFINITY ? 0.f : m_run;
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
       read_k(0);
@@ -339,34 +313,45 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      float most[4];
+      if (!EDGE || !odd) {
+        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        float most[4];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < 4; ++s) {
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, V[s % 2][dt]), __builtin_bit_cast(bf16x8, P[s]), acc[dt], 0, 0, 0);
-        if (s + 2 < 4) read_v(s + 2);
+          for (int dt = 0; dt < DT; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, V[s % 2][dt]), __builtin_bit_cast(bf16x8, P[s]), acc[dt], 0, 0, 0);
+          if (s + 2 < 4) read_v(s + 2);
+          if (!EDGE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float two = top(N[0][4 * s + i], N[1][4 * s + i]);
-          most[i] = s ? top(most[i], two) : two;
+            for (int i = 0; i < 4; ++i) {
+              const float two = top(N[0][4 * s + i], N[1][4 * s + i]);
+              most[i] = s ? top(most[i], two) : two;
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+        if (!EDGE) raise(sl2 * top(top(most[0], most[1]), top(most[2], most[3])));
       }
-      raise(sl2 * top(top(most[0], most[1]), top(most[2], most[3])));
+      if (EDGE) {
+        later |= odd;
+        if (t + 1 < tiles) {
+          if (masked(t + 1)) hide(t + 1, N);
+          raise(highest(N));
+        }
+      }
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) S[kt] = N[kt];
     };
     const int seen_whole = __builtin_amdgcn_readfirstlane((b_lo + 1) / TK);
     int t = 0;
     for (; t + 2 < seen_whole; t += 2) {
-      whole(t, lds_k1, lds_k0, lds_v0, lds_v1);
-      whole(t + 1, lds_k0, lds_k1, lds_v1, lds_v0);
+      step(std::false_type(), t, lds_k1, lds_k0, lds_v0, lds_v1);
+      step(std::false_type(), t + 1, lds_k0, lds_k1, lds_v1, lds_v0);
     }
     for (;; t += 2) {
-      step(t, lds_k1, lds_k0, lds_v0, lds_v1);
+      step(std::true_type(), t, lds_k1, lds_k0, lds_v0, lds_v1);
       if (t + 1 >= tiles) break;
-      step(t + 1, lds_k0, lds_k1, lds_v1, lds_v0);
+      step(std::true_type(), t + 1, lds_k0, lds_k1, lds_v1, lds_v0);
       if (t + 2 >= tiles) break;
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);              // all that was asked for has come
