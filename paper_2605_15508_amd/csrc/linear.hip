@@ -154,17 +154,34 @@ template <int D> __device__ __forceinline__ int place(int r, int c) {
   return D == 128 ? c ^ ((r & 3) << 2 | (r >> 2 & 3)) : c ^ ((r >> 1 & 1) << 2 | (r >> 2 & 3));
 }
 
-// sums over the lanes of each half up to the lane's own (DPP: within rows of 16, then the first row's total to the second)
-__device__ __forceinline__ float scan32(float x) {
-  auto add = [&](auto ctrl, auto rows) {
-    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, true));
-  };
-  add(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());      // row_shr:1
-  add(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
-  add(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
-  add(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
-  const float first = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(((threadIdx.x & 32) | 15) << 2, __builtin_bit_cast(int, x)));
-  return threadIdx.x & 16 ? x + first : x;
+// Sums over a half's 32 lanes, of which both halves hold the same: up to the lane's own, or behind it. Within rows of 16 lanes by shifts, from row to row
+// by a scalar.
+template <int FIRST>
+__device__ __forceinline__ float scan16(float x) {
+  auto add = [&](auto ctrl) { x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true)); };
+  add(std::integral_constant<int, FIRST>());
+  add(std::integral_constant<int, FIRST + 1>());
+  add(std::integral_constant<int, FIRST + 3>());
+  add(std::integral_constant<int, FIRST + 7>());
+  return x;
+}
+__device__ __forceinline__ float lane_of(float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); }
+__device__ __forceinline__ float sum_up_to(float x) {
+  x = scan16<0x111>(x);                                    // row_shr
+  return threadIdx.x & 16 ? x + lane_of(x, 15) : x;
+}
+__device__ __forceinline__ float sum_behind(float x) {
+  const float next = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x101, 0xf, 0xf, true));      // row_shl:1
+  const float y = scan16<0x101>((threadIdx.x & 31) == 15 ? lane_of(x, 16) : next);
+  return threadIdx.x & 16 ? y : y + lane_of(y, 16);
+}
+
+// A part's numbers lie as the waves hold them: element 4 e .. of tile m, four side by side, lane by lane, wave by wave. Place 4 q .. is this number of
+// the state and the three below it:
+template <int D> __device__ __forceinline__ int state_place(int q) {
+  constexpr int NW = D / 32;
+  const int lane = q & 63, wave = (q >> 6) % NW, e = (q >> 6) / NW % 4, m = (q >> 6) / NW / 4;
+  return (32 * m + 16 * (e >> 1) + 8 * (lane >> 5) + 4 * (e & 1)) * D + 32 * wave + (lane & 31);
 }
 
 // OUT: results, from the state before the segment; else what the segment adds to the state (or, of a sequence with one segment, its
@@ -243,8 +260,17 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   const bool carried = A.part && (OUT ? segments > 1 || A.G > 1 : A.out || len > A.part_rows);
   const float *from = carried ? (OUT ? A.part + part_at : nullptr) : state_in(A, piece.b);
   if (!carried && from) from += (size_t)g * D * D;
-  const int s_at = 8 * h * D + 32 * wave + col;
-  if (from) {
+  const int s_at = 8 * h * D + 32 * wave + col, p_at = 256 * wave + 4 * lane;
+  if (from && carried) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(from + p_at + (4 * m + e) * NW * 256);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[m][4 * e + i] = x[i];
+      }
+  } else if (from) {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -296,9 +322,8 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     for (int i = 0; i < MINE; ++i) {
       const int chunk = wave + i * NW;
       const float own = (base + chunk) * C + col < rows ? power(gates[i]) : 0.f;
-      const float turned = __shfl(own, (threadIdx.x & 32) | ((32 - col) & 31), 64);
-      c[i] = scan32(own);
-      after[i] = scan32(col ? turned : 0.f);        // behind row 31 - col
+      c[i] = sum_up_to(own);
+      after[i] = sum_behind(own);
       *(lds_f32)(decays + chunk * C * 4 + 4 * col) = c[i];
     }
     load_gates(base + BLOCK);
@@ -325,7 +350,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
       const int chunk = wave + i * NW, row = (base + chunk) * C, at = chunk * C * 4;
       auto of_chunk = [&](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), min(chunk, BLOCK - 1))); };
       const float factor = of_chunk(F), inverse = of_chunk(F_inv), c_end = of_chunk(end);
-      *(lds_f32)(decays + AT_KEY + at + 4 * (31 - col)) = row + 31 - col < rows ? __builtin_amdgcn_exp2f(after[i]) * inverse : 0.f;
+      *(lds_f32)(decays + AT_KEY + at + 4 * col) = row + col < rows ? __builtin_amdgcn_exp2f(after[i]) * inverse : 0.f;
       *(lds_f32)(decays + AT_QUERY + at + 4 * col) = A.scale * (c_end >= -60.f ? factor * __builtin_amdgcn_exp2f(c[i] - c_end) : 1.f);
     }
     all_waves();
@@ -550,16 +575,19 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   }
   multiply(exp2_32(low));
 
-  float *to;
   if (!OUT && carried) {
-    to = A.part + part_at;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4 *>(A.part + part_at + p_at + (4 * m + e) * NW * 256) = f32x4{S[m][4 * e], S[m][4 * e + 1], S[m][4 * e + 2], S[m][4 * e + 3]};
     if (threadIdx.x == 0) A.part_log[part] = all;
-  } else {
-    if (!last || hd != 0) return;
-    to = state_out(A, piece.b);
-    if (!to) return;
-    to += (size_t)g * D * D;
+    return;
   }
+  if (!last || hd != 0) return;
+  float *to = state_out(A, piece.b);
+  if (!to) return;
+  to += (size_t)g * D * D;
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -570,7 +598,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 template <int D>
 __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
   constexpr int PER = D * D / 1024;      // workgroups for a state
-  const int unit = blockIdx.x / PER, at = 4 * ((blockIdx.x % PER) * 256 + threadIdx.x);
+  const int unit = blockIdx.x / PER, q = (blockIdx.x % PER) * 256 + threadIdx.x, at = 4 * q, place = state_place<D>(q);
   const int b = A.by_heads.of(unit), g = unit - b * A.Hkv;
   int begin, len;
   seq_rows(A.seqs, b, begin, len);
@@ -580,7 +608,11 @@ __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
   if (A.out ? segments < 2 && A.G == 1 : all < 2) return;
   const int sums = A.out ? (segments - 1) * A.parts : all, stop = A.out ? sums + 1 : all;
   const float *from = state_in(A, b);
-  f32x4 S = from ? *reinterpret_cast<const f32x4 *>(from + (size_t)g * D * D + at) : f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 S = {0.f, 0.f, 0.f, 0.f};
+  if (from) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) S[i] = from[(size_t)g * D * D + place + i * D];
+  }
   const size_t first = ((size_t)A.by_part.of(begin) + b) * A.Hkv + g;
   constexpr int AT_ONCE = 8;
   for (int i0 = 0, next = 0; i0 < stop; i0 += AT_ONCE) {
@@ -603,7 +635,9 @@ __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
   }
   if (A.out) return;
   float *to = state_out(A, b);
-  if (to) *reinterpret_cast<f32x4 *>(to + (size_t)g * D * D + at) = S;
+  if (!to) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) to[(size_t)g * D * D + place + i * D] = S[i];
 }
 
 }  // namespace
