@@ -74,7 +74,9 @@ template <int D>
 __global__ void __launch_bounds__(256) linear_step_kernel(const LinearArgs A) {
   constexpr int RK = D / 32;              // rows of the state per thread
   constexpr int SLICES = D / 32, MAX = STS_LINEAR_STEP, HEADS = 4;      // heads that are worked on at once
-  __shared__ uint16_t lds_k[MAX][D], lds_v[MAX][32];
+  constexpr int QUERIES = 64, CHUNKS = D / 8, ASKS = QUERIES * CHUNKS / 256;
+  static_assert(QUERIES >= STS_MAX_GROUP && MAX * CHUNKS <= 256, "");
+  __shared__ __attribute__((aligned(16))) uint16_t lds_k[MAX][D], lds_v[MAX][32], lds_q[QUERIES][D];
   __shared__ float lds_f[MAX];
   __shared__ __attribute__((aligned(16))) float lds_o[2][HEADS][4][32];
 
@@ -89,20 +91,43 @@ __global__ void __launch_bounds__(256) linear_step_kernel(const LinearArgs A) {
   const float *from = state_in(A, b);
   const size_t head_at = (size_t)g * D * D;
 #pragma unroll
-  for (int r = 0; r < RK; ++r) S[r] = from ? *reinterpret_cast<const f32x4 *>(from + head_at + (row + r) * D + col) : f32x4{0.f, 0.f, 0.f, 0.f};
-  // the rows of K and V that are needed, and the decays
-  for (int i = tid; i < n * (D / 8); i += 256) {
-    const int t = i / (D / 8), c = i % (D / 8);
-    *reinterpret_cast<u32x4 *>(&lds_k[t][8 * c]) = *reinterpret_cast<const u32x4 *>(A.k + (begin + (int64_t)t) * A.kv_stride_n + g * A.kv_stride_h + 8 * c);
+  for (int r = 0; r < RK; ++r) S[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (from) {
+#pragma unroll
+    for (int r = 0; r < RK; ++r) S[r] = *reinterpret_cast<const f32x4 *>(from + head_at + (row + r) * D + col);
   }
-  for (int i = tid; i < n * 4; i += 256)
-    *reinterpret_cast<u32x4 *>(&lds_v[i / 4][8 * (i % 4)]) =
-        *reinterpret_cast<const u32x4 *>(A.v + (begin + (int64_t)(i / 4)) * A.kv_stride_n + g * A.kv_stride_h + 32 * slice + 8 * (i % 4));
-  if (tid < n) lds_f[tid] = (float)exp2_64((double)A.decay[A.decay_rows ? (begin + (size_t)tid) * A.Hkv + g : g] * LOG2E_64);
+  // Queries of as many rows as there is room for. They, the rows of K and V and the decays are all asked for before any is waited for.
+  const int rows = QUERIES / A.G;
+  u32x4 q[ASKS];
+  auto ask = [&](int t0) {
+    const int count = min(rows, n - t0) * A.G * CHUNKS;
+#pragma unroll
+    for (int i = 0; i < ASKS; ++i) {
+      const int at = tid + 256 * i, r = A.by_group.of(at / CHUNKS), h = at / CHUNKS - r * A.G;
+      if (at < count) q[i] = *reinterpret_cast<const u32x4 *>(A.q + (begin + t0 + (int64_t)r) * A.q_stride_n + (g * A.G + h) * A.q_stride_h + 8 * (at % CHUNKS));
+    }
+  };
+  auto put = [&](int t0) {
+    const int count = min(rows, n - t0) * A.G * CHUNKS;
+#pragma unroll
+    for (int i = 0; i < ASKS; ++i)
+      if (tid + 256 * i < count) *reinterpret_cast<u32x4 *>(&lds_q[0][8 * (tid + 256 * i)]) = q[i];
+  };
+  if (n > 0) {
+    const int tk = tid / CHUNKS, tv = tid / 4;
+    const u32x4 k = *reinterpret_cast<const u32x4 *>(A.k + (begin + (int64_t)min(tk, n - 1)) * A.kv_stride_n + g * A.kv_stride_h + 8 * (tid % CHUNKS));
+    const u32x4 v = *reinterpret_cast<const u32x4 *>(A.v + (begin + (int64_t)min(tv, n - 1)) * A.kv_stride_n + g * A.kv_stride_h + 32 * slice + 8 * (tid % 4));
+    const float decay = A.decay[A.decay_rows ? (begin + (size_t)min(tid, n - 1)) * A.Hkv + g : g];
+    if (A.out) ask(0);
+    if (tk < n) *reinterpret_cast<u32x4 *>(&lds_k[tk][8 * (tid % CHUNKS)]) = k;
+    if (tv < n) *reinterpret_cast<u32x4 *>(&lds_v[tv][8 * (tid % 4)]) = v;
+    if (tid < n) lds_f[tid] = (float)exp2_64((double)decay * LOG2E_64);
+    if (A.out) put(0);
+  }
   __syncthreads();
 
   int parity = 0;
-  for (int t = 0; t < n; ++t) {
+  for (int t = 0, r0 = 0; t < n; ++t) {
     const float f = lds_f[t];
     float kk[RK];
 #pragma unroll
@@ -111,25 +136,43 @@ __global__ void __launch_bounds__(256) linear_step_kernel(const LinearArgs A) {
 #pragma unroll
     for (int r = 0; r < RK; ++r) S[r] = S[r] * f + v * kk[r];
     if (!A.out) continue;
+    if (t - r0 == rows) {
+      r0 = t;
+      ask(t);
+      __syncthreads();
+      put(t);
+      __syncthreads();
+    }
     for (int h0 = 0; h0 < A.G; h0 += HEADS) {
-      const uint16_t *q = A.q + (begin + (int64_t)t) * A.q_stride_n + row;
       Words<RK / 2> w[HEADS];
+      f32x4 o[HEADS];
 #pragma unroll
-      for (int h = 0; h < HEADS; ++h) w[h] = *reinterpret_cast<const Words<RK / 2> *>(q + (g * A.G + min(h0 + h, A.G - 1)) * A.q_stride_h);
+      for (int h = 0; h < HEADS; ++h) w[h] = *reinterpret_cast<const Words<RK / 2> *>(&lds_q[(t - r0) * A.G + min(h0 + h, A.G - 1)][row]);
 #pragma unroll
       for (int h = 0; h < HEADS; ++h) {
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        o[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < RK; ++r) o += S[r] * of_bf16(r % 2 ? w[h].w[r / 2] >> 16 : w[h].w[r / 2] & 0xffffu);
-        // the wave's eight groups of rows: lanes 8, 16 and 32 apart
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          o[e] += __shfl_xor(o[e], 8, 64);
-          o[e] += __shfl_xor(o[e], 16, 64);
-          o[e] += __shfl_xor(o[e], 32, 64);
-        }
-        if ((tid & 63) < 8) *reinterpret_cast<f32x4 *>(&lds_o[parity][h][wave][4 * (tid & 7)]) = o;
+        for (int r = 0; r < RK; ++r) o[h] += S[r] * of_bf16(r % 2 ? w[h].w[r / 2] >> 16 : w[h].w[r / 2] & 0xffffu);
       }
+      // The wave's eight groups of rows are added up: first the halves, of which each goes on with two of the heads, then the rows of 16 lanes, with
+      // one head each, then the lanes that are 8 apart.
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float y[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float lo = o[h][e], hi = o[h + 2][e];
+          const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi), false, false);
+          const uint32_t p0 = p[0], p1 = p[1];
+          y[h] = __builtin_bit_cast(float, p0) + __builtin_bit_cast(float, p1);
+        }
+        const auto p = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, y[0]), __builtin_bit_cast(uint32_t, y[1]), false, false);
+        const uint32_t p0 = p[0], p1 = p[1];
+        const float z = __builtin_bit_cast(float, p0) + __builtin_bit_cast(float, p1);
+        x[e] = z + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, z), 0x128, 0xf, 0xf, true));       // row_ror:8
+      }
+      if (!(tid & 8)) *reinterpret_cast<f32x4 *>(&lds_o[parity][(tid >> 5 & 1) * 2 + (tid >> 4 & 1)][wave][4 * (tid & 7)]) = x;
       __syncthreads();
       if (tid < 32 * HEADS && h0 + tid / 32 < A.G) {
         const int h = tid / 32, c = tid % 32;
