@@ -427,7 +427,7 @@ sts_status sts_window_attn(const sts_window_params *p, void *stream);
  * Rows of q, k and v have strides of their own (slices of one projection's output, for instance), unit stride on d.
  *
  * Supported: d in {64,128}; Hq % Hkv == 0; Hq/Hkv <= 16; Hq <= 256; T * Hq/Hkv < 2^31 - 65536; strides multiples of 8 elements, of rows
- * at least d and at most 2^25, of heads not negative; q, k, v and out 16-byte aligned; scale * log2(e) finite; fewer than 2^24 workgroups.
+ * at least d and at most 2^24, of heads not negative; q, k, v and out 16-byte aligned; scale * log2(e) finite; fewer than 2^24 workgroups.
  *
  * sts_prompt_attn -- causal attention over whole prompts: query row i of a sequence sees the keys 0 .. i of its sequence,
  *     s_j = scale * <Q[i,t,:], K[j,g,:]>,   out[i,t,:] = sum_j exp(s_j - lse) V[j,g,:],   lse[t,i] = ln sum_j exp(s_j)
@@ -464,7 +464,7 @@ typedef struct {
  * With max_len <= 16 the recurrence is worked out row by row in fp32. Else by chunks of rows: k^T v enters the state as in fp32, while
  * the weights of a chunk's rows and the state (as the operand of q^T S alone) are rounded to bf16.
  * Values of v that are infinite or NaN do not reach rows before their own; from there on results and state that depend on them are NaN or
- * infinite. The workspace's size depends on the integer fields and on whether starts is NULL.
+ * infinite. The workspace's size depends on the integer fields and on whether starts and out are NULL.
  */
 typedef struct {
   int32_t B, T, max_len, Hq, Hkv, d;

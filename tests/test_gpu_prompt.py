@@ -89,6 +89,55 @@ def test_values_that_are_no_numbers_reach_no_row_before_them(Hq, at, d):
             assert torch.isnan(out[20 + at:170]).all() and torch.isneginf(lse[:, 20 + at:170]).all()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_offsets_beyond_32_bits(d):
+    """Rows 2^24 elements apart (the most there may be), behind one another in 4 GB and more."""
+    lens = [100, 3, 70]
+    T, starts = sum(lens), starts_of(lens)
+    q, k, v = data(T, 2, 1, d, 13)
+    big = torch.empty(T * 2 ** 24, dtype=torch.bfloat16, device=DEV).view(T, 2 ** 24 // d, d)
+    dq, dk, dv = big[:, :2], big[:, 5:6], big[:, 9:10]
+    for to, x in ((dq, q), (dk, k), (dv, v)):
+        to.copy_(x)
+    check_prompts(sts.sts_prompt_attn(dq, dk, dv, starts.to(DEV), 0.1, out_dtype=torch.float32), prompts(q, k, v, starts, 0.1))
+
+
+@pytest.mark.parametrize("size", [1e-20, 1e36])
+def test_values_of_all_sizes(size):
+    starts = starts_of([90, 40])
+    q, k, v = data(130, 4, 2, 128, 14)
+    v = (v.float() * size).to(torch.bfloat16)
+    check_prompts(run(q, k, v, starts, 0.1, out_dtype=torch.float32), prompts(q, k, v, starts, 0.1))
+
+
+def test_scores_far_apart():
+    """Scores from -4000 to 4000, of which nearly all weights are 0, in an order that raises the maximum again and again."""
+    starts = starts_of([200])
+    q, k, v = data(200, 2, 1, 64, 15)
+    q[:] = 4.0
+    k = (torch.arange(200).float()[:, None, None] * 20 - 2000).expand(200, 1, 64) / 64
+    k = k.to(torch.bfloat16).contiguous()
+    k[::3] = -k[::3]
+    check_prompts(run(q, k, v, starts, 0.5, out_dtype=torch.float32), prompts(q, k, v, starts, 0.5))
+
+
+def test_two_streams_at_once():
+    inputs = [[t.to(DEV) for t in data(700, 8, 2, 128, 16 + i)] for i in range(2)]
+    starts = starts_of([300, 0, 400]).to(DEV)
+    want = [sts.sts_prompt_attn(*x, starts, 0.1) for x in inputs]
+    streams = [torch.cuda.Stream() for _ in inputs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for x, s, to in zip(inputs, streams, got):
+            with torch.cuda.stream(s):
+                to.append(sts.sts_prompt_attn(*x, starts, 0.1))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        for o, z in g:
+            assert torch.equal(o, w[0]) and torch.equal(z, w[1])
+
+
 def test_many_sequences():
     """More than are looked through at once: 200 and 5000 of them, many empty."""
     g = torch.Generator().manual_seed(3)

@@ -59,7 +59,7 @@ def test_ctypes_structs_match_the_header(tmp_path):
 BOTH = [(dict(B=-1), EINVAL), (dict(T=-1), EINVAL), (dict(Hq=30), EINVAL), (dict(Hq=0), EINVAL), (dict(Hkv=0), EINVAL), (dict(d=96), EUNSUPPORTED),
         (dict(Hq=512, Hkv=256), EUNSUPPORTED), (dict(Hq=32, Hkv=1), EUNSUPPORTED), (dict(out_dtype=2), EINVAL), (dict(scale=float("nan")), EINVAL),
         (dict(scale=-3e38), EINVAL), (dict(kv_stride_n=120), EUNSUPPORTED), (dict(kv_stride_n=1028), EUNSUPPORTED), (dict(kv_stride_n=-1024), EUNSUPPORTED),
-        (dict(kv_stride_h=4), EUNSUPPORTED), (dict(kv_stride_h=-128), EUNSUPPORTED), (dict(kv_stride_n=1 << 26), EUNSUPPORTED), (dict(q_stride_n=64), EUNSUPPORTED),
+        (dict(kv_stride_h=4), EUNSUPPORTED), (dict(kv_stride_h=-128), EUNSUPPORTED), (dict(kv_stride_n=1 << 26), EUNSUPPORTED), (dict(kv_stride_n=(1 << 24) + 8), EUNSUPPORTED), (dict(q_stride_n=1 << 25), EUNSUPPORTED), (dict(q_stride_n=64), EUNSUPPORTED),
         (dict(q_stride_n=4100), EUNSUPPORTED), (dict(q_stride_h=-8), EUNSUPPORTED), (dict(q=None), EINVAL), (dict(out=None), EINVAL), (dict(k=None), EINVAL),
         (dict(v=None), EINVAL), (dict(q=FAR + 8), EUNSUPPORTED), (dict(k=FAR + 2), EUNSUPPORTED), (dict(v=FAR + 8), EUNSUPPORTED), (dict(out=FAR + 4), EUNSUPPORTED),
         (dict(T=1 << 30), EUNSUPPORTED), (dict(B=0x7fffffff), EUNSUPPORTED), (dict(B=1 << 24, Hkv=32), EUNSUPPORTED)]
@@ -91,10 +91,30 @@ def test_workspaces_go_by_the_shape_alone(lib):
     size = lambda **kw: lib.sts_linear_attn_workspace_bytes(ctypes.byref(linear(**kw)))  # noqa: E731
     assert size() == size(q=None, out=None, k=None, state=None, scale=2.0) > 8 * 128 * 128 * 4
     assert size(max_len=16) == 256                     # row by row
-    assert size(max_len=100) == 256                    # no sequence is cut
-    assert size(starts=None, B=5000) == 256 and size(starts=None, B=5) > 256
+    assert size(max_len=100, Hkv=32) == 256            # no sequence is cut, no group shares a state
+    assert size(starts=None, B=5000) == 256 and size(starts=None, B=5) > 256 and size(starts=None, B=50, Hkv=32) == 256
     assert size(max_len=5000) == size(max_len=0) == size(max_len=9000)
     assert size(d=96) == 0
+
+
+@pytest.fixture(scope="module")
+def resources():
+    if not os.path.exists(build.RESOURCES) or build.needs_build():
+        build.build(force=True)
+    return build.kernel_resources()
+
+
+@pytest.mark.parametrize("name,forms", [("prompt_attn_kernel", 2), ("linear_step_kernel", 2), ("linear_chunk_kernel", 4), ("linear_carry_kernel", 2)])
+def test_kernels_fit_their_registers(resources, name, forms):
+    found = {k: v for k, v in resources.items() if f"{len(name)}{name}I" in k}
+    assert len(found) == forms
+    for k, v in found.items():
+        assert v["ScratchSize"] == 0 and v["AGPRs"] == 0, k
+        # two workgroups of four waves on a compute unit, three of the small prompts', four of two waves of the small chunks'; six of the steps' by their LDS
+        half = "ILi64E" in k
+        most = {"prompt_attn_kernel": 168 if half else 256, "linear_step_kernel": 102, "linear_chunk_kernel": 256, "linear_carry_kernel": 128}[name]
+        lds = {"prompt_attn_kernel": 160 // 3 if half else 80, "linear_step_kernel": 160 // 6, "linear_chunk_kernel": 40 if half else 80, "linear_carry_kernel": 0}[name]
+        assert v["VGPRs"] <= most and v["LDS Size"] <= lds * 1024, k
 
 
 def test_enums_and_kinds():
