@@ -235,8 +235,8 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   constexpr int KS = D / 16, MT = D / 32, CH = D / 8;
   constexpr int NL = C * CH / (64 * NW), RL = 64 / CH;      // loads of a wave for 32 rows, rows that each covers
   constexpr int BLOCK = D == 128 ? 15 : 9, MINE = (BLOCK + NW - 1) / NW;   // chunks whose decays are worked out at once, those of a wave
-  // Three chunks of K, V and Q, and a block's decays: for each row its sum c, its weight as a key, its factor as a query, and for each chunk four
-  // numbers. Arrays of their own, so that the compiler can tell the loads that fill one from the reads of another; it would have reads of an array
+  // Three chunks of K, V and Q, and a block's decays: for each row its sum c, its weight as a key, its factor as a query, and for each chunk what
+  // concerns all rows. Arrays of their own, so that the compiler can tell the loads that fill one from the reads of another; it would have reads of an array
   // that no load fills wait for all loads, so that one load of no bytes goes to the decays', too.
   constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, ALL = (OUT ? 3 : 2) * TILE;
   constexpr int LOADS = (OUT ? 3 : 2) * NL, STORES = OUT ? 2 : 0;      // of a wave and chunk
@@ -349,12 +349,12 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 
   // ---- Decays, in powers of two: c_i the sum over the chunk's rows up to i. With u_i = exp(c_i - c_32)
   //     out_i = scale u_i (q_i . (exp(c_32) S) + sum exp(c_32 - c_j) (q_i . k_j) v_j),
-  // so that each key has one weight, which the state takes too. Not where u would leave fp32's range, or a decay is no number: in such a chunk (`apart`)
-  // each pair's weight is worked out.
-  // The state is held as S / F with 2^-16 < F <= 1: F is the decays' product so far but for a power of 2^16, by which the state is multiplied
+  // so that each key has one weight, which the state takes too. Not where u could leave fp32's range (a chunk's decays make up 2^-60 or less, or a row's
+  // doubles the state) or a decay is no number: in such a chunk (`apart`) each pair's weight is worked out.
+  // The state is held as S / F with 1 <= F < 2^16: F is the decays' product so far but for a power of 2^16, by which the state is multiplied
   // where F would leave that range (exactly), and a key's weight is divided by F. F's logarithm `low` is a sum in 64 bits: no factor's rounding adds up
   // over a long sequence.
-  // A chunk's four numbers: the power of two; apart (1) or not (0); the logarithm of F before the chunk; nothing.
+  // A chunk has the power of two, apart (1) or not (0), the logarithm of F before it, and 1 where a row doubles the state.
   double all = 0.0, low = 0.0;
   const lds_ptr decays = (lds_ptr)lds_d;
   auto number_of = [&](int at) { return *(lds_f32)(decays + at); };
@@ -368,12 +368,13 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
       c[i] = sum_up_to(own);
       after[i] = sum_behind(own);
       *(lds_f32)(decays + chunk * C * 4 + 4 * col) = c[i];
+      *(lds_f32)(decays + AT_CHUNK + 16 * chunk + 12) = __builtin_amdgcn_ballot_w64(own > 1.f) ? 1.f : 0.f;
     }
     load_gates(base + BLOCK);
     all_waves();
     // (no branches but those that all lanes take alike: the loop around would get ways through it that there are not, and the compiler's waits with them)
     const int mine = lane & 15;            // the lane's chunk
-    const float end = number_of((min(mine, BLOCK - 1) * C + 31) * 4);
+    const float end = number_of((min(mine, BLOCK - 1) * C + 31) * 4), grows = number_of(AT_CHUNK + 16 * mine + 12);
     double before = 0.0, behind = 0.0;
     const double first = low;
 #pragma unroll
@@ -383,18 +384,18 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
       behind = mine == i ? low : behind;
     }
     all += low - first;
-    auto whole = [](double x) { return __builtin_ceil(x * 0.0625) * 16.0; };
+    auto whole = [](double x) { return __builtin_floor(x * 0.0625) * 16.0; };
     const double low_before = before - whole(before), low_behind = behind - whole(behind);
     const float F = exp2_32(low_behind), F_inv = exp2_32(-low_behind), step = __builtin_amdgcn_exp2f((float)(whole(behind) - whole(before)));
     low -= whole(low);
-    *(__attribute__((address_space(3))) f32x4 *)(decays + AT_CHUNK + 16 * mine) = f32x4{step, end >= -60.f ? 0.f : 1.f, (float)low_before, 0.f};
+    *(__attribute__((address_space(3))) f32x4 *)(decays + AT_CHUNK + 16 * mine) = f32x4{step, end >= -60.f && grows == 0.f ? 0.f : 1.f, (float)low_before, grows};
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
       const int chunk = wave + i * NW, row = (base + chunk) * C, at = chunk * C * 4;
       auto of_chunk = [&](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), min(chunk, BLOCK - 1))); };
       const float factor = of_chunk(F), inverse = of_chunk(F_inv), c_end = of_chunk(end);
       *(lds_f32)(decays + AT_KEY + at + 4 * col) = row + col < rows ? __builtin_amdgcn_exp2f(after[i]) * inverse : 0.f;
-      *(lds_f32)(decays + AT_QUERY + at + 4 * col) = A.scale * (c_end >= -60.f ? factor * __builtin_amdgcn_exp2f(c[i] - c_end) : 1.f);
+      *(lds_f32)(decays + AT_QUERY + at + 4 * col) = A.scale * (c_end >= -60.f && of_chunk(grows) == 0.f ? factor * __builtin_amdgcn_exp2f(c[i] - c_end) : 1.f);
     }
     all_waves();
   };
@@ -549,8 +550,9 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
         bf16x8 P[2];
         weights(X, P);
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-          for (int key = 0; key < 16; ++key) {      // key by key, and a row is taken in only where it is seen
+        for (int s = 0; s < 2; ++s) {
+          if (!odd) R = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], R, 0, 0, 0);
+          for (int key = 0; key < (odd ? 16 : 0); ++key) {      // key by key, and a row is taken in only where it is seen
             u32x4 own_key;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -563,6 +565,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 #pragma unroll
             for (int e = 0; e < 16; ++e) R[e] += 16 * s + key <= col ? x[e] : 0.f;
           }
+        }
       }
     }
     if constexpr (OUT) {

@@ -233,6 +233,135 @@ def test_values_that_are_no_numbers_reach_no_row_before_them(at, d):
             assert torch.isfinite(rest[:, :2, others]).all() and torch.isfinite(S[1, 0][:, others]).all() and not torch.isfinite(S[1, 0][:, 3]).any()
 
 
+@pytest.mark.parametrize("d,past", [(64, 9), (128, 15)])
+def test_segments_of_many_chunks(d, past):
+    """Sixteen heads of a group, 256 in all: few segments, so that each has more chunks than a workgroup works out the decays of at once (nine
+    or fifteen). Chunks on both sides of that border forget nearly all (2^-200), or grow, or all but stay as they are."""
+    n = 1400
+    q, k, v, decay = data(n, 256, 16, d, 37, True, 0.1)
+    for chunk, value in ((past - 1, -4.0), (past, -6.0), (past + 1, 0.0), (past + 3, 0.02), (0, -5.0)):
+        for segment in range(0, n, 352 if d == 64 else 704):
+            decay[segment + 32 * chunk:segment + 32 * chunk + 32, 0] = value
+    first = states(1, 16, d, 10)
+    for out in (True, False):
+        o, S = run(q if out else None, k, v, decay, 0.1, starts=starts_of([n]), state=first, state_out=torch.empty(1, 16, d, d), out_dtype=torch.float32)
+        for g in (0, 13):
+            h, kv = slice(16 * g, 16 * g + 16), slice(g, g + 1)
+            check((o[:, h] if out else None, S[:, kv]), q[:, h], k[:, kv], v[:, kv], decay[:, kv], 0.1, starts_of([n]), first[:, kv], True, out=out, what=f"head {g}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("up", [0.02, 0.6, 3.0])
+def test_states_that_grow(up, d):
+    """Decays above 0: some rows by little, or by more than is taken back."""
+    n = 150
+    q, k, v, _ = data(n, 4, 2, d, 38)
+    g = torch.Generator().manual_seed(39)
+    decay = up * (torch.rand(n, 2, generator=g) * 2 - 1)
+    first = states(1, 2, d, 11)
+    got = run(q, k, v, decay, 0.1, starts=starts_of([n]), state=first, state_out=torch.empty(1, 2, d, d), out_dtype=torch.float32)
+    check(got, q, k, v, decay, 0.1, starts_of([n]), first, True)
+    blocks = [t[:16].view(1, 16, *t.shape[1:]) for t in (q, k, v, decay)]
+    out, S = run(*blocks, 0.1, state=first, state_out=torch.empty(1, 2, d, d), out_dtype=torch.float32)
+    check((out[0], S), q, k, v, decay, 0.1, starts_of([16]), first, False)
+
+
+@pytest.mark.parametrize("size", [1e35, 1e-20])
+@pytest.mark.parametrize("n", [10, 300])
+def test_values_of_all_sizes(n, size):
+    """Values whose sums are near the ends of fp32, with decays that take the state through many powers of two."""
+    d = 64
+    q, k, v, decay = data(n, 2, 2, d, 40, True, 0.4)
+    v = (v.float() * size).to(torch.bfloat16)
+    first = states(1, 2, d, 12) * size
+    got = run(q, k, v, decay, 0.1, starts=starts_of([n]), max_len=n, state=first, state_out=torch.empty(1, 2, d, d), out_dtype=torch.float32)
+    check(got, q, k, v, decay, 0.1, starts_of([n]), first, n > 16)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at", [0, 31, 32, 77, 149])
+def test_a_decay_that_is_no_number(at, d):
+    """Rows before it and the other head do not see it; from there on the head's results and its state are no numbers."""
+    n = 150
+    q, k, v, decay = data(n, 4, 2, d, 41)
+    decay[at, 0] = float("nan")
+    zero = torch.zeros(2, d, d)
+    for rows_, chunked in ((n, True), (min(at + 1, 16), False)):
+        if not chunked and at >= 16:
+            continue
+        out, S = run(q[:rows_], k[:rows_], v[:rows_], decay[:rows_], 0.1, starts=starts_of([rows_]), max_len=rows_, state_out=torch.empty(1, 2, d, d), out_dtype=torch.float32)
+        if at:
+            ref, _, e_ref, _ = linear(q[:at], k[:at], v[:at], decay[:at], 0.1, zero, chunked)
+            check_linear(out[:at], ref, e_ref, "before")
+        ref, all_s, e_ref, e_s = linear(q[:rows_, 2:], k[:rows_, 1:], v[:rows_, 1:], decay[:rows_, 1:], 0.1, zero[1:], chunked)
+        check_linear(out[:, 2:], ref, e_ref, "the other head")
+        check_linear(S[0, 1:], all_s[-1], e_s[-1], "the other head's state")
+        assert torch.isnan(out[at:, :2]).all() and torch.isnan(S[0, 0]).all()
+
+
+@pytest.mark.parametrize("max_len,lens", [(7, [20, 3, 9]), (40, [100, 30, 41])])
+def test_rows_behind_the_longest_are_left_out(max_len, lens):
+    d = 64
+    starts = starts_of(lens)
+    q, k, v, decay = data(sum(lens), 4, 2, d, 42)
+    first = states(3, 2, d, 13)
+    out = torch.full((sum(lens), 4, d), 5.0, device=DEV)
+    got = run(q, k, v, decay, 0.1, starts=starts, max_len=max_len, state=first, state_out=torch.empty(3, 2, d, d), out=out)
+    check(got, q, k, v, decay, 0.1, starts, first, max_len > 16, lens=torch.full((3,), max_len))
+    for b, n in enumerate(lens):
+        assert (out[int(starts[b]) + min(n, max_len):int(starts[b]) + n] == 5).all()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_nothing_behind_a_sequence_is_written(dt, d):
+    """The last chunk of a segment and of a sequence is not whole: the rows behind belong to the next sequence, or to nobody."""
+    lens = [131, 1, 45]
+    starts = starts_of(lens)
+    q, k, v, decay = data(200, 4, 1, d, 43)
+    out = torch.full((200, 4, d), 5.0, device=DEV, dtype=dt)
+    for b in range(3):                                # one at a time, each between rows that are not its own
+        only = torch.tensor([int(starts[b]), int(starts[b + 1])], dtype=torch.int32)
+        before = out.clone()
+        got = run(q, k, v, decay, 0.1, starts=only, out=out)
+        a, e = only.tolist()
+        assert torch.equal(out[:a], before[:a]) and torch.equal(out[e:], before[e:])
+        check((got[0][a:e], None), q[a:e], k[a:e], v[a:e], decay[a:e], 0.1, starts_of([e - a]), torch.zeros(1, 1, d, d), True)
+
+
+@pytest.mark.parametrize("lens", [[9, 8], [100, 40]])
+def test_offsets_beyond_32_bits(lens):
+    """Rows 2^24 elements apart (the most there may be), behind one another in 4 GB and more."""
+    d, T = 64, sum(lens)
+    q, k, v, decay = data(T, 2, 1, d, 44)
+    big = torch.empty(T * 2 ** 24, dtype=torch.bfloat16, device=DEV).view(T, 2 ** 18, d)
+    dq, dk, dv = big[:, :2], big[:, 5:6], big[:, 9:10]
+    for to, x in ((dq, q), (dk, k), (dv, v)):
+        to.copy_(x)
+    starts = starts_of(lens)
+    got = sts.sts_linear_attn(dq, dk, dv, on(decay), 0.1, starts=on(starts), max_len=max(lens), state_out=torch.empty(2, 1, d, d, device=DEV), out_dtype=torch.float32)
+    check(got, q, k, v, decay, 0.1, starts, torch.zeros(2, 1, d, d), max(lens) > 16)
+
+
+@pytest.mark.parametrize("n", [8, 500])
+def test_two_streams_at_once(n):
+    """Calls on two streams, which overlap as they like, with workspaces of their own give what they give one after the other."""
+    inputs = [[on(t) for t in data(2 * n, 8, 2, 128, 45 + i)] for i in range(2)]
+    starts = starts_of([n, n]).to(DEV)
+    want = [sts.sts_linear_attn(*x, 0.1, starts=starts, max_len=n, state_out=torch.empty(2, 2, 128, 128, device=DEV)) for x in inputs]
+    streams = [torch.cuda.Stream() for _ in inputs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for x, s, to in zip(inputs, streams, got):
+            with torch.cuda.stream(s):
+                to.append(sts.sts_linear_attn(*x, 0.1, starts=starts, max_len=n, state_out=torch.empty(2, 2, 128, 128, device=DEV)))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        for o, S in g:
+            assert torch.equal(o, w[0]) and torch.equal(S, w[1])
+
+
 def test_a_long_sequence_of_one_decay():
     """4096 rows with a decay close to 1: its factor's rounding is the same in every chunk and must not add up. On the GPU in 64 bits."""
     n, d = 4096, 64
