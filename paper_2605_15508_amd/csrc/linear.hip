@@ -70,15 +70,21 @@ __device__ __forceinline__ float of_bf16(uint32_t bits) { return __builtin_bit_c
 // ---------------------------------------------------------------------------------------------- recurrent form
 template <int N> struct Words { uint32_t w[N]; };
 
-template <int D>
+// A workgroup has 32 columns of a state, a thread four of them in D / 32 rows. All that it reads is asked for at once; the state stays in registers
+// and is written once. AT_ONCE rows of 4 / AT_ONCE heads each are a step: four results, whose sums over the state's rows are made together.
+//
+// With one row memory bounds it: 64 sequences with 32 heads of 128 take 53 us for the 268 MB of their states, 5.1 TB/s. More rows add vector instructions, 140
+// for a step of the wave: without other waves on its SIMD 0.5 us (0.2 us for each of four rows at once, 0.5 for one after the other).
+// The matrix instruction for fp32 (4x4x1, k v^T and q^T S both) was as slow: 13.1 us for 16 rows of a sequence with groups of four heads, 11.7 here.
+template <int D, int AT_ONCE>
 __global__ void __launch_bounds__(256) linear_step_kernel(const LinearArgs A) {
   constexpr int RK = D / 32;              // rows of the state per thread
-  constexpr int SLICES = D / 32, MAX = STS_LINEAR_STEP, HEADS = 4;      // heads that are worked on at once
+  constexpr int SLICES = D / 32, MAX = STS_LINEAR_STEP, HEADS = 4 / AT_ONCE;
   constexpr int QUERIES = 64, CHUNKS = D / 8, ASKS = QUERIES * CHUNKS / 256;
   static_assert(QUERIES >= STS_MAX_GROUP && MAX * CHUNKS <= 256, "");
-  __shared__ __attribute__((aligned(16))) uint16_t lds_k[MAX][D], lds_v[MAX][32], lds_q[QUERIES][D];
-  __shared__ float lds_f[MAX];
-  __shared__ __attribute__((aligned(16))) float lds_o[2][HEADS][4][32];
+  __shared__ __attribute__((aligned(16))) uint16_t lds_k[MAX + 3][D], lds_v[MAX + 3][32], lds_q[QUERIES + 3][D];      // (a step may look at what no row has)
+  __shared__ float lds_f[MAX + 3];
+  __shared__ __attribute__((aligned(16))) float lds_o[2][4][4][32];
 
   const int tid = threadIdx.x, wave = tid >> 6;
   const int unit = blockIdx.x / SLICES, slice = blockIdx.x % SLICES;
@@ -97,7 +103,7 @@ __global__ void __launch_bounds__(256) linear_step_kernel(const LinearArgs A) {
     for (int r = 0; r < RK; ++r) S[r] = *reinterpret_cast<const f32x4 *>(from + head_at + (row + r) * D + col);
   }
   // Queries of as many rows as there is room for. They, the rows of K and V and the decays are all asked for before any is waited for.
-  const int rows = QUERIES / A.G;
+  const int rows = QUERIES / A.G;        // (a multiple of AT_ONCE where that is not 1)
   u32x4 q[ASKS];
   auto ask = [&](int t0) {
     const int count = min(rows, n - t0) * A.G * CHUNKS;
@@ -112,6 +118,7 @@ __global__ void __launch_bounds__(256) linear_step_kernel(const LinearArgs A) {
 #pragma unroll
     for (int i = 0; i < ASKS; ++i)
       if (tid + 256 * i < count) *reinterpret_cast<u32x4 *>(&lds_q[0][8 * (tid + 256 * i)]) = q[i];
+    __syncthreads();
   };
   if (n > 0) {
     const int tk = tid / CHUNKS, tv = tid / 4;
@@ -123,49 +130,57 @@ __global__ void __launch_bounds__(256) linear_step_kernel(const LinearArgs A) {
     if (tv < n) *reinterpret_cast<u32x4 *>(&lds_v[tv][8 * (tid % 4)]) = v;
     if (tid < n) lds_f[tid] = (float)exp2_64((double)decay * LOG2E_64);
     if (A.out) put(0);
+    else __syncthreads();
   }
-  __syncthreads();
 
-  int parity = 0;
-  for (int t = 0, r0 = 0; t < n; ++t) {
-    const float f = lds_f[t];
-    float kk[RK];
+  struct Row { Words<RK / 2> k; u32x2 v; float f; };
+  auto row_of = [&](int t) { return Row{*reinterpret_cast<const Words<RK / 2> *>(&lds_k[t][row]), *reinterpret_cast<const u32x2 *>(&lds_v[t][4 * (tid & 7)]), lds_f[t]}; };
+  auto half = [](const auto &w, int i) { return of_bf16(i % 2 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu); };
+  auto take_in = [&](const Row &x) {
+    const uint32_t v0 = x.v[0], v1 = x.v[1];
+    const f32x4 v = {of_bf16(v0 & 0xffffu), of_bf16(v0 >> 16), of_bf16(v1 & 0xffffu), of_bf16(v1 >> 16)};
 #pragma unroll
-    for (int r = 0; r < RK; ++r) kk[r] = of_bf16(lds_k[t][row + r]);
-    const f32x4 v = {of_bf16(lds_v[t][4 * (tid & 7)]), of_bf16(lds_v[t][4 * (tid & 7) + 1]), of_bf16(lds_v[t][4 * (tid & 7) + 2]), of_bf16(lds_v[t][4 * (tid & 7) + 3])};
-#pragma unroll
-    for (int r = 0; r < RK; ++r) S[r] = S[r] * f + v * kk[r];
-    if (!A.out) continue;
-    if (t - r0 == rows) {
-      r0 = t;
+    for (int r = 0; r < RK; ++r) S[r] = S[r] * x.f + v * half(x.k.w, r);
+  };
+  if (!A.out) {
+#pragma unroll 4
+    for (int t = 0; t < n; ++t) take_in(row_of(t));
+  }
+  const int u = tid >> 5, c = tid & 31;             // the result of a step that the thread brings
+  const size_t own_out = ((size_t)(begin + u / HEADS) * A.Hq + g * A.G + u % HEADS) * D + 32 * slice + c;
+  for (int t = 0, r0 = 0, parity = 0; A.out && t < n; t += AT_ONCE) {
+    if (t - r0 >= rows) {
+      r0 = t;            // (all that is in LDS was read before the last barrier)
       ask(t);
-      __syncthreads();
       put(t);
-      __syncthreads();
     }
+    Row own[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) own[i] = row_of(t + i);
     for (int h0 = 0; h0 < A.G; h0 += HEADS) {
-      Words<RK / 2> w[HEADS];
-      f32x4 o[HEADS];
+      Words<RK / 2> w[4];
 #pragma unroll
-      for (int h = 0; h < HEADS; ++h) w[h] = *reinterpret_cast<const Words<RK / 2> *>(&lds_q[(t - r0) * A.G + min(h0 + h, A.G - 1)][row]);
+      for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const Words<RK / 2> *>(&lds_q[(t - r0) * A.G + h0 + i][row]);
+      f32x4 o[4];
 #pragma unroll
-      for (int h = 0; h < HEADS; ++h) {
-        o[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 4; ++i) {
+        if (i % HEADS == 0 && h0 == 0 && t + i / HEADS < n) take_in(own[i / HEADS]);
+        o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < RK; ++r) o[h] += S[r] * of_bf16(r % 2 ? w[h].w[r / 2] >> 16 : w[h].w[r / 2] & 0xffffu);
+        for (int r = 0; r < RK; ++r) o[i] += S[r] * half(w[i].w, r);
       }
-      // The wave's eight groups of rows are added up: first the halves, of which each goes on with two of the heads, then the rows of 16 lanes, with
-      // one head each, then the lanes that are 8 apart.
+      // The wave's eight groups of rows are added up: first the halves, of which each goes on with two of the four, then the rows of 16 lanes, with one
+      // each, then the lanes that are 8 apart.
       f32x4 x;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float y[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float lo = o[h][e], hi = o[h + 2][e];
+        for (int i = 0; i < 2; ++i) {
+          const float lo = o[i][e], hi = o[i + 2][e];
           const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi), false, false);
           const uint32_t p0 = p[0], p1 = p[1];
-          y[h] = __builtin_bit_cast(float, p0) + __builtin_bit_cast(float, p1);
+          y[i] = __builtin_bit_cast(float, p0) + __builtin_bit_cast(float, p1);
         }
         const auto p = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, y[0]), __builtin_bit_cast(uint32_t, y[1]), false, false);
         const uint32_t p0 = p[0], p1 = p[1];
@@ -174,14 +189,13 @@ __global__ void __launch_bounds__(256) linear_step_kernel(const LinearArgs A) {
       }
       if (!(tid & 8)) *reinterpret_cast<f32x4 *>(&lds_o[parity][(tid >> 5 & 1) * 2 + (tid >> 4 & 1)][wave][4 * (tid & 7)]) = x;
       __syncthreads();
-      if (tid < 32 * HEADS && h0 + tid / 32 < A.G) {
-        const int h = tid / 32, c = tid % 32;
-        const float o = A.scale * ((lds_o[parity][h][0][c] + lds_o[parity][h][1][c]) + (lds_o[parity][h][2][c] + lds_o[parity][h][3][c]));
-        const size_t at = ((begin + (size_t)t) * A.Hq + g * A.G + h0 + h) * D + 32 * slice + c;
-        if (A.out_dtype == STS_F32) static_cast<float *>(A.out)[at] = o;
-        else static_cast<__bf16 *>(A.out)[at] = (__bf16)o;
+      if (u < 4 && t + u / HEADS < n && h0 + u % HEADS < A.G) {
+        const float o = A.scale * ((lds_o[parity][u][0][c] + lds_o[parity][u][1][c]) + (lds_o[parity][u][2][c] + lds_o[parity][u][3][c]));
+        const size_t to = own_out + ((size_t)t * A.Hq + h0) * D;
+        if (A.out_dtype == STS_F32) static_cast<float *>(A.out)[to] = o;
+        else static_cast<__bf16 *>(A.out)[to] = (__bf16)o;
       }
-      parity ^= 1;       // (the next results go elsewhere; those after them come behind the next barrier)
+      parity ^= 1;         // (the next results go elsewhere; those after them come behind the next barrier)
     }
   }
   float *to = state_out(A, b);
@@ -690,8 +704,17 @@ __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
 
 hipError_t launch_linear_step(const LinearArgs &a, int d, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.seqs.B * a.Hkv * (d / 32))), block(256);
-  if (d == 128) STS_LAUNCH(linear_step_kernel<128>, grid, block, 0, s, a);
-  else STS_LAUNCH(linear_step_kernel<64>, grid, block, 0, s, a);
+  // Several rows at once where a group has fewer than four heads: 16 rows of 64 sequences without groups take 89 us, row by row 137. One row takes more
+  // registers then for nothing (54.5 us for those 53).
+  const int at_once = a.max_len == 1 || a.G > 2 ? 1 : a.G == 2 ? 2 : 4;
+  auto launch = [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    if (at_once == 4) STS_LAUNCH((linear_step_kernel<D, 4>), grid, block, 0, s, a);
+    else if (at_once == 2) STS_LAUNCH((linear_step_kernel<D, 2>), grid, block, 0, s, a);
+    else STS_LAUNCH((linear_step_kernel<D, 1>), grid, block, 0, s, a);
+  };
+  if (d == 128) launch(std::integral_constant<int, 128>());
+  else launch(std::integral_constant<int, 64>());
   return sts_take_launch_status();
 }
 

@@ -49,7 +49,7 @@ def check(got, q, k, v, decay, scale, starts, first, chunked, lens=None, out=Tru
             check_linear(S[b], all_s[-1], e_s[-1], f"{what} state {b}")
 
 
-BLOCKS = [(1, 1, 1, 1), (3, 1, 4, 1), (2, 5, 8, 2), (1, 16, 16, 1), (2, 7, 6, 2), (40, 1, 4, 4), (2, 16, 10, 2)]
+BLOCKS = [(1, 1, 1, 1), (3, 1, 4, 1), (2, 5, 8, 2), (1, 16, 16, 1), (2, 7, 6, 2), (40, 1, 4, 4), (2, 16, 10, 2), (2, 7, 3, 3), (1, 16, 2, 2), (3, 5, 4, 2), (1, 2, 2, 1)]
 
 
 @pytest.mark.parametrize("d", [64, 128])

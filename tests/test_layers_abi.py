@@ -104,16 +104,16 @@ def resources():
     return build.kernel_resources()
 
 
-@pytest.mark.parametrize("name,forms", [("prompt_attn_kernel", 2), ("linear_step_kernel", 2), ("linear_chunk_kernel", 4), ("linear_carry_kernel", 2)])
+@pytest.mark.parametrize("name,forms", [("prompt_attn_kernel", 2), ("linear_step_kernel", 6), ("linear_chunk_kernel", 4), ("linear_carry_kernel", 2)])
 def test_kernels_fit_their_registers(resources, name, forms):
     found = {k: v for k, v in resources.items() if f"{len(name)}{name}I" in k}
     assert len(found) == forms
     for k, v in found.items():
         assert v["ScratchSize"] == 0 and v["AGPRs"] == 0, k
-        # two workgroups of four waves on a compute unit, three of the small prompts', four of two waves of the small chunks'; six of the steps' by their LDS
+        # two workgroups of four waves on a compute unit, three of the small prompts', four of two waves of the small chunks'; three or more of the steps'
         half = "ILi64E" in k
-        most = {"prompt_attn_kernel": 168 if half else 256, "linear_step_kernel": 102, "linear_chunk_kernel": 256, "linear_carry_kernel": 128}[name]
-        lds = {"prompt_attn_kernel": 160 // 3 if half else 80, "linear_step_kernel": 160 // 6, "linear_chunk_kernel": 40 if half else 80, "linear_carry_kernel": 0}[name]
+        most = {"prompt_attn_kernel": 168 if half else 256, "linear_step_kernel": 168, "linear_chunk_kernel": 256, "linear_carry_kernel": 128}[name]
+        lds = {"prompt_attn_kernel": 160 // 3 if half else 80, "linear_step_kernel": 160 // 5, "linear_chunk_kernel": 40 if half else 80, "linear_carry_kernel": 0}[name]
         assert v["VGPRs"] <= most and v["LDS Size"] <= lds * 1024, k
 
 
