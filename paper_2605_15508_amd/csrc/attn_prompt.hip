@@ -122,13 +122,15 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
     k_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * k_chunk<D>(row, slot0);
     v_off[m] = (uint32_t)row * (uint32_t)row_bytes + 16 * v_chunk<D>(row, slot0);
   }
-  // K's or V's tile t (past the last: nothing but zeros)
-  auto load = [&](int t, const unsigned char *base, u32x4 *to, bool is_v) {
+  // the wave's load m of K's or V's tile t (past the last: nothing but zeros)
+  auto load_part = [&](int t, const unsigned char *base, u32x4 *to, bool is_v, int m) {
     const int n = __builtin_amdgcn_readfirstlane(min(places - t * TK, TK)), end = n > 0 ? (n - 1) * (int)row_bytes + 2 * D : 0;
-    u32x4 *const mine = to + wave * NL * 64;
     const __amdgpu_buffer_rsrc_t at = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(base + (int64_t)t * TK * row_bytes), 0, end, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(to + (wave * NL + m) * 64), 16, (int)(is_v ? v_off[m] : k_off[m]), 0, 0, 0);
+  };
+  auto load = [&](int t, const unsigned char *base, u32x4 *to, bool is_v) {
 #pragma unroll
-    for (int m = 0; m < NL; ++m) __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (lds_ptr)(mine + 64 * m), 16, (int)(is_v ? v_off[m] : k_off[m]), 0, 0, 0);
+    for (int m = 0; m < NL; ++m) load_part(t, base, to, is_v, m);
   };
 
   float m_run = -INFINITY, l_run = 0.f;
@@ -269,8 +271,6 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
     auto step = [&](auto edge, int t, const u32x4 *k_next, u32x4 *k_free, const u32x4 *v, u32x4 *v_free) {
       constexpr bool EDGE = decltype(edge)::value;
       arrived();
-      load(t + 2, kbase, k_free, false);
-      load(t + 1, vbase, v_free, true);
       int k_at = k_lane, v_at = v_lane;
       asm("" : "+v"(k_at), "+v"(v_at));
       constexpr int PART = 16 / KS;          // pairs of weights beside the two matrix instructions of a step
@@ -298,6 +298,10 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
+        if (s < NL) {                        // (all at once they would hold up the wave: 8192 rows 527 us, 516 so)
+          load_part(t + 2, kbase, k_free, false, s);
+          load_part(t + 1, vbase, v_free, true, s);
+        }
         if (s + 2 < KS) read_k(s + 2);
         else if (s + 2 == KS) read_v(0);
         else read_v(1);
