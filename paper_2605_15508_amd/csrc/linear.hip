@@ -233,6 +233,27 @@ __device__ __forceinline__ float sum_behind(float x) {
   return threadIdx.x & 16 ? y : y + lane_of(y, 16);
 }
 
+// the same in 64 bits over `places` lanes, up to the one before
+__device__ __forceinline__ double lane_of(double x, int lane) {
+  const u32x2 w = __builtin_bit_cast(u32x2, x);
+  const uint32_t w0 = w[0], w1 = w[1];
+  return __builtin_bit_cast(double, u32x2{(uint32_t)__builtin_amdgcn_readlane((int)w0, lane), (uint32_t)__builtin_amdgcn_readlane((int)w1, lane)});
+}
+template <int PLACES>
+__device__ __forceinline__ double sums_before(double x) {
+  auto lower = [&](auto ctrl) {
+    const u32x2 w = __builtin_bit_cast(u32x2, x);
+    const uint32_t w0 = w[0], w1 = w[1];
+    return __builtin_bit_cast(double, u32x2{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w0, decltype(ctrl)::value, 0xf, 0xf, true), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w1, decltype(ctrl)::value, 0xf, 0xf, true)});
+  };
+  x += lower(std::integral_constant<int, 0x111>());        // row_shr
+  x += lower(std::integral_constant<int, 0x112>());
+  x += lower(std::integral_constant<int, 0x114>());
+  x += lower(std::integral_constant<int, 0x118>());
+  const double y = lower(std::integral_constant<int, 0x111>());
+  return PLACES == 32 && threadIdx.x & 16 ? y + lane_of(x, 15) : y;
+}
+
 // A part's numbers lie as the waves hold them: element 4 e .. of tile m, four side by side, lane by lane, wave by wave. Place 4 q .. is this number of
 // the state and the three below it:
 template <int D> __device__ __forceinline__ int state_place(int q) {
@@ -248,14 +269,16 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   constexpr int NW = D / 32;             // waves, each with 32 columns of the state
   constexpr int KS = D / 16, MT = D / 32, CH = D / 8;
   constexpr int NL = C * CH / (64 * NW), RL = 64 / CH;      // loads of a wave for 32 rows, rows that each covers
-  constexpr int BLOCK = D == 128 ? 15 : 9, MINE = (BLOCK + NW - 1) / NW;   // chunks whose decays are worked out at once, those of a wave
+  // (What LDS has left at two and four workgroups. Each time takes 2 us: 8192 rows, 17 chunks a segment, 123 us with 15 at once, 119 with 18.)
+  constexpr int BLOCK = D == 128 ? 18 : 9, MINE = (BLOCK + NW - 1) / NW;   // chunks whose decays are worked out at once, those of a wave
+  constexpr int PLACES = BLOCK > 16 ? 32 : 16;              // lanes that have one of them, or none
   // Three chunks of K, V and Q, and a block's decays: for each row its sum c, its weight as a key, its factor as a query, and for each chunk what
   // concerns all rows. Arrays of their own, so that the compiler can tell the loads that fill one from the reads of another; it would have reads of an array
   // that no load fills wait for all loads, so that one load of no bytes goes to the decays', too.
   constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, ALL = (OUT ? 3 : 2) * TILE;
   constexpr int LOADS = (OUT ? 3 : 2) * NL, STORES = OUT ? 2 : 0;      // of a wave and chunk
   constexpr int AT_KEY = MINE * NW * C * 4, AT_QUERY = 2 * AT_KEY, AT_CHUNK = 3 * AT_KEY;
-  __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_2[ALL], lds_d[AT_CHUNK / 16 + 16];
+  __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_2[ALL], lds_d[AT_CHUNK / 16 + PLACES];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
@@ -387,17 +410,12 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     load_gates(base + BLOCK);
     all_waves();
     // (no branches but those that all lanes take alike: the loop around would get ways through it that there are not, and the compiler's waits with them)
-    const int mine = lane & 15;            // the lane's chunk
+    const int mine = lane & (PLACES - 1);  // the lane's chunk
     const float end = number_of((min(mine, BLOCK - 1) * C + 31) * 4), grows = number_of(AT_CHUNK + 16 * mine + 12);
-    double before = 0.0, behind = 0.0;
-    const double first = low;
-#pragma unroll
-    for (int i = 0; i < BLOCK; ++i) {      // (0 behind the last chunk)
-      before = mine == i ? low : before;
-      low += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, end), i));
-      behind = mine == i ? low : behind;
-    }
-    all += low - first;
+    const double sum = sums_before<PLACES>(mine < BLOCK ? end : 0.0), before = low + sum, behind = before + end;      // (0 behind the last chunk)
+    const double total = lane_of(sum, BLOCK - 1) + lane_of(end, BLOCK - 1);
+    low += total;
+    all += total;
     auto whole = [](double x) { return __builtin_floor(x * 0.0625) * 16.0; };
     const double low_before = before - whole(before), low_behind = behind - whole(behind);
     const float F = exp2_32(low_behind), F_inv = exp2_32(-low_behind), step = __builtin_amdgcn_exp2f((float)(whole(behind) - whole(before)));
