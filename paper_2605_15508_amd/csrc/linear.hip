@@ -10,6 +10,9 @@
 // products q . k by itself, so that these pass from accumulator to operand in their lane, as the state does: nothing goes through LDS but
 // rows of Q, K and V. Long sequences are cut into segments: one kernel sums up what each segment adds to the state, one
 // adds these up along the sequence, and a third starts every segment from the state before it.
+// What bounds it without groups: memory. 8192 rows with 32 heads of 128 take 119 us: sums 36 (170 MB, 4.6 TB/s), adding up 14 (64 MB), results 58
+// (300 MB, 5.1 TB/s), and what lies between three launches. With groups of heads (each with a state of its own in the results' kernel) matrix and vector instructions, which
+// take 44% and 48% of its cycles and hardly overlap: six prompts of 77 to 6001 rows, 32 heads in groups of four, 103 us, of which the results 75.
 #include "attn_util.h"
 #include "layers.h"
 
@@ -262,6 +265,9 @@ template <int D> __device__ __forceinline__ int state_place(int q) {
   return (32 * m + 16 * (e >> 1) + 8 * (lane >> 5) + 4 * (e & 1)) * D + 32 * wave + (lane & 31);
 }
 
+// Two workgroups of four waves on a compute unit (head size 64: four of two waves), three chunks in LDS for each: one that is worked on, one that has come, one under
+// way. A chunk of 32 rows takes 42 matrix instructions of a wave at head size 128 (24 of them for the state, whose terms are split in three) and 320 vector instructions.
+//
 // OUT: results, from the state before the segment; else what the segment adds to the state (or, of a sequence with one segment, its
 // state)
 template <int D, bool OUT>
@@ -672,7 +678,8 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     for (int e = 0; e < 16; ++e) to[s_at + (32 * m + 16 * (e >> 3) + (e & 7)) * D] = S[m][e];
 }
 
-// Along each sequence of several segments: the state before every segment takes the place of what the segment adds. A thread has four numbers.
+// Along each sequence of several segments: the state before every segment takes the place of what the segment adds. A thread has four numbers, and asks for
+// those of eight parts at once. Memory bounds it: 15 segments of 32 heads, 64 MB, 14 us (4.6 TB/s).
 template <int D>
 __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
   constexpr int PER = D * D / 1024;      // workgroups for a state
