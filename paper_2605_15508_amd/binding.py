@@ -831,8 +831,8 @@ def sts_linear_attn(q, k, v, decay, scale=1.0, starts=None, lens=None, max_len=N
         B, n = k.shape[:2]
         shape = None if q is None else tuple(q.shape)
         k, v, q = (None if t is None else t.view(B * n, *t.shape[2:]) for t in (k, v, q))
-        assert decay.dim() == 1 or tuple(decay.shape[:2]) == (B, n)
-        decay = decay if decay.dim() == 1 else decay.view(B * n, -1)
+        assert decay.dim() == 1 or (decay.dim() == 3 and tuple(decay.shape[:2]) == (B, n))
+        decay = decay if decay.dim() == 1 else decay.view(B * n, decay.shape[2])
         assert max_len is None, "max_len goes with starts"
     else:
         B = _starts(starts, dev)

@@ -329,14 +329,14 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     if (OUT) load_rows(chunk, q, A.q_stride_n, q_off, to + AT_Q);
     asm volatile("" ::: "memory");       // (a chunk's stores come behind these loads: see `turn`)
   };
-  // (a wave's part of a block's decays: row `col` of every NW-th chunk)
+  // (a wave's part of a block's decays: row `col` of every NW-th chunk; of a sequence without rows that of a row next to it, which nothing comes of)
   float gates[MINE];
   auto load_gates = [&](int base) {
 #pragma unroll
-    for (int i = 0; i < MINE; ++i) gates[i] = A.decay[A.decay_rows ? (begin + (size_t)min((base + wave + i * NW) * C + col, max(rows - 1, 0))) * A.Hkv + g : g];
+    for (int i = 0; i < MINE; ++i) gates[i] = A.decay[A.decay_rows ? (size_t)max(begin + min((base + wave + i * NW) * C + col, rows - 1), 0) * A.Hkv + g : g];
   };
   __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(A.k), 0, 0, 0x00027000), (lds_ptr)lds_d, 4, 0, 0, 0, 0);
-  if (rows > 0) load_gates(0);
+  load_gates(0);
   load(0, lds_0);
 
   // ---- the state: lane (h, col) has column 32 wave + col, in element 4 j + i of tile m the row 32 m + 16 (j / 2) + 8 h + 4 (j % 2) + i

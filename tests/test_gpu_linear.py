@@ -70,7 +70,7 @@ def test_blocks(B, n, Hq, Hkv, gates, d):
     check((None, S), q, k, v, decay, 0.1, starts, first, False, out=False, what="states only")
 
 
-PROMPTS = [(1, 1, [17]), (4, 1, [31, 32, 33]), (2, 2, [1, 0, 64, 65]), (8, 2, [100, 0, 257, 1]), (4, 4, [128, 129, 127]), (16, 1, [40, 385]), (3, 1, [300]), (32, 8, [50, 160])]
+PROMPTS = [(1, 1, [17]), (2, 2, [0, 20, 0]), (4, 2, [0, 140, 0, 0]), (4, 1, [31, 32, 33]), (2, 2, [1, 0, 64, 65]), (8, 2, [100, 0, 257, 1]), (4, 4, [128, 129, 127]), (16, 1, [40, 385]), (3, 1, [300]), (32, 8, [50, 160])]
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -450,6 +450,10 @@ def test_empty_batches():
     pool, first = torch.zeros(3, 2, 64, 64, device=DEV), states(3, 2, 64, 9).to(DEV)
     sts.sts_linear_attn(q, k, v, decay, 0.1, starts=torch.full((4,), 5, dtype=torch.int32, device=DEV), state=first, state_out=pool, out=out)
     assert (out == 3).all() and torch.equal(pool, first)
+    pool.zero_()
+    pool.zero_()                                    # blocks of no rows
+    o, _ = sts.sts_linear_attn(q[:0].view(3, 0, 4, 64), k[:0].view(3, 0, 2, 64), v[:0].view(3, 0, 2, 64), decay[:0].view(3, 0, 2), 0.1, state=first, state_out=pool)
+    assert o.shape == (3, 0, 4, 64) and torch.equal(pool, first)
     pool.zero_()
     o, _ = sts.sts_linear_attn(q[:0], k[:0], v[:0], decay[:0], 0.1, starts=torch.zeros(4, dtype=torch.int32, device=DEV), state=first, state_out=pool)
     assert o.shape == (0, 4, 64) and torch.equal(pool, first)
