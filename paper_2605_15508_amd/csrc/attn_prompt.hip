@@ -417,6 +417,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
             }
           }
       }
+      __syncthreads();             // (nobody reads the tiles any more)
     }
   }
 
@@ -427,22 +428,51 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2) prompt_attn_kerne
     const uint32_t q0 = q[0], q1 = q[1];
     l_run = __builtin_bit_cast(float, q0) + __builtin_bit_cast(float, q1);
   }
-  if (!ok) return;
+  // The wave's rows go through LDS (16 bytes at a time, at other places in every row, so that neither way meets in a bank), to be written as they lie in memory:
+  // lane by lane they would leave in pieces of 8 or 16 bytes.
   const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-  const size_t row = (size_t)piece.begin + p, at = (row * A.Hq + head) * D + 4 * h;
+  const size_t row = (size_t)piece.begin + p;
+  const lds_ptr mine = (lds_ptr)(wave == 0 ? lds_k0 : wave == 1 ? lds_k1 : wave == 2 ? lds_v0 : lds_v1);
+  auto write_out = [&](auto wide) {
+    constexpr bool F32 = decltype(wide)::value;
+    constexpr int PIECES = D * (F32 ? 4 : 2) / 16, AT_ONCE = 64 / PIECES;       // of a row; rows that a store covers
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const f32x4 o = {acc[dt][4 * e] * inv, acc[dt][4 * e + 1] * inv, acc[dt][4 * e + 2] * inv, acc[dt][4 * e + 3] * inv};
-      if (A.out_dtype == STS_F32) {
-        *reinterpret_cast<f32x4 *>(static_cast<float *>(A.out) + at + 32 * dt + 8 * e) = o;
-      } else {
-        const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[0], o[1]}), bf16x2)),
-                         __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[2], o[3]}), bf16x2))};
-        *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(A.out) + at + 32 * dt + 8 * e) = w;
+      for (int j = 0; j < (F32 ? 4 : 2); ++j) {
+        u32x4 w;
+        int at;
+        if constexpr (F32) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, acc[dt][4 * j + i] * inv);
+          at = 8 * dt + 2 * j + h;
+        } else {
+          // (channels 16 j + 4 h .. and 8 further on: the halves of the wave exchange some, so that each has eight side by side)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc[dt][8 * j + 2 * i] * inv, acc[dt][8 * j + 2 * i + 1] * inv}), bf16x2));
+            const uint32_t hi = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc[dt][8 * j + 4 + 2 * i] * inv, acc[dt][8 * j + 5 + 2 * i] * inv}), bf16x2));
+            const auto q = __builtin_amdgcn_permlane32_swap(lo, hi, false, false);
+            w[i] = q[0];
+            w[2 + i] = q[1];
+          }
+          at = 4 * dt + 2 * j + h;
+        }
+        *(__attribute__((address_space(3))) u32x4 *)(mine + 16 * (col * PIECES + (at ^ (col & (PIECES - 1))))) = w;
       }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // (of this wave alone)
+    const int piece_at = lane % PIECES;
+#pragma unroll
+    for (int i = 0; i < 32 / AT_ONCE; ++i) {
+      const int at = i * AT_ONCE + lane / PIECES, r = row_w + at;
+      const u32x4 w = *(lds_u32x4)(mine + 16 * (at * PIECES + (piece_at ^ (at & (PIECES - 1)))));
+      const int pos = A.by_group.of(min(r, rows - 1));
+      if (r < rows) *reinterpret_cast<u32x4 *>(static_cast<unsigned char *>(A.out) + (((size_t)piece.begin + pos) * A.Hq + g * A.G + r - pos * A.G) * (D * (F32 ? 4 : 2)) + 16 * piece_at) = w;
     }
+  };
+  if (A.out_dtype == STS_F32) write_out(std::true_type());
+  else write_out(std::false_type());
+  if (!ok) return;
   // (a row whose sum is no number has the logarithm -inf, as everywhere in the library)
   if (A.lse_out && h == 0) A.lse_out[(size_t)head * A.seqs.T + row] = l_run > 0.f ? (m_run + __builtin_amdgcn_logf(l_run)) * 0.69314718055994530942f : -INFINITY;
 }
