@@ -623,19 +623,29 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
           __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), to, at + 32 * j + 16 * h, 0, 0);
         }
       } else {
+        u32x4 w[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          u32x4 w;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{R[8 * j + 2 * i], R[8 * j + 2 * i + 1]}), bf16x2));
             const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{R[8 * j + 4 + 2 * i], R[8 * j + 5 + 2 * i]}), bf16x2));
             const auto swapped = __builtin_amdgcn_permlane32_swap(x, y, false, false);
-            w[i] = swapped[0];
-            w[2 + i] = swapped[1];
+            w[j][i] = swapped[0];
+            w[j][2 + i] = swapped[1];
           }
-          __builtin_amdgcn_raw_buffer_store_b128(w, to, at + 32 * j + 16 * h, 0, 0);
         }
+        // At head size 64 the rows of 16 lanes do so, too: a store writes the wave's 64 bytes of 16 rows, not 32 of 32 (sixteen prompts 109.4 us without, 104.1
+        // with; at head size 128, where more waves share a row, six prompts 102.9 and 104.8).
+#pragma unroll
+        for (int i = 0; D == 64 && i < 4; ++i) {
+          const uint32_t x = w[0][i], y = w[1][i];
+          const auto swapped = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+          w[0][i] = swapped[0];
+          w[1][i] = swapped[1];
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) __builtin_amdgcn_raw_buffer_store_b128(w[j], to, D == 64 ? (16 * j + (col & 15)) * pitch + 32 * wave * bytes + 2 * (col & 16) + 16 * h : at + 32 * j + 16 * h, 0, 0);
       }
     }
   };
