@@ -335,7 +335,10 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 #pragma unroll
     for (int i = 0; i < MINE; ++i) gates[i] = A.decay[A.decay_rows ? (size_t)max(begin + min((base + wave + i * NW) * C + col, rows - 1), 0) * A.Hkv + g : g];
   };
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(A.k), 0, 0, 0x00027000), (lds_ptr)lds_d, 4, 0, 0, 0, 0);
+  // (the load of no bytes: it writes zeros all the same, whenever it ends, so that it goes where no chunk has anything)
+  static_assert(16 * (PLACES - MINE * NW) >= 64, "");
+  if (lane < 16)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(A.k), 0, 0, 0x00027000), (lds_ptr)lds_d + AT_CHUNK + 16 * MINE * NW, 4, 0, 0, 0, 0);
   load_gates(0);
   load(0, lds_0);
 

@@ -389,6 +389,24 @@ def test_the_same_from_run_to_run(n):
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+@pytest.mark.parametrize("d,B,Hq,Hkv", [(64, 14, 16, 16), (128, 3, 32, 8), (128, 4, 16, 16)])
+def test_a_full_chip_gives_the_same_from_run_to_run(d, B, Hq, Hkv):
+    """More workgroups than run at once, so that some begin where others have ended, at another pace."""
+    lens = [2000 - 133 * b for b in range(B)]
+    q, k, v, decay = (on(t) for t in data(sum(lens), Hq, Hkv, d, 47))
+    starts = starts_of(lens).to(DEV)
+    call = lambda: sts.sts_linear_attn(q, k, v, decay, 0.1, starts=starts, max_len=2000, state_out=torch.empty(B, Hkv, d, d, device=DEV))  # noqa: E731
+    first = call()
+    for _ in range(20):
+        again = call()
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    b, g = B - 1, Hkv - 1                             # and that is right: the last sequence's last head
+    h, kv = slice(Hq - Hq // Hkv, Hq), slice(g, g + 1)
+    a, e = int(starts[b]), int(starts[b + 1])
+    rows_ = [t.cpu()[a:e] for t in (q[:, h], k[:, kv], v[:, kv], decay[:, kv])]
+    check((first[0][a:e, h], first[1][b:, kv]), *rows_, 0.1, starts_of([e - a]), torch.zeros(1, 1, d, d), True)
+
+
 def test_many_sequences():
     g = torch.Generator().manual_seed(30)
     lens = torch.randint(0, 4, (5000,), generator=g).tolist()
