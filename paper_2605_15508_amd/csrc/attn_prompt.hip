@@ -9,10 +9,10 @@
 // (j = 0..3, i = 0..3) of each 32, two j of which are what it supplies as the B operand of O^T += V^T P^T for 16 keys: P stays in its lane,
 // and V's operand takes the keys in that order, out of V's rows in LDS by the transposing read.
 //
-// What bounds it: the two products, and beside them at head size 128 the power that the card has: 8192 rows, 32 heads in groups of 4, take 500 us,
-// 1.1 PFLOP/s of what rows see (a plain product of the library reaches 1.2 to 1.4), with matrix instructions 66% of the cycles and vector
-// instructions 58% at a clock of 1.7 GHz that the load leaves (alone on its compute unit a block takes 0.87 us for a tile, of which the products are 0.43). At
-// head size 64 every exponential stands beside half the products: sixteen prompts of 100 to 4000 rows, 215 us, 0.8 PFLOP/s, vector instructions 77%.
+// What bounds it: the two products, and beside them at head size 128 the power that the card has: 8192 rows, 32 heads in groups of 4, take 490 us,
+// 1.1 PFLOP/s of what rows see (a plain product of the library reaches 1.2 to 1.4), with matrix instructions 67% of the cycles and vector
+// instructions 60% at a clock of 1.7 GHz that the load leaves (alone on its compute unit a block takes 0.87 us for a tile, of which the products are 0.43). At
+// head size 64 every exponential stands beside half the products: sixteen prompts of 100 to 4000 rows, 205 us, 0.8 PFLOP/s, vector instructions 82%.
 // Two workgroups on a compute unit (three at head size 64), since one wave's softmax is another's product. 128 rows of a block, not more, as the tiles that its
 // rows see in part cost as much as whole ones; 64 keys of a tile are what two tiles of K and V each leave of LDS.
 #include <float.h>

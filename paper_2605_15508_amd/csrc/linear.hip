@@ -10,9 +10,9 @@
 // products q . k by itself, so that these pass from accumulator to operand in their lane, as the state does: nothing goes through LDS but
 // rows of Q, K and V. Long sequences are cut into segments: one kernel sums up what each segment adds to the state, one
 // adds these up along the sequence, and a third starts every segment from the state before it.
-// What bounds it without groups: memory. 8192 rows with 32 heads of 128 take 119 us: sums 36 (170 MB, 4.6 TB/s), adding up 14 (64 MB), results 58
-// (300 MB, 5.1 TB/s), and what lies between three launches. With groups of heads (each with a state of its own in the results' kernel) matrix and vector instructions, which
-// take 44% and 48% of its cycles and hardly overlap: six prompts of 77 to 6001 rows, 32 heads in groups of four, 103 us, of which the results 75.
+// What bounds it without groups: memory. 8192 rows with 32 heads of 128 take 117 us: sums 35 (170 MB, 4.8 TB/s), adding up 14 (64 MB), results 60
+// (300 MB, 5.0 TB/s), and what lies between three launches. With groups of heads (each with a state of its own in the results' kernel) matrix and vector instructions, which
+// take 44% and 48% of its cycles and hardly overlap: six prompts of 77 to 6001 rows, 32 heads in groups of four, 101 us, of which the results 75.
 #include "attn_util.h"
 #include "layers.h"
 

@@ -185,6 +185,21 @@ def test_the_same_from_run_to_run_and_without_lse():
     assert lse is None and torch.equal(out, first[0])
 
 
+@pytest.mark.parametrize("d,B,Hq,Hkv", [(64, 14, 16, 4), (128, 7, 32, 8), (128, 3, 16, 16)])
+def test_a_full_chip_gives_the_same_from_run_to_run(d, B, Hq, Hkv):
+    """More workgroups than run at once, so that some begin where others have ended, at another pace."""
+    lens = [2500 - 171 * b for b in range(B)]
+    starts = starts_of(lens)
+    q, k, v = (t.to(DEV) for t in data(sum(lens), Hq, Hkv, d, 18))
+    first = sts.sts_prompt_attn(q, k, v, starts.to(DEV), 0.1)
+    for _ in range(20):
+        again = sts.sts_prompt_attn(q, k, v, starts.to(DEV), 0.1)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    a, e, G = int(starts[-2]), int(starts[-1]), Hq // Hkv                 # and that is right: the last sequence's last heads
+    ref = prompts(q[a:e, Hq - G:].cpu(), k[a:e, Hkv - 1:].cpu(), v[a:e, Hkv - 1:].cpu(), starts_of([e - a]), 0.1)
+    check_prompts((first[0][a:e, Hq - G:], first[1][Hq - G:, a:e]), ref)
+
+
 def test_starts_that_make_no_sense_touch_nothing_else():
     """Out of order and out of range: results are not defined, but nothing behind the tensors is written to."""
     T = 300
