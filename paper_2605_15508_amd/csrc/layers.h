@@ -87,7 +87,8 @@ struct LinearArgs {
   // (a multiple of STS_LINEAR_CHUNK); numbers of segments and of parts (piece_numbers); what each part adds to the state and the logarithm
   // of its decay, later the states before the segments in the places of their first parts
   int32_t segment, parts, part_rows, numbers, part_numbers;
-  Divisor by_segment, by_part, by_heads, by_group;
+  int32_t heads;                     // of a group that a workgroup of the results has, 1 or 2
+  Divisor by_segment, by_part, by_heads, by_group, by_turns;
   float *part;                       // [part_numbers][Hkv][d][d], or NULL: nothing is handed on
   double *part_log;                  // [part_numbers][Hkv]
 };

@@ -270,27 +270,27 @@ template <int D> __device__ __forceinline__ int state_place(int q) {
 //
 // OUT: results, from the state before the segment; else what the segment adds to the state (or, of a sequence with one segment, its
 // state)
-template <int D, bool OUT>
+template <int D, bool OUT, int HEADS>
 __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs A) {
   constexpr int NW = D / 32;             // waves, each with 32 columns of the state
   constexpr int KS = D / 16, MT = D / 32, CH = D / 8;
   constexpr int NL = C * CH / (64 * NW), RL = 64 / CH;      // loads of a wave for 32 rows, rows that each covers
   // (What LDS has left at two and four workgroups. Each time takes 2 us: 8192 rows, 17 chunks a segment, 123 us with 15 at once, 119 with 18.)
-  constexpr int BLOCK = D == 128 ? 18 : 9, MINE = (BLOCK + NW - 1) / NW;   // chunks whose decays are worked out at once, those of a wave
-  constexpr int PLACES = BLOCK > 16 ? 32 : 16;              // lanes that have one of them, or none
+  constexpr int BLOCK = D == 128 ? 18 : HEADS == 2 ? 16 : 9, MINE = (BLOCK + NW - 1) / NW;   // chunks whose decays are worked out at once, those of a wave
+  constexpr int PLACES = BLOCK >= 16 ? 32 : 16;              // lanes that have one of them, or none
   // Three chunks of K, V and Q, and a block's decays: for each row its sum c, its weight as a key, its factor as a query, and for each chunk what
   // concerns all rows. Arrays of their own, so that the compiler can tell the loads that fill one from the reads of another; it would have reads of an array
   // that no load fills wait for all loads, so that one load of no bytes goes to the decays', too.
-  constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, ALL = (OUT ? 3 : 2) * TILE;
-  constexpr int LOADS = (OUT ? 3 : 2) * NL, STORES = OUT ? 2 : 0;      // of a wave and chunk
+  constexpr int TILE = C * CH, AT_V = TILE, AT_Q = 2 * TILE, ALL = (OUT ? 2 + HEADS : 2) * TILE, DEPTH = HEADS == 2 ? 2 : 3;
+  constexpr int LOADS = (OUT ? 2 + HEADS : 2) * NL, STORES = OUT ? 2 * HEADS : 0;      // of a wave and chunk
   constexpr int AT_KEY = MINE * NW * C * 4, AT_QUERY = 2 * AT_KEY, AT_CHUNK = 3 * AT_KEY;
-  __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_2[ALL], lds_d[AT_CHUNK / 16 + PLACES];
+  __shared__ __attribute__((aligned(16))) u32x4 lds_0[ALL], lds_1[ALL], lds_2[DEPTH == 3 ? ALL : 1], lds_d[AT_CHUNK / 16 + PLACES];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
   // Neighbouring units on different dies (workgroup i runs on die i % 8), which evens out the numbers that no segment has; the heads of a group (each
   // with a state of its own, which is the same) on one die, one after the other: they read the same K and V.
-  const int turns = blockIdx.x / STS_XCDS, eight = OUT ? A.by_group.of(turns) : turns, hd = OUT ? turns - eight * A.G : 0;
+  const int turns = blockIdx.x / STS_XCDS, eight = OUT ? A.by_turns.of(turns) : turns, hd = OUT ? turns * HEADS - eight * A.G : 0;
   const int unit = eight * STS_XCDS + blockIdx.x % STS_XCDS;
   if (unit >= (OUT ? A.numbers : A.part_numbers) * A.Hkv) return;
   const int number = A.by_heads.of(unit), g = unit - number * A.Hkv, head = g * A.G + hd;
@@ -326,7 +326,10 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   auto load = [&](int chunk, u32x4 *to) {
     load_rows(chunk, k, A.kv_stride_n, kv_off, to);
     load_rows(chunk, v, A.kv_stride_n, kv_off, to + AT_V);
-    if (OUT) load_rows(chunk, q, A.q_stride_n, q_off, to + AT_Q);
+    if constexpr (OUT) {
+#pragma unroll
+      for (int hh = 0; hh < HEADS; ++hh) load_rows(chunk, q + hh * A.q_stride_h, A.q_stride_n, q_off, to + AT_Q + hh * TILE);
+    }
     asm volatile("" ::: "memory");       // (a chunk's stores come behind these loads: see `turn`)
   };
   // (a wave's part of a block's decays: row `col` of every NW-th chunk; of a sequence without rows that of a row next to it, which nothing comes of)
@@ -390,7 +393,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   };
   // The chunk has come: behind its loads lie the next chunk's and the last chunk's stores at least (memory operations end in their order). And
   // what was read is in registers.
-  auto turn = [] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS + STORES) : "memory"); };
+  auto turn = [] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(DEPTH == 3 ? LOADS + STORES : STORES) : "memory"); };
   auto all_waves = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
   // ---- Decays, in powers of two: c_i the sum over the chunk's rows up to i. With u_i = exp(c_i - c_32)
@@ -416,10 +419,11 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
       *(lds_f32)(decays + chunk * C * 4 + 4 * col) = c[i];
       *(lds_f32)(decays + AT_CHUNK + 16 * chunk + 12) = __builtin_amdgcn_ballot_w64(own > 1.f) ? 1.f : 0.f;
     }
-    load_gates(base + BLOCK);
+    if (HEADS == 1) load_gates(base + BLOCK);
     all_waves();
     // (no branches but those that all lanes take alike: the loop around would get ways through it that there are not, and the compiler's waits with them)
-    const int mine = lane & (PLACES - 1);  // the lane's chunk
+    int mine = lane & (PLACES - 1);        // the lane's chunk
+    asm("" : "+v"(mine));                   // (what comes of it is made anew, not kept in registers)
     const float end = number_of((min(mine, BLOCK - 1) * C + 31) * 4), grows = number_of(AT_CHUNK + 16 * mine + 12);
     const double sum = sums_before<PLACES>(mine < BLOCK ? end : 0.0), before = low + sum, behind = before + end;      // (0 behind the last chunk)
     const double total = lane_of(sum, BLOCK - 1) + lane_of(end, BLOCK - 1);
@@ -428,7 +432,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     auto whole = [](double x) { return __builtin_floor(x * 0.0625) * 16.0; };
     const double low_before = before - whole(before), low_behind = behind - whole(behind);
     const float F = exp2_32(low_behind), F_inv = exp2_32(-low_behind), step = __builtin_amdgcn_exp2f((float)(whole(behind) - whole(before)));
-    low -= whole(low);
+    low = lane_of(low - whole(low), 0);        // (the same in all lanes, and so in scalar registers)
     *(__attribute__((address_space(3))) f32x4 *)(decays + AT_CHUNK + 16 * mine) = f32x4{step, end >= -60.f && grows == 0.f ? 0.f : 1.f, (float)low_before, grows};
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
@@ -449,7 +453,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 
   auto body = [&](int chunk, int in_block, u32x4 *lds, u32x4 *free) {
     turn();
-    load(chunk + 2, free);                 // (before the reads: behind them the compiler would wait for the next chunk's)
+    load(chunk + DEPTH - 1, free);         // (before the reads: behind them the compiler would wait for the next chunk's)
     // (what comes of these is made anew in every chunk, not kept in registers)
     int r_at = r_lane, v_at = v_lane, k_at = k_lane;
     asm("" : "+v"(r_at), "+v"(v_at), "+v"(k_at));
@@ -463,13 +467,14 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 #pragma unroll
     for (int e = 0; e < 16; ++e) left[e] = *(lds_f32)(mine + AT_KEY + 4 * (8 * (e >> 2) + 4 * h + (e & 3)));
     const float own_factor = OUT ? *(lds_f32)(mine + AT_QUERY + 4 * col) : 0.f;
-    if constexpr (OUT) {
+    auto read_rows = [&](int hh) {
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         K[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)lds + (r_at ^ (32 * s))));
-        Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)(lds + AT_Q) + (r_at ^ (32 * s))));
+        Q[s] = __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)(lds + AT_Q + hh * TILE) + (r_at ^ (32 * s))));
       }
-    }
+    };
+    if constexpr (OUT) read_rows(0);
     __builtin_amdgcn_sched_barrier(0);
     if (chunk >= chunks) return;
     const float f0 = four[0], f1 = four[1];        // (a cast of a vector's element would be one of its first)
@@ -480,193 +485,205 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     // ---- X^T = K Q^T: row q . k of keys 8 j + 4 h + i and query col; O^T = S^T Q^T. The state enters the product as bf16 (half a step, 2^-8 of
     // each number; the state itself stays as it is). The order of instructions is given (the compiler's own waits for every operand by itself): matrix
     // instructions alternate with what makes operands of the state and of V.
-    f32x16 X = {}, O = {};
-    if constexpr (OUT) {
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        X = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K[s], Q[s], X, 0, 0, 0);
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{S[s / 2][8 * (s % 2) + 2 * e], S[s / 2][8 * (s % 2) + 2 * e + 1]}), bf16x2));
-        O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), Q[s], O, 0, 0, 0);
-      }
-    }
-    // V with its weights as the sum of three bf16 numbers, which hold an fp32's bits: the products enter the state as exactly as in fp32
     bf16x8 W[3][2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const u32x4 two = __builtin_bit_cast(u32x4, V[s]);
-      u32x4 w[3];
+    for (int hh = 0; hh < HEADS; ++hh) {
+      const bool to_state = hh == HEADS - 1;
+      if (hh > 0) {
+        read_rows(hh);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      f32x16 X = {}, O = {};
+      if constexpr (OUT) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f32x2 x = {left[8 * s + 2 * e] * __builtin_bit_cast(float, two[e] << 16), left[8 * s + 2 * e + 1] * __builtin_bit_cast(float, two[e] & 0xffff0000u)};
+        for (int s = 0; s < KS; ++s) {
+          X = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K[s], Q[s], X, 0, 0, 0);
+          u32x4 w;
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
-          const uint32_t top2 = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-          w[i][e] = top2;
-          x[0] -= __builtin_bit_cast(float, top2 << 16);
-          x[1] -= __builtin_bit_cast(float, top2 & 0xffff0000u);
+          for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{S[s / 2][8 * (s % 2) + 2 * e], S[s / 2][8 * (s % 2) + 2 * e + 1]}), bf16x2));
+          O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), Q[s], O, 0, 0, 0);
         }
       }
+      // V with its weights as the sum of three bf16 numbers, which hold an fp32's bits: the products enter the state as exactly as in fp32
+      if (to_state)
 #pragma unroll
-      for (int i = 0; i < 3; ++i) W[i][s] = __builtin_bit_cast(bf16x8, w[i]);
-    }
+      for (int s = 0; s < 2; ++s) {
+        const u32x4 two = __builtin_bit_cast(u32x4, V[s]);
+        u32x4 w[3];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+        for (int e = 0; e < 4; ++e) {
+          f32x2 x = {left[8 * s + 2 * e] * __builtin_bit_cast(float, two[e] << 16), left[8 * s + 2 * e + 1] * __builtin_bit_cast(float, two[e] & 0xffff0000u)};
 #pragma unroll
-      for (int s = 0; s < 2; ++s) T[2 * m + s] = transposed(lds, k_at, m, s);
-    bool odd = false;
-    if constexpr (OUT) {
-      // Has the chunk a value that is infinite or no number? Rows before it do not see it, but 0 times it is not 0.
-      float z = 0.f;
-      const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
+          for (int i = 0; i < 3; ++i) {
+            const uint32_t top2 = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+            w[i][e] = top2;
+            x[0] -= __builtin_bit_cast(float, top2 << 16);
+            x[1] -= __builtin_bit_cast(float, top2 & 0xffff0000u);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) W[i][s] = __builtin_bit_cast(bf16x8, w[i]);
+      }
+      if (to_state)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) T[2 * m + s] = transposed(lds, k_at, m, s);
+      bool odd = false;
+      if constexpr (OUT) {
+        // Has the chunk a value that is infinite or no number? Rows before it do not see it, but 0 times it is not 0.
+        float z = 0.f;
+        const bf16x2 none = {(__bf16)0.f, (__bf16)0.f};
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t two = __builtin_bit_cast(u32x4, V[s])[e];
+            z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), none, z, false);
+          }
+        odd = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x2, 160 / (2 * KS), 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (to_state && apart) multiply(f);
+
+      // ---- The state, and the weights of the chunk's rows, as bf16 (half a step, 2^-8 of each): none for keys behind the query, whatever their
+      // product is. (Worked out without a look at `apart` and `odd`, and once more where one of them holds.)
+      f32x16 R = O;
+      auto weights = [&](const f32x16 &x, bf16x8 (&P)[2]) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          u32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            f32x2 y;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
+              y[i] = key <= col ? x[at] : 0.f;
+            }
+            w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+          }
+          P[s] = __builtin_bit_cast(bf16x8, w);
+        }
+      };
+      if constexpr (OUT) {
+        f32x16 x;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = X[e] * left[e];
+        bf16x8 P[2];
+        weights(x, P);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) R = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], R, 0, 0, 0);
+      }
+      if (to_state)
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t two = __builtin_bit_cast(u32x4, V[s])[e];
-          z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), none, z, false);
+        for (int i = 2; i >= 0; --i)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(T[2 * m + s], W[i][s], S[m], 0, 0, 0);
+      if constexpr (OUT) {
+#pragma unroll
+        for (int i = 0; i < 6 * MT; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+          __builtin_amdgcn_sched_group_barrier(0x2, 48 / (4 * MT), 1);
         }
-      odd = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
+        __builtin_amdgcn_sched_barrier(0);
+        if (apart || odd) {
+          const float c = *(lds_f32)(mine + 4 * col), own = apart ? exp2_32((double)four[2] + c) : 1.f;
 #pragma unroll
-      for (int i = 0; i < 2 * KS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, 160 / (2 * KS), 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    if (apart) multiply(f);
-
-    // ---- The state, and the weights of the chunk's rows, as bf16 (half a step, 2^-8 of each): none for keys behind the query, whatever their
-    // product is. (Worked out without a look at `apart` and `odd`, and once more where one of them holds.)
-    f32x16 R = O;
-    auto weights = [&](const f32x16 &x, bf16x8 (&P)[2]) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          f32x2 y;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int at = 8 * s + 2 * e + i, key = 8 * (at >> 2) + 4 * h + (at & 3);
-            y[i] = key <= col ? x[at] : 0.f;
+          for (int e = 0; e < 16; ++e) {
+            const float pair = __builtin_amdgcn_exp2f(c - *(lds_f32)(mine + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));
+            R[e] = O[e] * own;
+            X[e] *= apart ? pair : left[e];
           }
-          w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
-        }
-        P[s] = __builtin_bit_cast(bf16x8, w);
-      }
-    };
-    if constexpr (OUT) {
-      f32x16 x;
+          bf16x8 P[2];
+          weights(X, P);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = X[e] * left[e];
-      bf16x8 P[2];
-      weights(x, P);
+          for (int s = 0; s < 2; ++s) {
+            if (!odd) R = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], R, 0, 0, 0);
+            for (int key = 0; key < (odd ? 16 : 0); ++key) {      // key by key, and a row is taken in only where it is seen
+              u32x4 own_key;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) R = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], R, 0, 0, 0);
-    }
+              for (int e = 0; e < 4; ++e) {
+                const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
+                own_key[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
+              }
+              const f32x16 zero = {};
+              const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, V[s]) & own_key),
+                                                                       __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, P[s]) & own_key), zero, 0, 0, 0);
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int i = 2; i >= 0; --i)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(T[2 * m + s], W[i][s], S[m], 0, 0, 0);
-    if constexpr (OUT) {
-#pragma unroll
-      for (int i = 0; i < 6 * MT; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-        __builtin_amdgcn_sched_group_barrier(0x2, 48 / (4 * MT), 1);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      if (apart || odd) {
-        const float c = *(lds_f32)(mine + 4 * col), own = apart ? exp2_32((double)four[2] + c) : 1.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float pair = __builtin_amdgcn_exp2f(c - *(lds_f32)(mine + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));
-          R[e] = O[e] * own;
-          X[e] *= apart ? pair : left[e];
-        }
-        bf16x8 P[2];
-        weights(X, P);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          if (!odd) R = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V[s], P[s], R, 0, 0, 0);
-          for (int key = 0; key < (odd ? 16 : 0); ++key) {      // key by key, and a row is taken in only where it is seen
-            u32x4 own_key;       // element e of the lane's eight: key 4 h + e % 4 + 8 (e / 4)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int k0 = 4 * h + 2 * (e & 1) + 8 * (e >> 1);
-              own_key[e] = (key == k0 ? 0xffffu : 0u) | (key == k0 + 1 ? 0xffff0000u : 0u);
+              for (int e = 0; e < 16; ++e) R[e] += 16 * s + key <= col ? x[e] : 0.f;
             }
-            const f32x16 zero = {};
-            const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, V[s]) & own_key),
-                                                                     __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, P[s]) & own_key), zero, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) R[e] += 16 * s + key <= col ? x[e] : 0.f;
           }
         }
       }
-    }
-    if constexpr (OUT) {
-      // Two stores or more, which `turn` counts. The lane has channels 8 j + 4 h + i; as bf16 the halves of the wave exchange some, so that each
-      // has eight channels side by side.
+      if constexpr (OUT) {
+        // Two stores or more, which `turn` counts. The lane has channels 8 j + 4 h + i; as bf16 the halves of the wave exchange some, so that each
+        // has eight channels side by side.
 #pragma unroll
-      for (int e = 0; e < 16; ++e) R[e] *= own_factor;
-      // (rows behind the last are behind the end that the stores are told)
-      const int n = __builtin_amdgcn_readfirstlane(min(rows - chunk * C, C)), bytes = A.out_dtype == STS_F32 ? 4 : 2, pitch = A.Hq * D * bytes;
-      const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(static_cast<unsigned char *>(A.out) + (((int64_t)begin + chunk * C) * A.Hq + head) * D * bytes, 0,
-                                                                          (n - 1) * pitch + D * bytes, 0x00027000);
-      const int at = col * pitch + 32 * wave * bytes;
-      if (A.out_dtype == STS_F32) {
+        for (int e = 0; e < 16; ++e) R[e] *= own_factor;
+        // (rows behind the last are behind the end that the stores are told)
+        const int n = __builtin_amdgcn_readfirstlane(min(rows - chunk * C, C)), bytes = A.out_dtype == STS_F32 ? 4 : 2, pitch = A.Hq * D * bytes;
+        const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(static_cast<unsigned char *>(A.out) + (((int64_t)begin + chunk * C) * A.Hq + head + hh) * D * bytes, 0,
+                                                                            (n - 1) * pitch + D * bytes, 0x00027000);
+        const int at = col * pitch + 32 * wave * bytes;
+        if (A.out_dtype == STS_F32) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x4 o = {R[4 * j], R[4 * j + 1], R[4 * j + 2], R[4 * j + 3]};
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), to, at + 32 * j + 16 * h, 0, 0);
-        }
-      } else {
-        u32x4 w[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{R[8 * j + 2 * i], R[8 * j + 2 * i + 1]}), bf16x2));
-            const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{R[8 * j + 4 + 2 * i], R[8 * j + 5 + 2 * i]}), bf16x2));
-            const auto swapped = __builtin_amdgcn_permlane32_swap(x, y, false, false);
-            w[j][i] = swapped[0];
-            w[j][2 + i] = swapped[1];
+          for (int j = 0; j < 4; ++j) {
+            const f32x4 o = {R[4 * j], R[4 * j + 1], R[4 * j + 2], R[4 * j + 3]};
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), to, at + 32 * j + 16 * h, 0, 0);
           }
-        }
-        // At head size 64 the rows of 16 lanes do so, too: a store writes the wave's 64 bytes of 16 rows, not 32 of 32 (sixteen prompts 109.4 us without, 104.1
-        // with; at head size 128, where more waves share a row, six prompts 102.9 and 104.8).
+        } else {
+          u32x4 w[2];
 #pragma unroll
-        for (int i = 0; D == 64 && i < 4; ++i) {
-          const uint32_t x = w[0][i], y = w[1][i];
-          const auto swapped = __builtin_amdgcn_permlane16_swap(x, y, false, false);
-          w[0][i] = swapped[0];
-          w[1][i] = swapped[1];
-        }
+          for (int j = 0; j < 2; ++j) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) __builtin_amdgcn_raw_buffer_store_b128(w[j], to, D == 64 ? (16 * j + (col & 15)) * pitch + 32 * wave * bytes + 2 * (col & 16) + 16 * h : at + 32 * j + 16 * h, 0, 0);
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{R[8 * j + 2 * i], R[8 * j + 2 * i + 1]}), bf16x2));
+              const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{R[8 * j + 4 + 2 * i], R[8 * j + 5 + 2 * i]}), bf16x2));
+              const auto swapped = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+              w[j][i] = swapped[0];
+              w[j][2 + i] = swapped[1];
+            }
+          }
+          // At head size 64 the rows of 16 lanes do so, too: a store writes the wave's 64 bytes of 16 rows, not 32 of 32 (sixteen prompts 109.4 us without, 104.1
+          // with; at head size 128, where more waves share a row, six prompts 102.9 and 104.8).
+#pragma unroll
+          for (int i = 0; D == 64 && i < 4; ++i) {
+            const uint32_t x = w[0][i], y = w[1][i];
+            const auto swapped = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+            w[0][i] = swapped[0];
+            w[1][i] = swapped[1];
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) __builtin_amdgcn_raw_buffer_store_b128(w[j], to, D == 64 ? (16 * j + (col & 15)) * pitch + 32 * wave * bytes + 2 * (col & 16) + 16 * h : at + 32 * j + 16 * h, 0, 0);
+        }
       }
     }
   };
   work_out(0);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // (no stores come behind the first loads)
-  load(1, lds_1);
+  if (DEPTH == 3) load(1, lds_1);
   // (three chunks at a time, present or not: with more ways out of the loop than one the compiler would see ways back into it that there are not, and
   // wait for the loads of a chunk to come)
   for (int base = 0;;) {
     int i = 0;
     do {
-      body(base + i, i, lds_0, lds_2);
+      body(base + i, i, lds_0, DEPTH == 3 ? lds_2 : lds_1);
       body(base + i + 1, i + 1, lds_1, lds_0);
-      body(base + i + 2, i + 2, lds_2, lds_1);
-      i += 3;
+      if (DEPTH == 3) body(base + i + 2, i + 2, lds_2, lds_1);
+      i += DEPTH;
     } while (i < BLOCK && base + i < chunks);
     base += BLOCK;
     if (base >= chunks) break;
+    if (HEADS == 2) load_gates(base);      // (only now: it has no registers for them meanwhile, and rarely more than one block)
     all_waves();                           // (nobody reads the last block's decays any more)
     work_out(base);
   }
@@ -685,10 +702,11 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   float *to = state_out(A, piece.b);
   if (!to) return;
   to += (size_t)g * D * D;
+  const int again = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), s_end = 8 * (again >> 5) * D + 32 * wave + (again & 31);      // (s_at, not kept in a register)
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) to[s_at + (32 * m + 16 * (e >> 3) + (e & 7)) * D] = S[m][e];
+    for (int e = 0; e < 16; ++e) to[s_end + (32 * m + 16 * (e >> 3) + (e & 7)) * D] = S[m][e];
 }
 
 // Along each sequence of several segments: the state before every segment takes the place of what the segment adds. A thread has four numbers, and asks for
@@ -756,14 +774,17 @@ hipError_t launch_linear_step(const LinearArgs &a, int d, hipStream_t s) {
   return sts_take_launch_status();
 }
 
-template <int D, bool OUT>
+template <int D, bool OUT, int HEADS>
 static hipError_t launch_chunks(const LinearArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)(OUT ? a.numbers : a.part_numbers) * a.Hkv + STS_XCDS - 1) / STS_XCDS * STS_XCDS * (OUT ? a.G : 1))), block(2 * D);
-  STS_LAUNCH((linear_chunk_kernel<D, OUT>), grid, block, 0, s, a);
+  const dim3 grid((unsigned)(((int64_t)(OUT ? a.numbers : a.part_numbers) * a.Hkv + STS_XCDS - 1) / STS_XCDS * STS_XCDS * (OUT ? a.G / HEADS : 1))), block(2 * D);
+  STS_LAUNCH((linear_chunk_kernel<D, OUT, HEADS>), grid, block, 0, s, a);
   return sts_take_launch_status();
 }
-hipError_t launch_linear_sums(const LinearArgs &a, int d, hipStream_t s) { return d == 128 ? launch_chunks<128, false>(a, s) : launch_chunks<64, false>(a, s); }
-hipError_t launch_linear_chunks(const LinearArgs &a, int d, hipStream_t s) { return d == 128 ? launch_chunks<128, true>(a, s) : launch_chunks<64, true>(a, s); }
+hipError_t launch_linear_sums(const LinearArgs &a, int d, hipStream_t s) { return d == 128 ? launch_chunks<128, false, 1>(a, s) : launch_chunks<64, false, 1>(a, s); }
+hipError_t launch_linear_chunks(const LinearArgs &a, int d, hipStream_t s) {
+  if (a.heads == 2) return d == 128 ? launch_chunks<128, true, 2>(a, s) : launch_chunks<64, true, 2>(a, s);
+  return d == 128 ? launch_chunks<128, true, 1>(a, s) : launch_chunks<64, true, 1>(a, s);
+}
 
 hipError_t launch_linear_carry(const LinearArgs &a, int d, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.seqs.B * a.Hkv * (d * d / 1024))), block(256);

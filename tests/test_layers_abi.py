@@ -104,7 +104,7 @@ def resources():
     return build.kernel_resources()
 
 
-@pytest.mark.parametrize("name,forms", [("prompt_attn_kernel", 2), ("linear_step_kernel", 6), ("linear_chunk_kernel", 4), ("linear_carry_kernel", 2)])
+@pytest.mark.parametrize("name,forms", [("prompt_attn_kernel", 2), ("linear_step_kernel", 6), ("linear_chunk_kernel", 6), ("linear_carry_kernel", 2)])
 def test_kernels_fit_their_registers(resources, name, forms):
     found = {k: v for k, v in resources.items() if f"{len(name)}{name}I" in k}
     assert len(found) == forms
