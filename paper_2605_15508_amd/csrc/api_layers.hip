@@ -29,9 +29,9 @@ constexpr int64_t MOST_GROUPS = 1 << 24;      // workgroups of 256 threads that 
 struct LinearPlan {
   bool step;                 // the recurrent form
   int32_t each, max_len;     // rows of a sequence without starts; rows of the longest
-  int32_t segment, parts, heads, numbers, part_numbers;
+  int32_t segment, heads, numbers;
   bool several;              // a sequence may have more than one segment
-  bool carry;                // states are handed on: between segments, and to the heads of a group
+  bool carry;                // states are handed on: between segments, and to the workgroups of a group
   size_t part_bytes, log_bytes;
   size_t total() const { return part_bytes + log_bytes ? part_bytes + log_bytes : 256; }
 };
@@ -51,27 +51,22 @@ sts_status plan_linear(const sts_linear_params *p, LinearPlan &pl) {
   if ((int64_t)p->B * p->Hkv * (p->d * p->d / 1024) >= MOST_GROUPS) return STS_EUNSUPPORTED;
   if (pl.step) return STS_OK;
   // Segments: as many as the chip runs workgroups at once, two on a compute unit (four of half the waves), counting half a one more for each sequence
-  // (its last), but of 128 rows at least. (32 heads: 8192 rows take 115 us, with twice as many segments 135, with half as many 118; six prompts of 77 to 6000
-  // rows 190, 193 and 320; 64K rows 496, 508 and 570.) With many sequences, as many as cut those of twice the average length.
+  // (its last), but of 128 rows at least. (32 heads: 8192 rows take 115 us, with twice as many segments 135, with half as many 118; in groups of four
+  // six prompts of 77 to 6000 rows 173, with three quarters as many 189, with half as many 258.) With many sequences, as many as cut those of twice the
+  // average length. Two heads of a group go to one workgroup where groups are even.
   pl.heads = p->Hq / p->Hkv % 2 == 0 ? 2 : 1;
   const int64_t at_once = (int64_t)(p->d == 128 ? 2 : 4) * sts_cu_count() * pl.heads / p->Hq, left = at_once - p->B / 2 > at_once / 2 ? at_once - p->B / 2 : at_once / 2;
   int64_t segment = (p->T / (left > 0 ? left : 1) + STS_LINEAR_CHUNK) / STS_LINEAR_CHUNK * STS_LINEAR_CHUNK;
   if (segment < 128) segment = 128;
-  // The sums are worked out once for all heads of a group: in two parts of each segment, so that more of the chip is at work. (Six prompts of 77 to
-  // 6000 rows, 32 heads in groups of 4: 36 us for the sums and 6 for what carries them on with one part, 23 and 8.5 with two, 17 and 12 with four.)
-  const int64_t parts = p->Hq > p->Hkv && pl.heads == 1 ? 2 : 1;
-  segment = (segment + parts * STS_LINEAR_CHUNK - 1) / (parts * STS_LINEAR_CHUNK) * (parts * STS_LINEAR_CHUNK);
-  const int64_t numbers = piece_numbers(p->T, segment, p->B), part_numbers = piece_numbers(p->T, segment / parts, p->B);
-  if (numbers * p->Hq + STS_XCDS * STS_MAX_GROUP >= MOST_GROUPS || part_numbers * p->Hkv + STS_XCDS >= MOST_GROUPS) return STS_EUNSUPPORTED;
+  const int64_t numbers = piece_numbers(p->T, segment, p->B);
+  if (numbers * p->Hq + STS_XCDS * STS_MAX_GROUP >= MOST_GROUPS) return STS_EUNSUPPORTED;
   pl.segment = (int32_t)segment;
-  pl.parts = (int32_t)parts;
   pl.numbers = (int32_t)numbers;
-  pl.part_numbers = (int32_t)part_numbers;
-  pl.several = pl.max_len > (p->out ? segment : segment / parts);
-  pl.carry = pl.several || (p->out && p->Hq > p->Hkv);
+  pl.several = pl.max_len > segment;
+  pl.carry = pl.several || (p->out && p->Hq / p->Hkv > pl.heads);
   if (pl.carry) {
-    pl.part_bytes = align256((size_t)part_numbers * p->Hkv * p->d * p->d * sizeof(float));
-    pl.log_bytes = align256((size_t)part_numbers * p->Hkv * sizeof(double));
+    pl.part_bytes = align256((size_t)numbers * p->Hkv * p->d * p->d * sizeof(float));
+    pl.log_bytes = align256((size_t)numbers * p->Hkv * sizeof(double));
   }
   return STS_OK;
 }
@@ -161,12 +156,8 @@ sts_status sts_linear_attn(const sts_linear_params *p, void *stream) {
   const int d = p->d;
   if (pl.step) return sts_run_kernel(STS_K_LINEAR_STEP, s, [&] { return launch_linear_step(a, d, s); }) == hipSuccess ? STS_OK : STS_EHIP;
   a.segment = pl.segment;
-  a.parts = pl.parts;
-  a.part_rows = pl.segment / pl.parts;
   a.numbers = pl.numbers;
-  a.part_numbers = pl.part_numbers;
   a.by_segment = divide_by(a.segment);
-  a.by_part = divide_by(a.part_rows);
   a.heads = pl.heads;
   a.by_turns = divide_by(a.G / a.heads);
   if (pl.carry) {

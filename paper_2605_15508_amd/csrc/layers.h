@@ -83,14 +83,13 @@ struct LinearArgs {
   int32_t num_slots, num_slots_out;
   void *out;
   int32_t out_dtype;
-  // Chunked form: rows of a segment, of which each workgroup of the results has one, and how many parts the sums before it are made in; a part's rows
-  // (a multiple of STS_LINEAR_CHUNK); numbers of segments and of parts (piece_numbers); what each part adds to the state and the logarithm
-  // of its decay, later the states before the segments in the places of their first parts
-  int32_t segment, parts, part_rows, numbers, part_numbers;
+  // Chunked form: rows of a segment (a multiple of STS_LINEAR_CHUNK), of which each workgroup has one; numbers of segments (piece_numbers); what each segment
+  // adds to the state and the logarithm of its decay, later the states before the segments
+  int32_t segment, numbers;
   int32_t heads;                     // of a group that a workgroup of the results has, 1 or 2
-  Divisor by_segment, by_part, by_heads, by_group, by_turns;
-  float *part;                       // [part_numbers][Hkv][d][d], or NULL: nothing is handed on
-  double *part_log;                  // [part_numbers][Hkv]
+  Divisor by_segment, by_heads, by_group, by_turns;
+  float *part;                       // [numbers][Hkv][d][d], or NULL: nothing is handed on
+  double *part_log;                  // [numbers][Hkv]
 };
 constexpr int STS_LINEAR_CHUNK = 32, STS_LINEAR_STEP = 16;      // rows of a chunk; rows of a sequence that the recurrent form takes at most
 

@@ -11,8 +11,9 @@
 // rows of Q, K and V. Long sequences are cut into segments: one kernel sums up what each segment adds to the state, one
 // adds these up along the sequence, and a third starts every segment from the state before it.
 // What bounds it without groups: memory. 8192 rows with 32 heads of 128 take 117 us: sums 35 (170 MB, 4.8 TB/s), adding up 14 (64 MB), results 60
-// (300 MB, 5.0 TB/s), and what lies between three launches. With groups of heads (each with a state of its own in the results' kernel) matrix and vector instructions, which
-// take 44% and 48% of its cycles and hardly overlap: six prompts of 77 to 6001 rows, 32 heads in groups of four, 101 us, of which the results 75.
+// (300 MB, 5.0 TB/s), and what lies between three launches. With groups of heads, of which a workgroup of the
+// results has two that share a state, matrix and vector instructions, which hardly overlap: six prompts of 77 to 6001 rows, 32 heads in groups of four, 90 us, of
+// which the results 55 (with a head for each workgroup 103 and 75).
 #include "attn_util.h"
 #include "layers.h"
 
@@ -257,7 +258,7 @@ __device__ __forceinline__ double sums_before(double x) {
   return PLACES == 32 && threadIdx.x & 16 ? y + lane_of(x, 15) : y;
 }
 
-// A part's numbers lie as the waves hold them: element 4 e .. of tile m, four side by side, lane by lane, wave by wave. Place 4 q .. is this number of
+// A segment's numbers lie as the waves hold them: element 4 e .. of tile m, four side by side, lane by lane, wave by wave. Place 4 q .. is this number of
 // the state and the three below it:
 template <int D> __device__ __forceinline__ int state_place(int q) {
   constexpr int NW = D / 32;
@@ -266,7 +267,8 @@ template <int D> __device__ __forceinline__ int state_place(int q) {
 }
 
 // Two workgroups of four waves on a compute unit (head size 64: four of two waves), three chunks in LDS for each: one that is worked on, one that has come, one under
-// way. A chunk of 32 rows takes 42 matrix instructions of a wave at head size 128 (24 of them for the state, whose terms are split in three) and 320 vector instructions.
+// way; two of them where the queries of two heads come with each. A chunk of 32 rows takes 24 matrix instructions of a wave at head size 128 for the state, whose terms
+// are split in three, 18 for each head, and some 160 vector instructions for either.
 //
 // OUT: results, from the state before the segment; else what the segment adds to the state (or, of a sequence with one segment, its
 // state)
@@ -292,17 +294,17 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   // with a state of its own, which is the same) on one die, one after the other: they read the same K and V.
   const int turns = blockIdx.x / STS_XCDS, eight = OUT ? A.by_turns.of(turns) : turns, hd = OUT ? turns * HEADS - eight * A.G : 0;
   const int unit = eight * STS_XCDS + blockIdx.x % STS_XCDS;
-  if (unit >= (OUT ? A.numbers : A.part_numbers) * A.Hkv) return;
+  if (unit >= A.numbers * A.Hkv) return;
   const int number = A.by_heads.of(unit), g = unit - number * A.Hkv, head = g * A.G + hd;
-  const PackedPiece piece = find_piece(A.seqs, number, [&](int begin) { return OUT ? A.by_segment.of(begin) : A.by_part.of(begin); });
+  const PackedPiece piece = find_piece(A.seqs, number, [&](int begin) { return A.by_segment.of(begin); });
   if (piece.b < 0) return;
-  const int len = rows_of(A, piece.b, piece.len), most = OUT ? A.segment : A.part_rows, first = piece.index * most;
+  const int len = rows_of(A, piece.b, piece.len), first = piece.index * A.segment;
   const int segments = max((len + A.segment - 1) / A.segment, 1);
   if (first >= max(len, 1)) return;
   // (the last segment's state is brought by the results' kernel)
-  if (!OUT && A.out && piece.index >= (segments - 1) * A.parts) return;
+  if (!OUT && A.out && piece.index >= segments - 1) return;
   // (the same for all lanes, which the compiler does not see)
-  const int rows = __builtin_amdgcn_readfirstlane(min(most, len - first)), begin = __builtin_amdgcn_readfirstlane(piece.begin + first), chunks = (rows + C - 1) / C;
+  const int rows = __builtin_amdgcn_readfirstlane(min(A.segment, len - first)), begin = __builtin_amdgcn_readfirstlane(piece.begin + first), chunks = (rows + C - 1) / C;
   const bool last = first + rows >= len;
 
   // ---- loads, straight to LDS. Rows behind the last lie behind the end that the loads are told and come as zeros; so do whole chunks (the number of
@@ -347,9 +349,9 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 
   // ---- the state: lane (h, col) has column 32 wave + col, in element 4 j + i of tile m the row 32 m + 16 (j / 2) + 8 h + 4 (j % 2) + i
   f32x16 S[MT];
-  const size_t part = (OUT ? (size_t)A.by_part.of(piece.begin) + piece.b + (size_t)piece.index * A.parts : (size_t)number) * A.Hkv + g, part_at = part * D * D;
-  // (Heads of a group start from a copy of a sequence's state: the one that writes the state behind its rows may be done before another begins.)
-  const bool carried = A.part && (OUT ? segments > 1 || A.G > 1 : A.out || len > A.part_rows);
+  const size_t part = (size_t)number * A.Hkv + g, part_at = part * D * D;
+  // (Workgroups of one group start from a copy of a sequence's state: the one that writes the state behind its rows may be done before another begins.)
+  const bool carried = A.part && (segments > 1 || (OUT && A.G > HEADS));
   const float *from = carried ? (OUT ? A.part + part_at : nullptr) : state_in(A, piece.b);
   if (!carried && from) from += (size_t)g * D * D;
   const int s_at = 8 * h * D + 32 * wave + col, p_at = 256 * wave + 4 * lane;
@@ -710,7 +712,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 }
 
 // Along each sequence of several segments: the state before every segment takes the place of what the segment adds. A thread has four numbers, and asks for
-// those of eight parts at once. Memory bounds it: 15 segments of 32 heads, 64 MB, 14 us (4.6 TB/s).
+// those of eight segments at once. Memory bounds it: 15 segments of 32 heads, 64 MB, 14 us (4.6 TB/s).
 template <int D>
 __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
   constexpr int PER = D * D / 1024;      // workgroups for a state
@@ -719,19 +721,19 @@ __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
   int begin, len;
   seq_rows(A.seqs, b, begin, len);
   len = rows_of(A, b, len);
-  // (what the sums' kernel leaves: the parts before the last segment, or all of a sequence with several of them)
-  const int segments = max((len + A.segment - 1) / A.segment, 1), all = max((len + A.part_rows - 1) / A.part_rows, 1);
-  if (A.out ? segments < 2 && A.G == 1 : all < 2) return;
-  const int sums = A.out ? (segments - 1) * A.parts : all, stop = A.out ? sums + 1 : all;
+  // (what the sums' kernel leaves: the segments before the last, or all of a sequence with several of them where there are no results)
+  const int segments = max((len + A.segment - 1) / A.segment, 1);
+  if (segments < 2 && !(A.out && A.G > A.heads)) return;
+  const int sums = A.out ? segments - 1 : segments;
   const float *from = state_in(A, b);
   f32x4 S = {0.f, 0.f, 0.f, 0.f};
   if (from) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) S[i] = from[(size_t)g * D * D + place + i * D];
   }
-  const size_t first = ((size_t)A.by_part.of(begin) + b) * A.Hkv + g;
+  const size_t first = ((size_t)A.by_segment.of(begin) + b) * A.Hkv + g;
   constexpr int AT_ONCE = 8;
-  for (int i0 = 0, next = 0; i0 < stop; i0 += AT_ONCE) {
+  for (int i0 = 0; i0 < segments; i0 += AT_ONCE) {
     f32x4 own[AT_ONCE];
     float f[AT_ONCE];
 #pragma unroll
@@ -742,10 +744,7 @@ __global__ void __launch_bounds__(256) linear_carry_kernel(const LinearArgs A) {
     }
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
-      if (A.out && i0 + i == next && next < stop) {
-        *reinterpret_cast<f32x4 *>(A.part + (first + (size_t)next * A.Hkv) * D * D + at) = S;
-        next += A.parts;
-      }
+      if (A.out && i0 + i < segments) *reinterpret_cast<f32x4 *>(A.part + (first + (size_t)(i0 + i) * A.Hkv) * D * D + at) = S;
       S = S * f[i] + own[i];
     }
   }
@@ -776,7 +775,7 @@ hipError_t launch_linear_step(const LinearArgs &a, int d, hipStream_t s) {
 
 template <int D, bool OUT, int HEADS>
 static hipError_t launch_chunks(const LinearArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)(OUT ? a.numbers : a.part_numbers) * a.Hkv + STS_XCDS - 1) / STS_XCDS * STS_XCDS * (OUT ? a.G / HEADS : 1))), block(2 * D);
+  const dim3 grid((unsigned)(((int64_t)a.numbers * a.Hkv + STS_XCDS - 1) / STS_XCDS * STS_XCDS * (OUT ? a.G / HEADS : 1))), block(2 * D);
   STS_LAUNCH((linear_chunk_kernel<D, OUT, HEADS>), grid, block, 0, s, a);
   return sts_take_launch_status();
 }

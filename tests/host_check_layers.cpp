@@ -49,18 +49,17 @@ static void check_linear(const LinearArgs &a, int d) {
 static void check_chunks(const LinearArgs &a, int d) {
   check_linear(a, d);
   if (a.max_len <= STS_LINEAR_STEP) fail("chunks: few rows");
-  if (a.parts < 1 || a.part_rows * a.parts != a.segment || a.part_rows % STS_LINEAR_CHUNK) fail("chunks: segments");
-  if (a.numbers != (int64_t)a.seqs.T / a.segment + a.seqs.B || a.part_numbers != (int64_t)a.seqs.T / a.part_rows + a.seqs.B) fail("chunks: numbers");
-  if ((int64_t)a.numbers * a.Hq >= 1 << 24 || (int64_t)a.part_numbers * a.Hkv >= 1 << 24) fail("chunks: grid");
+  if (a.segment < STS_LINEAR_CHUNK || a.segment % STS_LINEAR_CHUNK || a.numbers != (int64_t)a.seqs.T / a.segment + a.seqs.B) fail("chunks: segments");
+  if ((int64_t)a.numbers * a.Hq >= 1 << 24 || a.heads < 1 || a.heads > 2 || a.G % a.heads) fail("chunks: grid");
+  check_divisor(a.by_turns, a.G / a.heads, "chunks: by_turns");
   if (31 * a.q_stride_n * 2 + 2 * d > 0x7fffffff || 31 * a.kv_stride_n * 2 + 2 * d > 0x7fffffff) fail("chunks: offsets beyond 31 bits");
   check_divisor(a.by_segment, a.segment, "chunks: by_segment");
-  check_divisor(a.by_part, a.part_rows, "chunks: by_part");
   if (a.part) {
-    in_ws(a.part, (size_t)a.part_numbers * a.Hkv * d * d * 4, "chunks: part");
-    in_ws(a.part_log, (size_t)a.part_numbers * a.Hkv * 8, "chunks: part_log");
+    in_ws(a.part, (size_t)a.numbers * a.Hkv * d * d * 4, "chunks: part");
+    in_ws(a.part_log, (size_t)a.numbers * a.Hkv * 8, "chunks: part_log");
   }
-  // what any kernel may hand on has a place: several segments, the heads of a group, several parts where there are no results
-  if (!a.part && (a.out ? a.max_len > a.segment || a.G > 1 : a.max_len > a.part_rows)) fail("chunks: nowhere for states to go");
+  // what any kernel may hand on has a place: several segments, the heads of a group
+  if (!a.part && (a.max_len > a.segment || (a.out && a.G > a.heads))) fail("chunks: nowhere for states to go");
 }
 hipError_t launch_linear_step(const LinearArgs &a, int d, hipStream_t) {
   ++g_steps;
