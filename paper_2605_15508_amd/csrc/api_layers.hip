@@ -45,8 +45,8 @@ sts_status plan_linear(const sts_linear_params *p, LinearPlan &pl) {
   pl.each = p->B > 0 ? p->T / p->B : 0;
   pl.max_len = !p->starts ? pl.each : p->max_len == 0 || p->max_len > p->T ? p->T : p->max_len;
   // Row by row up to 16 rows, by chunks (of 32, whose time hardly depends on how many rows there are) behind that. 16 rows in us, row by row and by
-  // chunks: one sequence with groups of four heads 11.7 and 12.4, without groups 6.9 and 9.6; 8 sequences 12.8 and 16.7, 17.0 and 13.2; 64 sequences
-  // 45.6 and 73.5, 89 and 66.
+  // chunks: one sequence with groups of four heads 11.7 and 12.0, without groups 6.9 and 9.4; 8 sequences 12.7 and 16.0, 16.9 and 13.2; 64 sequences
+  // 45.6 and 51.9, 88 and 67. (8 rows of 64 sequences 29 and 51, 61 and 63.)
   pl.step = pl.max_len <= STS_LINEAR_STEP;
   if ((int64_t)p->B * p->Hkv * (p->d * p->d / 1024) >= MOST_GROUPS) return STS_EUNSUPPORTED;
   if (pl.step) return STS_OK;
