@@ -455,7 +455,7 @@ typedef struct {
  * States lie in pools of slots [num_slots][Hkv][d (K's channel)][d (V's)], state_stride elements from slot to slot: sequence b starts from slot
  * slots[b] of `state` (slots NULL: b) and its state behind its last row goes to slot slots_out[b] of `state_out`. Without `state`, or with a
  * slot outside the pool (-1, for instance), a sequence starts from zeros; without state_out, or with such a slot, its state is not kept. Both
- * pools may be one, and a sequence's two slots the same; else no slot may be read or written by one sequence and written by another of the
+ * pools may be one, and a sequence's two slots the same (in place with `slots`, slots_out has to be given as well: NULL is slot b here, too); else no slot may be read or written by one sequence and written by another of the
  * same call: what it then holds is not defined. A sequence without rows has its state copied.
  * lens (optional): only the first lens[b] rows of sequence b count. So a verification block is one call with out and without state_out, and
  * once it is known how many rows were accepted, a second with lens, state_out, and q and out NULL.

@@ -812,13 +812,31 @@ def _state_pool(pool, slots, B, Hkv, d, dev):
     return _list_ptr(pool), pool.stride(0) if pool.shape[0] > 1 else Hkv * d * d, _per_batch(slots, B, dev), pool.shape[0]
 
 
+def _slots_behind(state, slots, state_out, B):
+    """The slots that the states behind the rows go to where the caller names none: those that were read where both pools are one (whatever tensor
+    objects name it: two slices of a wider pool are one, too), else the sequences' numbers, which must be no places that another sequence reads."""
+    if state is None or state_out is None or min(B, state.shape[0], state_out.shape[0]) == 0:
+        return None
+    at, to = state.data_ptr(), state_out.data_ptr()
+    step, step_to = state.stride(0) * 4, state_out.stride(0) * 4
+    n, size = state.shape[0] if slots is not None else B, state[0].numel() * 4
+    if at == to and (n == 1 or state_out.shape[0] == 1 or step == step_to):
+        if slots is None or state.shape == state_out.shape:
+            return slots
+    step = max(step, size)
+    meets = lambda x: any(0 <= i < n and abs(at + i * step - x) < size for i in ((x - at) // step, (x - at) // step + 1))  # noqa: E731
+    apart = to >= at + (n - 1) * step + size or at >= to + (B - 1) * step_to + size
+    assert apart or not any(meets(to + b * step_to) for b in range(B)), "state_out lies in the pool that states are read from: slots_out says which slots are written"
+    return None
+
+
 def sts_linear_attn(q, k, v, decay, scale=1.0, starts=None, lens=None, max_len=None, state=None, slots=None, state_out=None, slots_out=None,
                     out=None, out_dtype=None, workspace=None, prepare=False):
     """Linear attention with a decay for each head -> (out, state_out). Packed: q [T,Hq,d], k/v [T,Hkv,d] bf16 (rows and heads strided ok), starts
     [B+1] int32 (device), max_len the longest sequence's rows if known (host; None: T). Or B sequences of the same length without starts: q
     [B,n,Hq,d], k/v [B,n,Hkv,d], whose rows can be viewed as packed ones. decay: fp32 logarithms, [Hkv] or one per row and KV head. state and
-    state_out [slots,Hkv,d,d] fp32 pools, slots and slots_out [B] int32 (None: sequence b has slot b; slots_out None also where state_out is state
-    and slots is given: the same slots). lens [B]: rows that count. q None: states only, out is None. Rows of no sequence, and those behind
+    state_out [slots,Hkv,d,d] fp32 pools, slots and slots_out [B] int32 (None: sequence b has slot b; slots_out None where both pools
+    are the same memory and slots is given: the same slots; where they overlap otherwise and a written slot might be one that is read, slots_out has to be given). lens [B]: rows that count. q None: states only, out is None. Rows of no sequence, and those behind
     lens, stay as they are in `out`. prepare=True returns a PreparedCall. See sts_linear_attn in include/sts.h."""
     import torch
 
@@ -848,9 +866,10 @@ def sts_linear_attn(q, k, v, decay, scale=1.0, starts=None, lens=None, max_len=N
     else:
         assert out is None
     assert decay.device == dev and decay.dtype == torch.float32 and decay.is_contiguous() and tuple(decay.shape) in ((Hkv,), (T, Hkv))
-    if state_out is not None and state_out is state and slots_out is None:
-        slots_out = slots
     sp, ss, sl, sn = _state_pool(state, slots, B, Hkv, d, dev)
+    if slots_out is None:
+        _state_pool(state_out, None, B, Hkv, d, dev)
+        slots_out = _slots_behind(state, slots, state_out, B)
     op, os_, ol, on = _state_pool(state_out, slots_out, B, Hkv, d, dev)
     p = LinearParams(B=B, T=T, max_len=0 if max_len is None else _i32(max_len), Hq=Hq, Hkv=Hkv, d=d, q=None if q is None else _list_ptr(q), k=_ptr(k), v=_ptr(v),
                      q_stride_n=qn, q_stride_h=qh, kv_stride_n=kn, kv_stride_h=kh, decay=_ptr(decay), decay_rows=1 if decay.dim() == 2 else 0,

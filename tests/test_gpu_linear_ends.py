@@ -1,0 +1,38 @@
+"""sts_linear_attn where it can go wrong at the ends of what it takes: pools named by several tensors, values, scales and states far from 1, against
+the recurrence in 64 bits within bounds derived from the roundings (layers_util.linear)."""
+import math
+
+import pytest
+import torch
+
+import paper_2605_15508_amd as sts
+from layers_util import check_linear, linear, starts_of
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def data(n, Hq, Hkv, d, seed, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    q, k, v = (torch.randn(n, h, d, generator=g) for h in (Hq, Hkv, Hkv))
+    return q.to(torch.bfloat16), k.to(torch.bfloat16), (v * size).to(torch.bfloat16), torch.rand(n, Hkv, generator=g)
+
+
+@pytest.mark.parametrize("n", [5, 70])
+def test_in_place_through_two_slices_of_a_pool(n):
+    """A layer's states out of a wider pool, sliced anew for each argument: the sequences' own slots are written, and no others."""
+    B, Hkv, d = 2, 2, 64
+    q, k, v, r = data(B * n, 4, Hkv, d, 1)
+    decay = -0.1 * r
+    wide = torch.randn(3, 6, 2 * Hkv, d, d, generator=torch.Generator().manual_seed(2)).to(DEV)
+    before = wide.clone()
+    slots = torch.tensor([4, 1], dtype=torch.int32, device=DEV)
+    out, _ = sts.sts_linear_attn(q.to(DEV), k.to(DEV), v.to(DEV), decay.to(DEV), 0.1, starts=starts_of([n, n]).to(DEV), max_len=n, state=wide[1, :, Hkv:], slots=slots,
+                                 state_out=wide[1, :, Hkv:], out_dtype=torch.float32)
+    for b, s in enumerate((4, 1)):
+        at = slice(b * n, b * n + n)
+        ref, all_s, e, e_s = linear(q[at], k[at], v[at], decay[at], 0.1, before[1, s, Hkv:].cpu(), n > 16)
+        check_linear(out[at], ref, e, f"sequence {b}")
+        check_linear(wide[1, s, Hkv:], all_s[-1], e_s[-1], f"state {b}")
+        wide[1, s, Hkv:] = before[1, s, Hkv:]
+    assert torch.equal(wide, before)
