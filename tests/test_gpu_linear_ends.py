@@ -36,3 +36,25 @@ def test_in_place_through_two_slices_of_a_pool(n):
         check_linear(wide[1, s, Hkv:], all_s[-1], e_s[-1], f"state {b}")
         wide[1, s, Hkv:] = before[1, s, Hkv:]
     assert torch.equal(wide, before)
+
+
+def spread(r, bits):
+    """Decays that make up 2^-bits a chunk of 32 rows, by a tenth more or less for each row."""
+    return -bits * math.log(2) / 32 * (0.9 + 0.2 * r)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", [5, 20, 29, 31, 40, 50, 59, 65])
+@pytest.mark.parametrize("size", [1.0, 1e-20])
+def test_small_values_and_strong_decays(size, bits, d):
+    """Seven chunks, so that the factor that the state is held by takes many values. Nothing is added to the bound: sums on the way are at most 2^46
+    smaller than the results, 2^-112 for these values, where fp32's numbers of less than 2^-126 still have steps of 2^-149."""
+    n, Hkv = 224, 2
+    q, k, v, r = data(n, 4, Hkv, d, 3, size)
+    decay = spread(r, bits)
+    first = torch.randn(1, Hkv, d, d, generator=torch.Generator().manual_seed(4)) * size
+    out, S = sts.sts_linear_attn(q.to(DEV), k.to(DEV), v.to(DEV), decay.to(DEV), 0.1, starts=starts_of([n]).to(DEV), max_len=n, state=first.to(DEV),
+                                 state_out=torch.empty(1, Hkv, d, d, device=DEV), out_dtype=torch.float32)
+    ref, all_s, e, e_s = linear(q, k, v, decay, 0.1, first[0], True)
+    check_linear(out, ref, e, f"{size} {bits}")
+    check_linear(S[0], all_s[-1], e_s[-1], f"{size} {bits} state")
