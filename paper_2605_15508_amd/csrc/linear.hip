@@ -404,12 +404,14 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   // so that each key has one weight, which the state takes too. Not where a chunk's decays make up 2^-30 or less, a row's doubles the state or a decay is
   // no number: in such a chunk (`apart`) each pair's weight is worked out, which takes the results' kernel a quarter longer (8192 rows with 32 heads 120 us in all
   // without such chunks, 135 with none but such). Sums in a chunk that is not apart are smaller than the results by up to u F, 2^46: from 2^-60 on, 2^76, results of
-  // values of 1e-20 were lost in fp32's smallest numbers.
+  // values of 1e-20 were lost in fp32's smallest numbers. With a scale beyond 2^48, whose product with u F could leave
+  // fp32's range (u F is up to 2^78 where decays are above 0), every chunk is one such.
   // The state is held as S / F with 1 <= F < 2^16: F is the decays' product so far but for a power of 2^16, by which the state is multiplied
   // where F would leave that range (exactly), and a key's weight is divided by F. F's logarithm `low` is a sum in 64 bits: no factor's rounding adds up
   // over a long sequence.
   // A chunk has the power of two, apart (1) or not (0), the logarithm of F before it, and 1 where a row doubles the state.
   double all = 0.0, low = 0.0;
+  const float weakest = __builtin_fabsf(A.scale) < 0x1p48f ? WEAKEST : INFINITY;
   const lds_ptr decays = (lds_ptr)lds_d;
   auto number_of = [&](int at) { return *(lds_f32)(decays + at); };
   auto work_out = [&](int base) {
@@ -438,14 +440,14 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
     const double low_before = before - whole(before), low_behind = behind - whole(behind);
     const float F = exp2_32(low_behind), F_inv = exp2_32(-low_behind), step = __builtin_amdgcn_exp2f((float)(whole(behind) - whole(before)));
     low = lane_of(low - whole(low), 0);        // (the same in all lanes, and so in scalar registers)
-    *(__attribute__((address_space(3))) f32x4 *)(decays + AT_CHUNK + 16 * mine) = f32x4{step, end >= WEAKEST && grows == 0.f ? 0.f : 1.f, (float)low_before, grows};
+    *(__attribute__((address_space(3))) f32x4 *)(decays + AT_CHUNK + 16 * mine) = f32x4{step, end >= weakest && grows == 0.f ? 0.f : 1.f, (float)low_before, grows};
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
       const int chunk = wave + i * NW, row = (base + chunk) * C, at = chunk * C * 4;
       auto of_chunk = [&](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), min(chunk, BLOCK - 1))); };
       const float factor = of_chunk(F), inverse = of_chunk(F_inv), c_end = of_chunk(end);
       *(lds_f32)(decays + AT_KEY + at + 4 * col) = row + col < rows ? __builtin_amdgcn_exp2f(after[i]) * inverse : 0.f;
-      *(lds_f32)(decays + AT_QUERY + at + 4 * col) = A.scale * (c_end >= WEAKEST && of_chunk(grows) == 0.f ? factor * __builtin_amdgcn_exp2f(c[i] - c_end) : 1.f);
+      *(lds_f32)(decays + AT_QUERY + at + 4 * col) = A.scale * (c_end >= weakest && of_chunk(grows) == 0.f ? factor * __builtin_amdgcn_exp2f(c[i] - c_end) : 1.f);
     }
     all_waves();
   };

@@ -58,3 +58,21 @@ def test_small_values_and_strong_decays(size, bits, d):
     ref, all_s, e, e_s = linear(q, k, v, decay, 0.1, first[0], True)
     check_linear(out, ref, e, f"{size} {bits}")
     check_linear(S[0], all_s[-1], e_s[-1], f"{size} {bits} state")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", [0, 5, 29, 50])
+@pytest.mark.parametrize("scale,size", [(1e14, 1.0), (1e25, 1.0), (1e30, 1.0), (-1e38, 1e-20), (1e-30, 1e20)])
+def test_scales_of_all_sizes(scale, size, bits, d):
+    """A factor of the results is multiplied with the scale: the product must not leave fp32's range where results do not."""
+    n, Hkv = 100, 2
+    q, k, v, r = data(n, 4, Hkv, d, 5, size)
+    decay = spread(r, bits)
+    out, _ = sts.sts_linear_attn(q.to(DEV), k.to(DEV), v.to(DEV), decay.to(DEV), scale, starts=starts_of([n]).to(DEV), max_len=n, out_dtype=torch.float32)
+    ref, _, e, _ = linear(q, k, v, decay, scale, torch.zeros(Hkv, d, d), True)
+    assert ref.abs().max() < 1e38 * 3
+    check_linear(out, ref, e, f"{scale}")
+    blocks = [t[:9].view(1, 9, *t.shape[1:]).to(DEV) for t in (q, k, v, decay)]
+    out, _ = sts.sts_linear_attn(*blocks, scale, out_dtype=torch.float32)
+    ref, _, e, _ = linear(q[:9], k[:9], v[:9], decay[:9], scale, torch.zeros(Hkv, d, d), False)
+    check_linear(out[0], ref, e, f"{scale} row by row")
