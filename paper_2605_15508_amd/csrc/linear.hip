@@ -402,8 +402,8 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
   // ---- Decays, in powers of two: c_i the sum over the chunk's rows up to i. With u_i = exp(c_i - c_32)
   //     out_i = scale u_i (q_i . (exp(c_32) S) + sum exp(c_32 - c_j) (q_i . k_j) v_j),
   // so that each key has one weight, which the state takes too. Not where a chunk's decays make up 2^-30 or less, a row's doubles the state or a decay is
-  // no number: in such a chunk (`apart`) each pair's weight is worked out, which takes the results' kernel a quarter longer (8192 rows with 32 heads 120 us in all
-  // without such chunks, 135 with none but such). Sums in a chunk that is not apart are smaller than the results by up to u F, 2^46: from 2^-60 on, 2^76, results of
+  // no number: in such a chunk (`apart`) each pair's weight is worked out, which takes the results' kernel a quarter to a third longer (8192 rows with 32
+  // heads 119 us in all without such chunks, 134 with none but such; six prompts in groups of four heads 103 and 125). Sums in a chunk that is not apart are smaller than the results by up to u F, 2^46: from 2^-60 on, 2^76, results of
   // values of 1e-20 were lost in fp32's smallest numbers. With a scale beyond 2^48, whose product with u F could leave
   // fp32's range (u F is up to 2^78 where decays are above 0), every chunk is one such.
   // The state is held as S / F with 1 <= F < 2^16: F is the decays' product so far but for a power of 2^16, by which the state is multiplied
@@ -557,7 +557,30 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (to_state && apart) multiply(f);
+      // Where decays are strong, q . S may leave fp32's range though what they leave of it does not: then it is made from S 2^-32.
+      float unscale = 1.f;
+      if (apart) {
+        if constexpr (OUT) {
+          float z[2] = {0.f, 0.f};             // 0 times the products: 0, or no number
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[e % 2] = __builtin_fmaf(O[e], 0.f, z[e % 2]);
+          if (__builtin_amdgcn_ballot_w64(z[0] + z[1] != 0.f) != 0) {
+            unscale = 0x1p32f;
+            int at = r_lane;
+            asm("" : "+v"(at));
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+              u32x4 w;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{S[s / 2][8 * (s % 2) + 2 * e] * 0x1p-32f, S[s / 2][8 * (s % 2) + 2 * e + 1] * 0x1p-32f}), bf16x2));
+              const f32x16 zero = {};
+              O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, *(lds_u32x4)((lds_ptr)(lds + AT_Q + hh * TILE) + (at ^ (32 * s)))), s ? O : zero, 0, 0, 0);
+              __builtin_amdgcn_sched_barrier(0);         // (one operand's registers at a time)
+            }
+          }
+        }
+        if (to_state) multiply(f);
+      }
 
       // ---- The state, and the weights of the chunk's rows, as bf16 (half a step, 2^-8 of each): none for keys behind the query, whatever their
       // product is. (Worked out without a look at `apart` and `odd`, and once more where one of them holds.)
@@ -603,7 +626,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
         }
         __builtin_amdgcn_sched_barrier(0);
         if (apart || odd) {
-          const float c = *(lds_f32)(mine + 4 * col), own = apart ? exp2_32((double)four[2] + c) : 1.f;
+          const float c = *(lds_f32)(mine + 4 * col), own = apart ? exp2_32((double)four[2] + c) * unscale : 1.f;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float pair = __builtin_amdgcn_exp2f(c - *(lds_f32)(mine + 4 * (8 * (e >> 2) + 4 * h + (e & 3))));

@@ -76,3 +76,19 @@ def test_scales_of_all_sizes(scale, size, bits, d):
     out, _ = sts.sts_linear_attn(*blocks, scale, out_dtype=torch.float32)
     ref, _, e, _ = linear(q[:9], k[:9], v[:9], decay[:9], scale, torch.zeros(Hkv, d, d), False)
     check_linear(out[0], ref, e, f"{scale} row by row")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,at", [(9, 4), (100, 0), (100, 40), (1000, 700)])
+def test_minus_infinity_forgets_states_of_any_size(n, at, d):
+    """From row `at` on results and state are those of a sequence that begins there."""
+    Hkv = 2
+    q, k, v, r = data(n, 4, Hkv, d, 6, 1e-10)
+    decay = -0.05 * r
+    decay[at] = -math.inf
+    first = torch.full((1, Hkv, d, d), 3e38)
+    out, S = sts.sts_linear_attn(q.to(DEV), k.to(DEV), v.to(DEV), decay.to(DEV), 0.1, starts=starts_of([n]).to(DEV), max_len=n, state=first.to(DEV),
+                                 state_out=torch.empty(1, Hkv, d, d, device=DEV), out_dtype=torch.float32)
+    ref, all_s, e, e_s = linear(q[at:], k[at:], v[at:], decay[at:], 0.1, torch.zeros(Hkv, d, d), n > 16)
+    check_linear(out[at:], ref, e)
+    check_linear(S[0], all_s[-1], e_s[-1], "state")
