@@ -43,14 +43,15 @@ def spread(r, bits):
     return -bits * math.log(2) / 32 * (0.9 + 0.2 * r)
 
 
+@pytest.mark.parametrize("Hq", [2, 4])          # one head to a workgroup, or two
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("bits", [5, 20, 29, 31, 40, 50, 59, 65])
 @pytest.mark.parametrize("size", [1.0, 1e-20])
-def test_small_values_and_strong_decays(size, bits, d):
+def test_small_values_and_strong_decays(size, bits, d, Hq):
     """Seven chunks, so that the factor that the state is held by takes many values. Nothing is added to the bound: sums on the way are at most 2^46
     smaller than the results, 2^-112 for these values, where fp32's numbers of less than 2^-126 still have steps of 2^-149."""
     n, Hkv = 224, 2
-    q, k, v, r = data(n, 4, Hkv, d, 3, size)
+    q, k, v, r = data(n, Hq, Hkv, d, 3, size)
     decay = spread(r, bits)
     first = torch.randn(1, Hkv, d, d, generator=torch.Generator().manual_seed(4)) * size
     out, S = sts.sts_linear_attn(q.to(DEV), k.to(DEV), v.to(DEV), decay.to(DEV), 0.1, starts=starts_of([n]).to(DEV), max_len=n, state=first.to(DEV),
@@ -60,13 +61,14 @@ def test_small_values_and_strong_decays(size, bits, d):
     check_linear(S[0], all_s[-1], e_s[-1], f"{size} {bits} state")
 
 
+@pytest.mark.parametrize("Hq", [2, 4])          # one head to a workgroup, or two
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("bits", [0, 5, 29, 50])
 @pytest.mark.parametrize("scale,size", [(1e14, 1.0), (1e25, 1.0), (1e30, 1.0), (-1e38, 1e-20), (1e-30, 1e20)])
-def test_scales_of_all_sizes(scale, size, bits, d):
+def test_scales_of_all_sizes(scale, size, bits, d, Hq):
     """A factor of the results is multiplied with the scale: the product must not leave fp32's range where results do not."""
     n, Hkv = 100, 2
-    q, k, v, r = data(n, 4, Hkv, d, 5, size)
+    q, k, v, r = data(n, Hq, Hkv, d, 5, size)
     decay = spread(r, bits)
     out, _ = sts.sts_linear_attn(q.to(DEV), k.to(DEV), v.to(DEV), decay.to(DEV), scale, starts=starts_of([n]).to(DEV), max_len=n, out_dtype=torch.float32)
     ref, _, e, _ = linear(q, k, v, decay, scale, torch.zeros(Hkv, d, d), True)
@@ -78,12 +80,13 @@ def test_scales_of_all_sizes(scale, size, bits, d):
     check_linear(out[0], ref, e, f"{scale} row by row")
 
 
+@pytest.mark.parametrize("Hq", [2, 4])          # one head to a workgroup, or two
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n,at", [(9, 4), (100, 0), (100, 40), (1000, 700)])
-def test_minus_infinity_forgets_states_of_any_size(n, at, d):
+def test_minus_infinity_forgets_states_of_any_size(n, at, d, Hq):
     """From row `at` on results and state are those of a sequence that begins there."""
     Hkv = 2
-    q, k, v, r = data(n, 4, Hkv, d, 6, 1e-10)
+    q, k, v, r = data(n, Hq, Hkv, d, 6, 1e-10)
     decay = -0.05 * r
     decay[at] = -math.inf
     first = torch.full((1, Hkv, d, d), 3e38)
