@@ -432,7 +432,8 @@ sts_status sts_window_attn(const sts_window_params *p, void *stream);
  * sts_prompt_attn -- causal attention over whole prompts: query row i of a sequence sees the keys 0 .. i of its sequence,
  *     s_j = scale * <Q[i,t,:], K[j,g,:]>,   out[i,t,:] = sum_j exp(s_j - lse) V[j,g,:],   lse[t,i] = ln sum_j exp(s_j)
  * with g = t / (Hq/Hkv). What a row does not see never reaches its result, NaN and infinities included; a row that sees a key with NaN is NaN, its
- * lse -inf. Weights enter the second product as bf16, sums and statistics are fp32. No workspace.
+ * lse -inf. Weights enter the second product as bf16, sums and statistics are fp32. No workspace. Rows see the keys of this call alone: the parts of a prompt
+ * whose beginning is in a cache already go through sts_window_attn, with a window of all tokens.
  */
 typedef struct {
   int32_t B, T, Hq, Hkv, d;
@@ -461,8 +462,9 @@ typedef struct {
  * once it is known how many rows were accepted, a second with lens, state_out, and q and out NULL.
  *
  * starts NULL: T / B rows for each sequence. max_len (0: T) is the length of the longest sequence: rows of a sequence behind it are left out.
- * With max_len <= 16 the recurrence is worked out row by row in fp32. Else by chunks of rows: k^T v enters the state as in fp32, while
- * the weights of a chunk's rows and the state (as the operand of q^T S alone) are rounded to bf16.
+ * With max_len <= 16 the recurrence is worked out row by row in fp32, and results are right to fp32. Else by chunks of 32 rows: k^T v enters the state as in
+ * fp32, while the weights of a chunk's rows and the state (as the operand of q^T S alone) are rounded to bf16 (2^-8 of each). There values and states of less than
+ * 1e-20 may lose bits, and decays that come to less than 2^-112 within a chunk forget all that was before them, of whatever size.
  * Values of v that are infinite or NaN do not reach rows before their own; from there on results and state that depend on them are NaN or
  * infinite. The workspace's size depends on the integer fields and on whether starts and out are NULL.
  */

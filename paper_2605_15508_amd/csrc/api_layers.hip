@@ -44,16 +44,18 @@ sts_status plan_linear(const sts_linear_params *p, LinearPlan &pl) {
   if (p->max_len < 0 || (!p->starts && p->B > 0 && p->T % p->B != 0)) return STS_EINVAL;
   pl.each = p->B > 0 ? p->T / p->B : 0;
   pl.max_len = !p->starts ? pl.each : p->max_len == 0 || p->max_len > p->T ? p->T : p->max_len;
-  // Row by row up to 16 rows, by chunks (of 32, whose time hardly depends on how many rows there are) behind that. 16 rows in us, row by row and by
-  // chunks: one sequence with groups of four heads 11.7 and 12.0, without groups 6.9 and 9.4; 8 sequences 12.7 and 16.0, 16.9 and 13.2; 64 sequences
-  // 45.6 and 51.9, 88 and 67. (8 rows of 64 sequences 29 and 51, 61 and 63.)
+  // Row by row up to 16 rows, by chunks (of 32, whose time hardly depends on how many rows there are) behind that. 16 rows of 32 heads in us, row by row
+  // and by chunks: 8 sequences with groups of four heads 12.8 and 15.9, without groups 16.8 and 12.9; 64 sequences 44.8 and 53.6, 93 and 72; 12 rows of 64
+  // 37.4 and 57.3, 80 and 72; 8 rows 29.2 and 52.8, 67 and 71. So batches without groups lose up to a quarter between 10 and 16 rows. They stay row by row, too: a
+  // block's results are right to fp32 then, whatever the batch beside it, where those of chunks hold weights and states as bf16.
   pl.step = pl.max_len <= STS_LINEAR_STEP;
   if ((int64_t)p->B * p->Hkv * (p->d * p->d / 1024) >= MOST_GROUPS) return STS_EUNSUPPORTED;
   if (pl.step) return STS_OK;
-  // Segments: as many as the chip runs workgroups at once, two on a compute unit (four of half the waves), counting half a one more for each sequence
-  // (its last), but of 128 rows at least. (32 heads: 8192 rows take 115 us, with twice as many segments 135, with half as many 118; in groups of four
-  // six prompts of 77 to 6000 rows 173, with three quarters as many 189, with half as many 258.) With many sequences, as many as cut those of twice the
-  // average length. Two heads of a group go to one workgroup where groups are even.
+  // Segments: as many as the chip runs workgroups at once, two on a compute unit (four of half the waves), less half a one for each sequence (its last is
+  // not whole), but no fewer than half as many, and of 128 rows at least. In us, with so many, twice, three quarters and half as many: 8192 rows with 32 heads 119,
+  // 144, 127, 117; six prompts of 77 to 6001 rows, 32 heads in groups of four, 90, 105, 100, 105, and six of 1000 to 12000 202, 213, 234, 284; sixteen
+  // of 500 to 4000 rows, 16 heads of 64, 100, 106, 107, 121. (Where the rows divide evenly a segment has a chunk more than it need have.)
+  // Two heads of a group go to one workgroup where groups are even.
   pl.heads = p->Hq / p->Hkv % 2 == 0 ? 2 : 1;
   const int64_t at_once = (int64_t)(p->d == 128 ? 2 : 4) * sts_cu_count() * pl.heads / p->Hq, left = at_once - p->B / 2 > at_once / 2 ? at_once - p->B / 2 : at_once / 2;
   int64_t segment = (p->T / (left > 0 ? left : 1) + STS_LINEAR_CHUNK) / STS_LINEAR_CHUNK * STS_LINEAR_CHUNK;

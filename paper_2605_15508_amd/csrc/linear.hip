@@ -10,10 +10,10 @@
 // products q . k by itself, so that these pass from accumulator to operand in their lane, as the state does: nothing goes through LDS but
 // rows of Q, K and V. Long sequences are cut into segments: one kernel sums up what each segment adds to the state, one
 // adds these up along the sequence, and a third starts every segment from the state before it.
-// What bounds it without groups: memory. 8192 rows with 32 heads of 128 take 117 us: sums 35 (170 MB, 4.8 TB/s), adding up 14 (64 MB), results 60
-// (300 MB, 5.0 TB/s), and what lies between three launches. With groups of heads, of which a workgroup of the
-// results has two that share a state, matrix and vector instructions, which hardly overlap: six prompts of 77 to 6001 rows, 32 heads in groups of four, 90 us, of
-// which the results 55 (with a head for each workgroup 103 and 75).
+// What bounds it without groups: memory. 8192 rows with 32 heads of 128 take 118 us: sums 35 (170 MB, 4.8 TB/s), adding up 14 (64 MB), results 60
+// (300 MB, 5.0 TB/s), and what lies between three launches; 131 us where no input is left in the cache behind the L2s from the pass before (sums 43, results 61 to 72).
+// With groups of heads, of which a workgroup of the results has two that share a state, matrix and vector instructions, which hardly overlap: six prompts of 77
+// to 6001 rows, 32 heads in groups of four, 89 us, of which the results 61 (with a head for each workgroup 103 and 75).
 #include "attn_util.h"
 #include "layers.h"
 
@@ -401,11 +401,11 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
 
   // ---- Decays, in powers of two: c_i the sum over the chunk's rows up to i. With u_i = exp(c_i - c_32)
   //     out_i = scale u_i (q_i . (exp(c_32) S) + sum exp(c_32 - c_j) (q_i . k_j) v_j),
-  // so that each key has one weight, which the state takes too. Not where a chunk's decays make up 2^-30 or less, a row's doubles the state or a decay is
+  // so that each key has one weight, which the state takes too. Not where a chunk's decays make up less than 2^-30, a row's doubles the state or a decay is
   // no number: in such a chunk (`apart`) each pair's weight is worked out, which takes the results' kernel a quarter to a third longer (8192 rows with 32
-  // heads 119 us in all without such chunks, 134 with none but such; six prompts in groups of four heads 103 and 125). Sums in a chunk that is not apart are smaller than the results by up to u F, 2^46: from 2^-60 on, 2^76, results of
-  // values of 1e-20 were lost in fp32's smallest numbers. With a scale beyond 2^48, whose product with u F could leave
-  // fp32's range (u F is up to 2^78 where decays are above 0), every chunk is one such.
+  // heads 119 us in all without such chunks, 134 with none but such; another six prompts in groups of four heads 103 and 125). Sums in a chunk that is not
+  // apart are smaller than the results by up to u F, 2^46; with 2^-60 in place of 2^-30, 2^76, results of values of 1e-20 were lost among fp32's smallest
+  // numbers. Where the scale is beyond 2^48, its product with u F could leave fp32's range (u F is up to 2^78 where decays are above 0): every chunk is apart.
   // The state is held as S / F with 1 <= F < 2^16: F is the decays' product so far but for a power of 2^16, by which the state is multiplied
   // where F would leave that range (exactly), and a key's weight is divided by F. F's logarithm `low` is a sum in 64 bits: no factor's rounding adds up
   // over a long sequence.
@@ -684,7 +684,7 @@ __global__ void __launch_bounds__(2 * D, 2) linear_chunk_kernel(const LinearArgs
             }
           }
           // At head size 64 the rows of 16 lanes do so, too: a store writes the wave's 64 bytes of 16 rows, not 32 of 32 (sixteen prompts 109.4 us without, 104.1
-          // with; at head size 128, where more waves share a row, six prompts 102.9 and 104.8).
+          // with; at head size 128, where more waves share a row, it makes no difference: 8192 rows 119 us without, 121 with, six prompts 90 and 89).
 #pragma unroll
           for (int i = 0; D == 64 && i < 4; ++i) {
             const uint32_t x = w[0][i], y = w[1][i];
