@@ -9,6 +9,7 @@ different streams never share scratch (the C interface leaves that to the caller
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Dict, Optional, Tuple
 
@@ -819,7 +820,7 @@ def _slots_behind(state, slots, state_out, B):
         return None
     at, to = state.data_ptr(), state_out.data_ptr()
     step, step_to = state.stride(0) * 4, state_out.stride(0) * 4
-    n, size = state.shape[0] if slots is not None else B, state[0].numel() * 4
+    n, size = state.shape[0] if slots is not None else B, math.prod(state.shape[1:]) * 4
     if at == to and (n == 1 or state_out.shape[0] == 1 or step == step_to):
         if slots is None or state.shape == state_out.shape:
             return slots
@@ -867,10 +868,10 @@ def sts_linear_attn(q, k, v, decay, scale=1.0, starts=None, lens=None, max_len=N
         assert out is None
     assert decay.device == dev and decay.dtype == torch.float32 and decay.is_contiguous() and tuple(decay.shape) in ((Hkv,), (T, Hkv))
     sp, ss, sl, sn = _state_pool(state, slots, B, Hkv, d, dev)
-    if slots_out is None:
-        _state_pool(state_out, None, B, Hkv, d, dev)
-        slots_out = _slots_behind(state, slots, state_out, B)
     op, os_, ol, on = _state_pool(state_out, slots_out, B, Hkv, d, dev)
+    if slots_out is None:
+        slots_out = _slots_behind(state, slots, state_out, B)
+        ol = _per_batch(slots_out, B, dev)
     p = LinearParams(B=B, T=T, max_len=0 if max_len is None else _i32(max_len), Hq=Hq, Hkv=Hkv, d=d, q=None if q is None else _list_ptr(q), k=_ptr(k), v=_ptr(v),
                      q_stride_n=qn, q_stride_h=qh, kv_stride_n=kn, kv_stride_h=kh, decay=_ptr(decay), decay_rows=1 if decay.dim() == 2 else 0,
                      starts=_ptr(starts), lens=_per_batch(lens, B, dev), scale=float(scale), state=sp, state_stride=ss, slots=sl, num_slots=sn,
